@@ -303,6 +303,74 @@ sim_status sim_schedule_noalloc(int32_t P, int32_t K, sim_variant variant, sim_d
                                 uint32_t* stale, uint32_t* seq, void* cuda_stream);
 const char* sim_noalloc_last_error(void);
 
+/* ---- operators of a parameter server for models of language-model size -------------------------------------------------
+ *
+ * The simulated server averages the first K pushes and takes a plain gradient step (Eq. 2 / Eq. 3).  The calls below are the
+ * step and the number formats of a server and its workers when the model is large: AdamW over the model's list of tensors,
+ * with the K pushes averaged on the way.  They work on the caller's DEVICE buffers and enqueue on the given stream;
+ * sim_last_error(NULL) describes a failure.
+ */
+
+/* Element types.  SIM_MXFP4: E2M1 codes, two a byte (the even element in the low half), with one scale byte per block of 32
+ * consecutive elements: 2^(byte - 127), byte 0xFF: a NaN block. */
+typedef enum { SIM_F32 = 0, SIM_BF16 = 1, SIM_F16 = 2, SIM_MXFP4 = 3 } sim_dtype;
+
+/*
+ * One parameter tensor of n elements (any n >= 0; contiguous).  All pointers are DEVICE pointers except the arrays g and
+ * g_scale themselves, which are HOST arrays of n_grads device pointers, one per push.  Pointers need only the alignment of
+ * their element type; where all of a tensor's streams start on 16-byte boundaries (8-bit states: 8 bytes, MXFP4 pushes: 4)
+ * the accesses are wide.  Tensors and their buffers must not overlap.
+ *   p       SIM_F32 or SIM_BF16, updated in place (bf16 parameters are rounded to nearest each step)
+ *   g       SIM_F32, SIM_BF16, SIM_F16, or SIM_MXFP4: ceil(n / 2) bytes of codes with ceil(n / 32) scale bytes in g_scale
+ *   m, v    32-bit states: fp32 [n] first and second moment.  8-bit states: E4M3 codes [n] of m and of sqrt(v), with
+ *           ceil(n / 32) scale bytes each in m_scale and v_scale (2^(byte - 127)).  Zeros (codes and scales) are the start.
+ *   shadow  optional bf16 copy of p, written each step (p SIM_F32): what workers fetch
+ */
+typedef struct {
+  int64_t n;
+  sim_dtype p_type, g_type;
+  void* p;
+  const void* const* g;
+  const uint8_t* const* g_scale;
+  void* m;
+  void* v;
+  uint8_t* m_scale;
+  uint8_t* v_scale;
+  void* shadow;
+  float weight_decay;
+} sim_adamw_tensor;
+
+typedef struct sim_adamw sim_adamw;   /* opaque; holds tables only, no state: buffers stay the caller's */
+
+/*
+ * Binds a list of tensors with n_grads push buffers each on the current device.  state_bits is 32 or 8.  Allocates and fills
+ * the tables (waits for the copy); no later call allocates or waits.  Errors: SIM_ERR_ARG for an empty list, n_grads outside
+ * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps not finite or not > 0, a tensor with missing or misaligned
+ * pointers or unknown types; SIM_ERR_ALLOC / SIM_ERR_CUDA otherwise.  *out is NULL on failure.
+ */
+sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, int32_t n_grads, int32_t state_bits, double beta1,
+                            double beta2, double eps, uint64_t seed, sim_adamw** out);
+
+/*
+ * Step t (1, 2, ...; below 2^32) of every tensor, with the first K of its push buffers, in order:
+ *   g = (grad_scale / K) sum_{l<K} g_l,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
+ * 8-bit states: the step uses m and v in fp32; what is kept is rounded stochastically, with 16-bit numbers from
+ * Philox4x32-10 (key = seed; counter = (element / 8, tag 2, t, index in the list)), so the same calls give the same bits
+ * whatever else runs.  A positive sqrt(v) is never kept as zero.  A gradient that is not finite makes its element's states
+ * (8 bits: its block's) NaN.  Elements outside [0, n) are neither read nor written.  Enqueues one launch per combination of
+ * parameter and gradient type on cuda_stream (a stream of the handle's device); the handle is only read, so steps of
+ * different handles may overlap.
+ */
+sim_status sim_adamw_step(const sim_adamw* h, int64_t t, float lr, float grad_scale, int32_t K, void* cuda_stream);
+
+/* The same with t and lr read from DEVICE memory when the step runs, for steps captured in a CUDA graph: the caller advances
+ * *t (>= 1) before each replay. */
+sim_status sim_adamw_step_device(const sim_adamw* h, const int64_t* t, const float* lr, float grad_scale, int32_t K, void* cuda_stream);
+
+/* Waits for the device and frees the tables. */
+void sim_adamw_destroy(sim_adamw* h);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,7 +23,9 @@ EXPORTS = ["sim_create", "sim_set_params", "sim_set_adasync", "sim_set_adasync_l
            "sim_trace_size", "sim_get_trace", "sim_get_params", "sim_eval_loss", "sim_error_curve", "sim_set_eval_every", "sim_risk_trace_size",
            "sim_get_risk_trace", "sim_risk_curve", "sim_risk_envelope", "sim_selftest_wait_timeout", "sim_n_params", "sim_last_error",
            "sim_destroy", "sim_draw_delays", "sim_draw_indices", "sim_simulate_host", "sim_sweep_host", "sim_schedule_noalloc",
-           "sim_noalloc_last_error"]
+           "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy"]
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # SIM_F32, SIM_BF16, SIM_F16
+MXFP4 = 3
 
 
 class SimProblem(C.Structure):
@@ -34,6 +36,12 @@ class SimProblem(C.Structure):
 
 class SimDelay(C.Structure):
     _fields_ = [("kind", C.c_int), ("mu", C.c_double), ("shift", C.c_double)]
+
+
+class SimAdamwTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("p_type", C.c_int), ("g_type", C.c_int), ("p", C.c_void_p), ("g", C.POINTER(C.c_void_p)),
+                ("g_scale", C.POINTER(C.c_void_p)), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("shadow", C.c_void_p), ("weight_decay", C.c_float)]
 
 
 class SimError(RuntimeError):
@@ -82,8 +90,13 @@ def _load():
     L.sim_schedule_noalloc.argtypes = [i32, i32, C.c_int, SimDelay, u64, i64, i32, i32, dbl, i64] + [vp] * 6
     L.sim_noalloc_last_error.argtypes = []
     L.sim_noalloc_last_error.restype = C.c_char_p
+    L.sim_adamw_create.argtypes = [C.POINTER(SimAdamwTensor), i32, i32, i32, dbl, dbl, dbl, u64, C.POINTER(vp)]
+    L.sim_adamw_step.argtypes = [vp, i64, C.c_float, C.c_float, i32, vp]
+    L.sim_adamw_step_device.argtypes = [vp, vp, vp, C.c_float, i32, vp]
+    L.sim_adamw_destroy.argtypes = [vp]
+    L.sim_adamw_destroy.restype = None
     for name in EXPORTS:
-        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error"):
+        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy"):
             getattr(L, name).restype = C.c_int
     return L
 
@@ -377,3 +390,119 @@ def sweep_host(data, runs, *, P, delay_kind, mu, shift=0.0, eta, m, seed, n_repl
                               SimDelay(DELAYS[delay_kind], mu, shift), eta, m, seed, n_replicas, replica_base,
                               hp(w0, np.float32), iters, *ptrs))
     return out
+
+
+# ---- operators of a parameter server for models of language-model size ---------------------------------------------------
+class MxTensor:
+    """A matrix [rows, cols] in MXFP4: E2M1 codes (two a byte, even element in the low half, rows padded to 128 elements) and
+    a power-of-two scale byte per block of 32 elements of a row.  layout "linear": scale bytes [rows, ceil(cols / 32)]; a
+    single row is also the form of a pushed gradient.  layout "tiles": the order the products read, 512 bytes per 128 rows x
+    4 blocks (row r of a tile at byte 16 (r % 32) + 4 (r / 32))."""
+
+    __slots__ = ("codes", "scales", "rows", "cols", "layout")
+
+    def __init__(self, codes, scales, rows, cols, layout):
+        if layout not in ("linear", "tiles"):
+            raise ValueError("layout must be 'linear' or 'tiles'")
+        blocks, pitch = -(-cols // 32), 64 * -(-cols // 128)
+        need_c = -(-cols // 2) if rows == 1 and layout == "linear" else rows * pitch
+        need_s = rows * blocks if layout == "linear" else 512 * -(-rows // 128) * -(-cols // 128)
+        for name, t, need in (("codes", codes, need_c), ("scales", scales, need_s)):
+            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < need:
+                raise ValueError("%s must be a contiguous CUDA uint8 tensor of at least %d bytes" % (name, need))
+        self.codes, self.scales, self.rows, self.cols, self.layout = codes, scales, rows, cols, layout
+
+
+def _ptr_array(pointers):
+    return (C.c_void_p * len(pointers))(*pointers)
+
+
+class AdamW:
+    """AdamW over a list of tensors, stepped by the library in one launch per combination of types.
+
+    params: CUDA tensors (float32 or bfloat16), updated in place.  grads: one list per push, each with a gradient per
+    parameter - tensors (float32, bfloat16, float16) or MxTensor of one row in the linear layout; a step averages the first K
+    pushes.  weight_decay: a number, or one per parameter.  state_bits 32 keeps fp32 moments, 8 keeps E4M3 codes of m and
+    sqrt(v) with a scale per 32 elements.  state: dict of lists ("m", "v"; 8 bits also "m_scale", "v_scale") to work on
+    instead of fresh zeros.  shadow: optional bfloat16 copies written each step.  All tensors are borrowed, contiguous and on
+    one device, must not overlap, and must stay at their addresses; this object keeps them alive."""
+
+    def __init__(self, params, grads, *, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, state=None, shadow=None,
+                 seed=0):
+        self._h = C.c_void_p()
+        params, grads = list(params), [list(g) for g in grads]
+        if not params or not grads or any(len(g) != len(params) for g in grads):
+            raise ValueError("params and at least one push with a gradient per parameter are required")
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 32 or 8")
+        self.device, self.n_grads, self.state_bits = params[0].device, len(grads), state_bits
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * len(params)
+        kinds = ("m", "v") if state_bits == 32 else ("m", "v", "m_scale", "v_scale")
+        if state is None:
+            dt = torch.float32 if state_bits == 32 else torch.uint8
+            state = {k: [torch.zeros(-(-p.numel() // 32) if k.endswith("scale") else p.numel(), dtype=dt, device=self.device) for p in params] for k in kinds}
+        if len(decay) != len(params) or (shadow is not None and len(shadow) != len(params)) or any(k not in state or len(state[k]) != len(params) for k in kinds):
+            raise ValueError("weight_decay, shadow and every list of state need one entry per parameter")
+
+        def check(t, dtypes, n, what, i):
+            if not t.is_cuda or t.device != self.device or not t.is_contiguous() or t.dtype not in dtypes or t.numel() != n:
+                raise ValueError("%s of parameter %d must be a contiguous tensor of %d elements on %s, of type %s" % (
+                    what, i, n, self.device, " or ".join(str(d) for d in dtypes)))
+            return t.data_ptr()
+
+        recs, keep = (SimAdamwTensor * len(params))(), []
+        for i, p in enumerate(params):
+            n = p.numel()
+            check(p, (torch.float32, torch.bfloat16), n, "the data", i)
+            r = recs[i]
+            r.n, r.p_type, r.p, r.weight_decay = n, DTYPES[p.dtype], p.data_ptr(), float(decay[i])
+            mine = [g[i] for g in grads]
+            if isinstance(mine[0], MxTensor):
+                for q in mine:
+                    if not isinstance(q, MxTensor) or q.rows != 1 or q.cols != n or q.layout != "linear" or q.codes.device != self.device or q.scales.device != self.device:
+                        raise ValueError("the gradients of parameter %d must all be MxTensor of one row of %d elements, linear layout, on %s" % (i, n, self.device))
+                r.g_type = MXFP4
+                arrays = _ptr_array([q.codes.data_ptr() for q in mine]), _ptr_array([q.scales.data_ptr() for q in mine])
+                r.g_scale = C.cast(arrays[1], C.POINTER(C.c_void_p))
+            else:
+                if any(isinstance(g, MxTensor) or g.dtype != mine[0].dtype for g in mine):
+                    raise ValueError("the gradients of parameter %d must have one type" % i)
+                arrays = (_ptr_array([check(g, tuple(DTYPES), n, "a gradient", i) for g in mine]),)
+                r.g_type = DTYPES[mine[0].dtype]
+            r.g = C.cast(arrays[0], C.POINTER(C.c_void_p))
+            keep.append(arrays)
+            codes = (torch.float32,) if state_bits == 32 else (torch.uint8, torch.float8_e4m3fn)
+            r.m, r.v = check(state["m"][i], codes, n, "m", i), check(state["v"][i], codes, n, "v", i)
+            if state_bits == 8:
+                r.m_scale = check(state["m_scale"][i], (torch.uint8,), -(-n // 32), "m_scale", i)
+                r.v_scale = check(state["v_scale"][i], (torch.uint8,), -(-n // 32), "v_scale", i)
+            if shadow is not None and shadow[i] is not None:
+                r.shadow = check(shadow[i], (torch.bfloat16,), n, "shadow", i)
+        self.params, self.grads, self.state, self.shadow = params, grads, state, shadow
+        with torch.cuda.device(self.device):
+            _check(lib.sim_adamw_create(recs, len(params), len(grads), state_bits, betas[0], betas[1], eps, seed, C.byref(self._h)))
+
+    def step(self, step, lr, *, K=None, grad_scale=1.0, stream=None):
+        """Step number `step` (1, 2, ...) with learning rate lr and the average of the first K pushes (default: all), on
+        `stream` (default: the device's current one).  step and lr may both be CUDA tensors of one element (int64, float32):
+        they are read when the step runs, for steps captured in a graph."""
+        st = torch.cuda.current_stream(self.device) if stream is None else stream
+        K = self.n_grads if K is None else K
+        if torch.is_tensor(step) or torch.is_tensor(lr):
+            for t, dt in ((step, torch.int64), (lr, torch.float32)):
+                if not torch.is_tensor(t) or t.device != self.device or t.dtype != dt or t.numel() != 1:
+                    raise ValueError("step and lr must both be numbers, or CUDA tensors of one int64 and one float32 on %s" % self.device)
+            _check(lib.sim_adamw_step_device(self._h, _ptr(step), _ptr(lr), grad_scale, K, _stream_ptr(st)))
+        else:
+            _check(lib.sim_adamw_step(self._h, step, lr, grad_scale, K, _stream_ptr(st)))
+
+    def close(self):
+        if self._h:
+            lib.sim_adamw_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

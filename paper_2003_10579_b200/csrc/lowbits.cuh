@@ -1,0 +1,154 @@
+// Conversions between fp32 and block-scaled 8- and 4-bit floats, device side.
+//
+// A block is 32 consecutive elements with one scale 2^k, stored as the byte k + 127 (E8M0; 0xFF: the block held an
+// infinity or a NaN and reads as NaN).  k is the smallest exponent >= -127 for which no magnitude of the block exceeds
+// L 2^k, L the format's largest value: 448 = 1.75 * 2^8 for E4M3, 6 = 1.5 * 2^2 for E2M1.  So nothing saturates and
+// every element is off by at most half a step (nearest) or less than one step (stochastic).
+//
+// Stochastic rounding takes |x| to step * floor(|x| / step + u), u = k16 / 2^16.  Below the leading bits that a format keeps,
+// an fp32 magnitude holds |x| / step's fraction; adding u at that place and clearing what lies below is that formula in
+// integer arithmetic, exactly.  Magnitudes under the format's smallest normal have a fixed step: they are moved up to it first,
+// rounding towards zero, which cannot cross the points k16 / 2^16 that the addition compares with.
+#pragma once
+#include "device_rng.cuh"
+
+namespace ssim {
+
+constexpr uint32_t ABS_MASK = 0x7FFFFFFFu, INF_BITS = 0x7F800000u;
+
+// Scale byte of a block whose largest magnitude has the bits `amax`; TOP is the mantissa of L, EMAX its exponent.
+template <uint32_t TOP, int EMAX>
+__device__ __forceinline__ uint32_t block_scale_code(uint32_t amax) {
+  if (amax >= INF_BITS) return 255u;
+  const int code = (int)(amax >> 23) - EMAX + ((amax & 0x7FFFFFu) > TOP ? 1 : 0);
+  return (uint32_t)max(code, 0);
+}
+__device__ __forceinline__ uint32_t scale_code_e4m3(uint32_t amax) { return block_scale_code<0x600000u, 8>(amax); }
+__device__ __forceinline__ uint32_t scale_code_e2m1(uint32_t amax) { return block_scale_code<0x400000u, 2>(amax); }
+
+// 2^k of a scale byte (2^-127 is subnormal in fp32; 0xFF is NaN), and 2^-k (a NaN block: 2^-127, its codes do not matter)
+__device__ __forceinline__ float scale_value(uint32_t code) {
+  return __uint_as_float(code == 0u ? 0x00400000u : code == 255u ? 0x7FC00000u : code << 23);
+}
+__device__ __forceinline__ float scale_inverse(uint32_t code) { return __uint_as_float(code == 255u ? 0x00400000u : (254u - code) << 23); }
+
+// |x| / scale on a format of MBITS mantissa bits whose smallest normal is 2^EMIN, rounded stochastically with k16 in [0, 2^16)
+template <int MBITS, int EMIN>
+__device__ __forceinline__ float round_stochastic(float a, uint32_t k16) {
+  constexpr int LOW = 23 - MBITS;                               // bits that go
+  constexpr float NORMAL = EMIN == 0 ? 1.f : 1.f / (float)(1 << -EMIN);
+  const float base = a < NORMAL ? NORMAL : 0.f;
+  const uint32_t y = (__float_as_uint(__fadd_rz(a, base)) + (k16 << (LOW - 16))) & ~((1u << LOW) - 1u);
+  return __uint_as_float(y) - base;
+}
+
+// the 16-bit number of element e of a group of eight
+__device__ __forceinline__ uint32_t half_word(const U4& u, int e) {
+  const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
+  return (e & 1) ? w >> 16 : w & 0xFFFFu;
+}
+
+// two values that E4M3 / E2M1 holds exactly, or rounded to nearest even -> codes, `lo` in the low byte / nibble
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 from_e4m3x2(uint32_t codes) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)codes));
+  float2 v;
+  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v.x), "=f"(v.y) : "r"(h));
+  return v;
+}
+__device__ __forceinline__ uint32_t to_e2m1x2(float lo, float hi) {
+  uint32_t r;
+  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tmov.b32 %0, {c, 0, 0, 0};\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float2 from_e2m1x2(uint32_t codes) {
+  uint32_t h;
+  asm("{\n\t.reg .b8 c, d1, d2, d3;\n\tmov.b32 {c, d1, d2, d3}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(h) : "r"(codes));
+  float2 v;
+  asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v.x), "=f"(v.y) : "r"(h));
+  return v;
+}
+
+// ---- eight consecutive elements of a tensor, as fp32 --------------------------------------------------------------------
+enum : int { T_F32 = 0, T_BF16 = 1, T_F16 = 2, T_MXFP4 = 3 };
+
+__device__ __forceinline__ float bf16_to_float(uint32_t h) { return __uint_as_float(h << 16); }
+__device__ __forceinline__ uint32_t float_to_bf16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t float_to_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float f16_to_float(uint32_t h) {
+  float v;
+  asm("cvt.f32.f16 %0, %1;" : "=f"(v) : "h"((uint16_t)h));
+  return v;
+}
+
+template <int T> struct Elem;
+template <> struct Elem<T_F32> {
+  static constexpr int bytes = 4;
+  static __device__ __forceinline__ float get(const void* p, long long i) { return static_cast<const float*>(p)[i]; }
+  static __device__ __forceinline__ void put(void* p, long long i, float v) { static_cast<float*>(p)[i] = v; }
+  static __device__ __forceinline__ void get8(const void* p, long long i, float (&v)[8]) {   // 16-byte aligned
+    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    const float4 a = q[0], b = q[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  static __device__ __forceinline__ void put8(void* p, long long i, const float (&v)[8]) {
+    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+    q[0] = make_float4(v[0], v[1], v[2], v[3]);
+    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+  }
+};
+template <> struct Elem<T_BF16> {
+  static constexpr int bytes = 2;
+  static __device__ __forceinline__ float get(const void* p, long long i) { return bf16_to_float(static_cast<const uint16_t*>(p)[i]); }
+  static __device__ __forceinline__ void put(void* p, long long i, float v) { static_cast<uint16_t*>(p)[i] = (uint16_t)float_to_bf16x2(v, 0.f); }
+  static __device__ __forceinline__ void get8(const void* p, long long i, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { v[2 * k] = __uint_as_float(w[k] << 16); v[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u); }
+  }
+  static __device__ __forceinline__ void put8(void* p, long long i, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) =
+        make_uint4(float_to_bf16x2(v[0], v[1]), float_to_bf16x2(v[2], v[3]), float_to_bf16x2(v[4], v[5]), float_to_bf16x2(v[6], v[7]));
+  }
+};
+template <> struct Elem<T_F16> {
+  static constexpr int bytes = 2;
+  static __device__ __forceinline__ float get(const void* p, long long i) { return f16_to_float(static_cast<const uint16_t*>(p)[i]); }
+  static __device__ __forceinline__ void put(void* p, long long i, float v) { static_cast<uint16_t*>(p)[i] = (uint16_t)float_to_f16x2(v, 0.f); }
+  static __device__ __forceinline__ void get8(const void* p, long long i, float (&v)[8]) {
+    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) { v[2 * k] = f16_to_float(w[k] & 0xFFFFu); v[2 * k + 1] = f16_to_float(w[k] >> 16); }
+  }
+  static __device__ __forceinline__ void put8(void* p, long long i, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) =
+        make_uint4(float_to_f16x2(v[0], v[1]), float_to_f16x2(v[2], v[3]), float_to_f16x2(v[4], v[5]), float_to_f16x2(v[6], v[7]));
+  }
+};
+
+// eight MXFP4 codes of one word -> values in units of the scale
+__device__ __forceinline__ void e2m1x8(uint32_t w, float (&v)[8]) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 t = from_e2m1x2((w >> (8 * k)) & 0xFFu);
+    v[2 * k] = t.x;
+    v[2 * k + 1] = t.y;
+  }
+}
+
+}  // namespace ssim

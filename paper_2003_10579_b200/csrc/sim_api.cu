@@ -9,6 +9,7 @@
 #include <string>
 #include <vector>
 
+#include "error.cuh"
 #include "linear_kernel.cuh"
 #include "softmax_kernel.cuh"
 #include "softmax_ws_kernel.cuh"
@@ -34,6 +35,13 @@ struct TraceBuffers {
 };
 
 }  // namespace
+
+namespace ssim {
+sim_status record_error(sim_status st, const char* msg) noexcept {
+  try { g_last_error = msg; } catch (...) {}
+  return st;
+}
+}  // namespace ssim
 
 struct sim_handle {
   sim_problem prob{};
