@@ -371,6 +371,44 @@ sim_status sim_adamw_step_device(const sim_adamw* h, const int64_t* t, const flo
 /* Waits for the device and frees the tables. */
 void sim_adamw_destroy(sim_adamw* h);
 
+/*
+ * MXFP4 matrices.  A matrix [rows][cols] has codes in rows of 64 ceil(cols / 128) bytes (SIM_MXFP4's order; the tail of a row is
+ * zero), 16-byte aligned, and one scale byte per block of 32 elements of a row in one of two orders:
+ *   tiles = 0   [rows][ceil(cols / 32)]; with rows = 1 the form of a pushed gradient (SIM_MXFP4 of sim_adamw_tensor)
+ *   tiles = 1   the order sim_mx_matmul reads, 16-byte aligned: 512 bytes per 128 rows x 4 blocks, the tiles of one row group one
+ *               behind the other; row r of a tile at byte 16 (r % 32) + 4 (r / 32), its four blocks side by side
+ * The two calls give the sizes of the buffers (0 for sizes outside [1, 2^40] or 2^48 elements).
+ */
+int64_t sim_mx_codes_bytes(int64_t rows, int64_t cols);
+int64_t sim_mx_scales_bytes(int64_t rows, int64_t cols, int32_t tiles);
+
+/*
+ * Quantises x [rows][cols] (SIM_F32, SIM_BF16 or SIM_F16; rows ld elements apart) along its rows into codes / scales, along its
+ * columns into codes_t / scales_t (an MXFP4 matrix [cols][rows]), or both from one read: either pair may be NULL.  A block's scale
+ * is the smallest power of two, at least 2^-127, for which no magnitude of the block exceeds six times it, so nothing
+ * saturates; elements are rounded to nearest even, or, with stochastic != 0, to step * floor(|x| / step + u) with u = 16 bits of
+ * Philox4x32-10 / 2^16 (key = seed; counter = (position along the block's axis / 8, tag 3 for rows and 4 for columns, row of the
+ * result), so results do not depend on what else runs).  A block with an infinity or a NaN gets the NaN scale.
+ * Enqueued on cuda_stream; allocates nothing.  SIM_ERR_ARG for bad sizes, types, alignment or a pair of which half is missing.
+ */
+sim_status sim_mx_quantize(const void* x, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, int32_t tiles, int32_t stochastic,
+                           uint64_t seed, uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* cuda_stream);
+
+/* The values of an MXFP4 matrix, rounded once to SIM_F32, SIM_BF16 or SIM_F16 (infinity where one is
+ * beyond the type's range), into out [rows][cols] with rows ld apart. */
+sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int32_t tiles, sim_dtype type, void* out,
+                             int64_t ld, void* cuda_stream);
+
+/*
+ * c [M][N] = A B^T for MXFP4 A [M][K] and B [N][K], both with scales in tiles: fp32 accumulation on the tensor cores, one
+ * rounding to SIM_F32 or SIM_BF16; rows of c ldc apart.  With x [tokens][in] and weights w [out][in]: the layer's output is
+ * the product of x and w; the gradient by x that of dy and w's columns (codes_t of w); the gradient by w that of dy's and x's columns.
+ * M, N, K in [1, 2^30].  Few rows split K over a cluster of blocks and add the parts in a fixed order: same bits every time.
+ * Enqueued on cuda_stream; allocates nothing.  A device-side wait that runs out leaves its part of c NaN.
+ */
+sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, int64_t M, int64_t N,
+                         int64_t K, sim_dtype type, void* c, int64_t ldc, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

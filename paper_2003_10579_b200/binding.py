@@ -23,7 +23,8 @@ EXPORTS = ["sim_create", "sim_set_params", "sim_set_adasync", "sim_set_adasync_l
            "sim_trace_size", "sim_get_trace", "sim_get_params", "sim_eval_loss", "sim_error_curve", "sim_set_eval_every", "sim_risk_trace_size",
            "sim_get_risk_trace", "sim_risk_curve", "sim_risk_envelope", "sim_selftest_wait_timeout", "sim_n_params", "sim_last_error",
            "sim_destroy", "sim_draw_delays", "sim_draw_indices", "sim_simulate_host", "sim_sweep_host", "sim_schedule_noalloc",
-           "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy"]
+           "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy",
+           "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul"]
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # SIM_F32, SIM_BF16, SIM_F16
 MXFP4 = 3
 
@@ -95,9 +96,15 @@ def _load():
     L.sim_adamw_step_device.argtypes = [vp, vp, vp, C.c_float, i32, vp]
     L.sim_adamw_destroy.argtypes = [vp]
     L.sim_adamw_destroy.restype = None
+    L.sim_mx_codes_bytes.argtypes = [i64, i64]
+    L.sim_mx_scales_bytes.argtypes = [i64, i64, i32]
+    L.sim_mx_quantize.argtypes = [vp, C.c_int, i64, i64, i64, i32, i32, u64, vp, vp, vp, vp, vp]
+    L.sim_mx_dequantize.argtypes = [vp, vp, i64, i64, i32, C.c_int, vp, i64, vp]
+    L.sim_mx_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, C.c_int, vp, i64, vp]
     for name in EXPORTS:
-        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy"):
+        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy", "sim_mx_codes_bytes", "sim_mx_scales_bytes"):
             getattr(L, name).restype = C.c_int
+    L.sim_mx_codes_bytes.restype = L.sim_mx_scales_bytes.restype = i64
     return L
 
 
@@ -506,3 +513,67 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+def _matrix(x, what):
+    """A CUDA tensor of one or two dimensions with neighbouring elements along the last -> (rows, cols, elements between rows)."""
+    if not x.is_cuda or x.dtype not in DTYPES or x.dim() not in (1, 2) or x.numel() == 0:
+        raise ValueError("%s must be a CUDA tensor of float32, bfloat16 or float16 with one or two dimensions and at least one element" % what)
+    rows, cols = (1, x.shape[0]) if x.dim() == 1 else x.shape
+    if (cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(0) < cols):
+        raise ValueError("%s must have neighbouring elements along its last dimension and rows that do not overlap" % what)
+    return rows, cols, x.stride(0) if rows > 1 else cols
+
+
+def _mx_empty(rows, cols, layout, device):
+    tiles = layout == "tiles"
+    return MxTensor(torch.empty(lib.sim_mx_codes_bytes(rows, cols), dtype=torch.uint8, device=device),
+                    torch.empty(lib.sim_mx_scales_bytes(rows, cols, tiles), dtype=torch.uint8, device=device), rows, cols, layout)
+
+
+def mx_quantize(x, *, along="rows", rounding="nearest", seed=0, layout="tiles", stream=None):
+    """MXFP4 form of a matrix (or vector: one row).  along "rows" -> MxTensor [rows, cols]; "cols" -> MxTensor [cols, rows] with
+    blocks along x's columns; "both" -> the two from one read.  rounding "nearest" (even) or "stochastic" (from `seed`)."""
+    if along not in ("rows", "cols", "both") or rounding not in ("nearest", "stochastic") or layout not in ("linear", "tiles"):
+        raise ValueError("along: rows, cols or both; rounding: nearest or stochastic; layout: linear or tiles")
+    rows, cols, ld = _matrix(x, "x")
+    with torch.cuda.device(x.device):
+        st = torch.cuda.current_stream() if stream is None else stream
+        q = _mx_empty(rows, cols, layout, x.device) if along != "cols" else None
+        qt = _mx_empty(cols, rows, layout, x.device) if along != "rows" else None
+        ptrs = [None if t is None else _ptr(b) for t in (q, qt) for b in ((t.codes, t.scales) if t is not None else (None, None))]
+        _check(lib.sim_mx_quantize(_ptr(x), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed, *ptrs, _stream_ptr(st)))
+    return (q, qt) if along == "both" else q if q is not None else qt
+
+
+def mx_dequantize(q, dtype=torch.float32, *, out=None, stream=None):
+    """The values of an MxTensor as a matrix [rows, cols] of dtype (float32, bfloat16, float16), or into `out`."""
+    if out is None:
+        if dtype not in DTYPES:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
+    rows, cols, ld = _matrix(out, "out")
+    if (rows, cols) != (q.rows, q.cols) or out.device != q.codes.device or q.scales.device != q.codes.device:
+        raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.codes.device))
+    with torch.cuda.device(out.device):
+        st = torch.cuda.current_stream() if stream is None else stream
+        _check(lib.sim_mx_dequantize(_ptr(q.codes), _ptr(q.scales), rows, cols, q.layout == "tiles", DTYPES[out.dtype], _ptr(out), ld, _stream_ptr(st)))
+    return out
+
+
+def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
+    """a b^T [a.rows, b.rows] of two MxTensors with as many columns, layout "tiles", as bfloat16 or float32, or into `out`."""
+    if a.cols != b.cols or a.layout != "tiles" or b.layout != "tiles" or len({t.device for t in (a.codes, a.scales, b.codes, b.scales)}) != 1:
+        raise ValueError("both operands need the same number of columns, the layout 'tiles' and one device")
+    if out is None:
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("dtype must be bfloat16 or float32")
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+    rows, cols, ld = _matrix(out, "out")
+    if (rows, cols) != (a.rows, b.rows) or out.device != a.codes.device or out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.codes.device))
+    with torch.cuda.device(out.device):
+        st = torch.cuda.current_stream() if stream is None else stream
+        _check(lib.sim_mx_matmul(_ptr(a.codes), _ptr(a.scales), _ptr(b.codes), _ptr(b.scales), a.rows, b.rows, a.cols, DTYPES[out.dtype], _ptr(out), ld,
+                                 _stream_ptr(st)))
+    return out

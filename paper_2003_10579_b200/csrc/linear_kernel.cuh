@@ -13,6 +13,7 @@
 // asynchronous variants every version is also written to the replica's version pool, from
 // which stale snapshots w_tau are read back.
 #pragma once
+#include "ptx_util.cuh"
 #include "schedule_kernel.cuh"
 
 namespace ssim {
@@ -61,57 +62,12 @@ __host__ __device__ __forceinline__ long long w1_tiled_index(long long k, long l
   return (((k >> 7) * (H >> 5) + (n >> 5)) << 12) + ((k & 127) << 5) + (((((n & 31) >> 2) ^ (k & 7)) << 2) | (n & 3));
 }
 
-// ---- shared-memory barrier and bulk-copy primitives ------------------------------------------
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_fence_init() {
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-// Bounded wait: gives up after `limit` polls (the default is a few seconds' worth) and reports it.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t limit = 1u << 24) {
-  for (uint32_t i = 0; i < limit; ++i) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (i > 4096) __nanosleep(128);
-  }
-  return false;
-}
 // After a wait has run out: before the block gives up its shared memory, give the row copies that are still in flight
 // a bounded time to land.  At tile (st, parity) the producer is at most one ring ahead: stages st.. complete phase
 // `parity`, stages below st the next one.  A stage that was never issued simply uses up its (short) limit.
 __device__ __forceinline__ void drain_ring(uint64_t* full, int S, int st, uint32_t parity) {
   for (int s = 0; s < S; ++s) mbar_wait((uint32_t)__cvta_generic_to_shared(&full[s]), s >= st ? parity : parity ^ 1u, 1u << 14);
 }
-// global -> shared bulk copy of `bytes` (multiple of 16, both addresses 16-byte aligned)
-__device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-      ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
-}
-// 4-byte asynchronous copy whose completion is counted as one arrival on `bar`
-__device__ __forceinline__ void word_g2s_arrive(uint32_t dst, const void* src, uint32_t bar) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
-  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, off);

@@ -1,0 +1,182 @@
+// C entry points of MXFP4 quantisation, reading back and products (mx_kernel.cuh, mx_gemm_kernel.cuh).
+#include <cstdio>
+
+#include "error.cuh"
+#include "mx_gemm_kernel.cuh"
+#include "mx_kernel.cuh"
+
+using namespace ssim;
+
+namespace {
+
+sim_status cuda_failed(const char* where, cudaError_t e) {
+  char msg[200];
+  std::snprintf(msg, sizeof msg, "%s: %s", where, cudaGetErrorString(e));
+  return record_error(e == cudaErrorMemoryAllocation ? SIM_ERR_ALLOC : SIM_ERR_CUDA, msg);
+}
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool bad_size(int64_t rows, int64_t cols) { return rows < 1 || cols < 1 || rows > (int64_t)1 << 40 || cols > (int64_t)1 << 40 || rows > ((int64_t)1 << 48) / cols; }
+int elem_bytes(sim_dtype t) { return t == SIM_F32 ? 4 : 2; }
+
+int sm_count() {
+  int dev = 0, sms = 148;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  return sms;
+}
+unsigned grid_for(long long threads) {
+  const long long blocks = (threads + 255) / 256, full = 8ll * sm_count();
+  return (unsigned)(blocks < full ? blocks : full);
+}
+
+template <int T, bool SR>
+cudaError_t quantize(const MxQuantArgs& a, cudaStream_t st) {
+  if (!a.codes_t) {
+    mx_quantize_rows_kernel<T, SR><<<grid_for(a.rows * ((a.cols + 127) / 128) * 16), 256, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  constexpr int smem = mx_tile_smem<T>();
+  cudaError_t e = cudaFuncSetAttribute(mx_quantize_tile_kernel<T, SR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) return e;
+  const long long tiles = ((a.rows + 127) / 128) * ((a.cols + 127) / 128), full = (long long)(227 * 1024 / smem) * sm_count();
+  mx_quantize_tile_kernel<T, SR><<<(unsigned)(tiles < full ? tiles : full), 256, smem, st>>>(a);
+  return cudaGetLastError();
+}
+template <int T>
+cudaError_t quantize_sr(const MxQuantArgs& a, cudaStream_t st) { return a.stochastic ? quantize<T, true>(a, st) : quantize<T, false>(a, st); }
+
+// rows of codes as a 2-D byte tensor; box: 128 bytes (256 elements of k) x box_rows, 128-byte swizzle, zeros outside
+bool make_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t cols, uint32_t box_rows) {
+  PFN_encodeTiled fn = tc_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)mx_pitch(cols), (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {dims[0]};
+  const cuuint32_t box[2] = {128, box_rows}, one[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(codes), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN, int T, bool SWAP, bool SPLIT>
+cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
+  auto kern = mx_gemm_kernel<BN, T, SWAP, SPLIT>;
+  // partial sums of a split tile lie in the ring's bytes
+  static_assert(!SPLIT || 128 * (BN + 1) * 4 <= MxgShape<BN>::OFF_BARS, "the partial sums must fit the ring");
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MxgShape<BN>::SMEM);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1);
+  cfg.blockDim = dim3(MXG_THREADS, 1, 1);
+  cfg.dynamicSmemBytes = MxgShape<BN>::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  if (SPLIT) {
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1; attr.val.clusterDim.y = (unsigned)split; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, kern, ma, mb, g);
+}
+template <int BN, int T, bool SWAP>
+cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
+  return split > 1 ? launch<BN, T, SWAP, true>(ma, mb, g, split, st) : launch<BN, T, SWAP, false>(ma, mb, g, split, st);
+}
+template <int T, bool SWAP>
+cudaError_t launch_bn(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
+  switch (bn) {
+    case 16: return launch_split<16, T, SWAP>(ma, mb, g, split, st);
+    case 32: return launch_split<32, T, SWAP>(ma, mb, g, split, st);
+    case 64: return launch_split<64, T, SWAP>(ma, mb, g, split, st);
+    case 128: return launch_split<128, T, SWAP>(ma, mb, g, split, st);
+    default: return launch<256, T, SWAP, false>(ma, mb, g, 1, st);
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t sim_mx_codes_bytes(int64_t rows, int64_t cols) { return bad_size(rows, cols) ? 0 : rows * mx_pitch(cols); }
+int64_t sim_mx_scales_bytes(int64_t rows, int64_t cols, int32_t tiles) {
+  if (bad_size(rows, cols)) return 0;
+  return tiles ? (rows + 127) / 128 * ((cols + 127) / 128) * 512 : rows * ((cols + 31) / 32);
+}
+
+sim_status sim_mx_quantize(const void* x, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, int32_t tiles, int32_t stochastic,
+                           uint64_t seed, uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* cuda_stream) {
+  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_quantize: rows and cols must be >= 1, below 2^40 each and 2^48 together");
+  if (type != SIM_F32 && type != SIM_BF16 && type != SIM_F16) return record_error(SIM_ERR_ARG, "sim_mx_quantize: type must be SIM_F32, SIM_BF16 or SIM_F16");
+  if (ld < cols || ld > ((int64_t)1 << 50) / rows) return record_error(SIM_ERR_ARG, "sim_mx_quantize: ld must be at least cols");
+  if (!x || !aligned(x, elem_bytes(type))) return record_error(SIM_ERR_ARG, "sim_mx_quantize: x must be aligned to its type");
+  if (!codes != !scales || !codes_t != !scales_t || (!codes && !codes_t))
+    return record_error(SIM_ERR_ARG, "sim_mx_quantize: codes and scales of the rows, of the columns, or of both are required");
+  if (!aligned(codes, 16) || !aligned(codes_t, 16) || (tiles && (!aligned(scales, 16) || !aligned(scales_t, 16))))
+    return record_error(SIM_ERR_ARG, "sim_mx_quantize: codes and tiled scales must be 16-byte aligned");
+  MxQuantArgs a{};
+  a.x = x; a.rows = rows; a.cols = cols; a.ld = ld; a.codes = codes; a.scales = scales; a.codes_t = codes_t; a.scales_t = scales_t;
+  a.tiles = tiles ? 1 : 0; a.stochastic = stochastic ? 1 : 0; a.seed = seed;
+  a.vec = aligned(x, 16) && (rows == 1 || ld * elem_bytes(type) % 16 == 0) ? 1 : 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const cudaError_t e = type == SIM_F32 ? quantize_sr<T_F32>(a, st) : type == SIM_BF16 ? quantize_sr<T_BF16>(a, st) : quantize_sr<T_F16>(a, st);
+  return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_quantize", e);
+}
+
+sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int32_t tiles, sim_dtype type, void* out,
+                             int64_t ld, void* cuda_stream) {
+  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: rows and cols must be >= 1, below 2^40 each and 2^48 together");
+  if (type != SIM_F32 && type != SIM_BF16 && type != SIM_F16) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: type must be SIM_F32, SIM_BF16 or SIM_F16");
+  if (ld < cols || ld > ((int64_t)1 << 50) / rows) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: ld must be at least cols");
+  if (!codes || !scales || !out || !aligned(out, elem_bytes(type))) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: codes, scales and out (aligned to its type) are required");
+  MxReadArgs a{};
+  a.codes = codes; a.scales = scales; a.rows = rows; a.cols = cols; a.ld = ld; a.out = out; a.tiles = tiles ? 1 : 0;
+  a.vec = aligned(out, 16) && (rows == 1 || ld * elem_bytes(type) % 16 == 0) ? 1 : 0;
+  a.word = aligned(codes, 4) ? 1 : 0;
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const unsigned grid = grid_for(rows * ((cols + 7) / 8));
+  if (type == SIM_F32) mx_dequantize_kernel<T_F32><<<grid, 256, 0, st>>>(a);
+  else if (type == SIM_BF16) mx_dequantize_kernel<T_BF16><<<grid, 256, 0, st>>>(a);
+  else mx_dequantize_kernel<T_F16><<<grid, 256, 0, st>>>(a);
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_dequantize", e);
+}
+
+sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, int64_t M, int64_t N,
+                         int64_t K, sim_dtype type, void* c, int64_t ldc, void* cuda_stream) {
+  const int64_t top = (int64_t)1 << 30;
+  if (M < 1 || N < 1 || K < 1 || M > top || N > top || K > top) return record_error(SIM_ERR_ARG, "sim_mx_matmul: M, N and K must be in [1, 2^30]");
+  if (type != SIM_F32 && type != SIM_BF16) return record_error(SIM_ERR_ARG, "sim_mx_matmul: the result is SIM_F32 or SIM_BF16");
+  if (ldc < N || ldc > ((int64_t)1 << 50) / M) return record_error(SIM_ERR_ARG, "sim_mx_matmul: ldc must be at least N");
+  if (!a_codes || !a_scales || !b_codes || !b_scales || !c || !aligned(c, elem_bytes(type)))
+    return record_error(SIM_ERR_ARG, "sim_mx_matmul: operands and result (aligned to its type) are required");
+  if (!aligned(a_codes, 16) || !aligned(a_scales, 16) || !aligned(b_codes, 16) || !aligned(b_scales, 16))
+    return record_error(SIM_ERR_ARG, "sim_mx_matmul: codes and scales must be 16-byte aligned");
+  // few rows: they become the B operand of the instruction (16, 32 or 64 wide), the other matrix its 128-row A operand
+  const bool swap = M <= 64 && M <= N;
+  const int64_t ra = swap ? N : M, rb = swap ? M : N;
+  const int kb = (int)((K + 127) / 128), sms = sm_count();
+  const int64_t tiles_a = (ra + 127) / 128;
+  int bn = rb <= 16 ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
+  if (rb > 128 && tiles_a * ((rb + 255) / 256) >= sms) bn = 256;
+  const int64_t tiles_b = (rb + bn - 1) / bn;
+  if (tiles_a * tiles_b > (int64_t)1 << 30) return record_error(SIM_ERR_ARG, "sim_mx_matmul: the result has too many tiles");
+  int split = 1;
+  if (bn < 256)     // fewer tiles than two a multiprocessor: split k over a cluster, four 128-element blocks each at least
+    while (split < 8 && tiles_a * tiles_b * split * 2 <= 2 * sms && kb >= split * 2 * 4) split *= 2;
+  MxgArgs g{};
+  g.a_scales = swap ? b_scales : a_scales; g.b_scales = swap ? a_scales : b_scales;
+  g.rows_a = ra; g.rows_b = rb; g.kb = kb;
+  g.kb_split = ((kb + split - 1) / split + 1) / 2 * 2;
+  split = (kb + g.kb_split - 1) / g.kb_split;          // every block of a cluster has a part
+  g.tiles_a = (int)tiles_a; g.tiles_b = (int)tiles_b;
+  g.d = c; g.ldd = ldc;
+  g.vec = aligned(c, 16) && ldc * elem_bytes(type) % 16 == 0 ? 1 : 0;
+  CUtensorMap ma, mb;
+  if (!make_map(&ma, swap ? b_codes : a_codes, ra, K, 128) || !make_map(&mb, swap ? a_codes : b_codes, rb, K, (uint32_t)bn))
+    return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
+  const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  cudaError_t e;
+  if (type == SIM_F32) e = swap ? launch_bn<T_F32, true>(bn, ma, mb, g, split, st) : launch_bn<T_F32, false>(bn, ma, mb, g, split, st);
+  else e = swap ? launch_bn<T_BF16, true>(bn, ma, mb, g, split, st) : launch_bn<T_BF16, false>(bn, ma, mb, g, split, st);
+  return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_matmul", e);
+}
+
+}  // extern "C"

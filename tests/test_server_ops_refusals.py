@@ -64,3 +64,31 @@ def test_adamw_binding_checks_tensors_before_the_library_sees_them(B):
         B.AdamW([], [])
     with pytest.raises(ValueError):
         B.MxTensor(torch.zeros(64, dtype=torch.uint8), torch.zeros(4, dtype=torch.uint8), 1, 128, "linear")
+
+
+def test_mx_calls_refuse_bad_arguments(B):
+    L, f = B.lib, 0x10000
+    assert L.sim_mx_codes_bytes(3, 129) == 3 * 128 and L.sim_mx_scales_bytes(129, 129, 1) == 4 * 512 and L.sim_mx_scales_bytes(3, 33, 0) == 6
+    assert L.sim_mx_codes_bytes(0, 5) == 0 and L.sim_mx_scales_bytes(1 << 30, 1 << 30, 1) == 0
+
+    def quant(x=f, type=0, rows=4, cols=64, ld=64, tiles=1, codes=f, scales=f, codes_t=None, scales_t=None):
+        return L.sim_mx_quantize(x, type, rows, cols, ld, tiles, 0, 0, codes, scales, codes_t, scales_t, None)
+
+    for kw in (dict(x=None), dict(x=f + 2), dict(type=3), dict(type=-1), dict(rows=0), dict(cols=0), dict(cols=-5), dict(rows=1 << 41), dict(ld=63), dict(ld=1 << 50),
+               dict(codes=None), dict(scales=None), dict(codes=None, scales=None), dict(codes_t=f), dict(scales_t=f), dict(codes=f + 8), dict(scales=f + 4),
+               dict(codes_t=f + 8, scales_t=f), dict(codes_t=f, scales_t=f + 8)):
+        assert quant(**kw) == 1, kw
+        assert b"sim_mx_quantize" in L.sim_last_error(None)
+
+    def read(codes=f, scales=f, rows=4, cols=64, type=0, out=f, ld=64):
+        return L.sim_mx_dequantize(codes, scales, rows, cols, 1, type, out, ld, None)
+
+    for kw in (dict(codes=None), dict(scales=None), dict(out=None), dict(out=f + 2), dict(type=3), dict(rows=0), dict(cols=0), dict(ld=63)):
+        assert read(**kw) == 1, kw
+
+    def product(a=f, sa=f, b=f, sb=f, M=4, N=4, K=64, type=0, c=f, ldc=4):
+        return L.sim_mx_matmul(a, sa, b, sb, M, N, K, type, c, ldc, None)
+
+    for kw in (dict(a=None), dict(sa=None), dict(b=None), dict(sb=None), dict(c=None), dict(c=f + 2), dict(a=f + 8), dict(sb=f + 8), dict(M=0), dict(N=0), dict(K=0),
+               dict(K=(1 << 30) + 1), dict(type=2), dict(type=3), dict(ldc=3), dict(M=1 << 30, N=1 << 30, ldc=1 << 30)):
+        assert product(**kw) == 1, kw
