@@ -345,7 +345,7 @@ typedef struct sim_adamw sim_adamw;   /* opaque; holds tables only, no state: bu
 /*
  * Binds a list of tensors with n_grads push buffers each on the current device.  state_bits is 32 or 8.  Allocates and fills
  * the tables (waits for the copy); no later call allocates or waits.  Errors: SIM_ERR_ARG for an empty list, n_grads outside
- * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps not finite or not > 0, a tensor with missing or misaligned
+ * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps not finite or below 2^-126, a tensor with missing or misaligned
  * pointers or unknown types; SIM_ERR_ALLOC / SIM_ERR_CUDA otherwise.  *out is NULL on failure.
  */
 sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, int32_t n_grads, int32_t state_bits, double beta1,
@@ -357,7 +357,7 @@ sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, 
  *   p = p (1 - lr weight_decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
  * 8-bit states: the step uses m and v in fp32; what is kept is rounded stochastically, with 16-bit numbers from
  * Philox4x32-10 (key = seed; counter = (element / 8, tag 2, t, index in the list)), so the same calls give the same bits
- * whatever else runs.  A positive sqrt(v) is never kept as zero.  A gradient that is not finite makes its element's states
+ * whatever else runs.  A positive sqrt(v) is never kept as zero (v below 2^-126 counts as zero).  A gradient that is not finite makes its element's states
  * (8 bits: its block's) NaN.  Elements outside [0, n) are neither read nor written.  Enqueues one launch per combination of
  * parameter and gradient type on cuda_stream (a stream of the handle's device); the handle is only read, so steps of
  * different handles may overlap.

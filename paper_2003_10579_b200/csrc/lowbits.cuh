@@ -32,20 +32,67 @@ __device__ __forceinline__ float scale_value(uint32_t code) {
 }
 __device__ __forceinline__ float scale_inverse(uint32_t code) { return __uint_as_float(code == 255u ? 0x00400000u : (254u - code) << 23); }
 
-// |x| / scale on a format of MBITS mantissa bits whose smallest normal is 2^EMIN, rounded stochastically with k16 in [0, 2^16)
+// x / scale (any sign) on a format of MBITS mantissa bits whose smallest normal is 2^EMIN, rounded stochastically with k16 in
+// [0, 2^16).  round_normal: |x| / scale is at least the smallest normal (or x is zero and k16 does not matter: see the mask).
+template <int MBITS>
+__device__ __forceinline__ float round_normal(float a, uint32_t k16) {
+  constexpr int LOW = 23 - MBITS;                               // bits that go
+  return __uint_as_float((k16 * (1u << (LOW - 16)) + __float_as_uint(a)) & ~((1u << LOW) - 1u));
+}
 template <int MBITS, int EMIN>
 __device__ __forceinline__ float round_stochastic(float a, uint32_t k16) {
-  constexpr int LOW = 23 - MBITS;                               // bits that go
   constexpr float NORMAL = EMIN == 0 ? 1.f : 1.f / (float)(1 << -EMIN);
-  const float base = a < NORMAL ? NORMAL : 0.f;
-  const uint32_t y = (__float_as_uint(__fadd_rz(a, base)) + (k16 << (LOW - 16))) & ~((1u << LOW) - 1u);
-  return __uint_as_float(y) - base;
+  const float mag = fabsf(a), base = mag < NORMAL ? NORMAL : 0.f;
+  return copysignf(round_normal<MBITS>(__fadd_rz(mag, base), k16) - base, a);
+}
+
+// largest magnitude of three, NaN if one is NaN
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float min3_abs(float a, float b, float c) {
+  float r;
+  asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t amax8(const float (&x)[8]) {   // bits of the largest magnitude; at least INF_BITS if one is not finite
+  return __float_as_uint(max3_abs(max3_abs(x[0], x[1], x[2]), max3_abs(x[3], x[4], x[5]), max3_abs(x[6], x[7], 0.f))) & ABS_MASK;
+}
+__device__ __forceinline__ float amin8(const float (&x)[8]) {
+  return min3_abs(min3_abs(x[0], x[1], x[2]), min3_abs(x[3], x[4], x[5]), fminf(fabsf(x[6]), fabsf(x[7])));
+}
+
+// Philox4x32-10 (device_rng.cuh) with the ten round keys worked out once, where the key is the same for a whole launch
+struct PhiloxKeys { uint32_t k[20]; };
+__host__ inline PhiloxKeys philox_keys(uint64_t seed) {
+  PhiloxKeys q;
+  uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  for (int r = 0; r < 10; ++r) {
+    q.k[2 * r] = k0; q.k[2 * r + 1] = k1;
+    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
+  }
+  return q;
+}
+__device__ __forceinline__ U4 philox_keyed(const PhiloxKeys& q, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
+    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ q.k[2 * r], n2 = (uint32_t)(p0 >> 32) ^ c3 ^ q.k[2 * r + 1];
+    c0 = n0; c1 = (uint32_t)p1; c2 = n2; c3 = (uint32_t)p0;
+  }
+  return U4{c0, c1, c2, c3};
 }
 
 // the 16-bit number of element e of a group of eight
 __device__ __forceinline__ uint32_t half_word(const U4& u, int e) {
   const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
-  return (e & 1) ? w >> 16 : w & 0xFFFFu;
+  return __byte_perm(w, 0u, (e & 1) ? 0x4432 : 0x4410);
+}
+__device__ __forceinline__ uint32_t half_word_swapped(const U4& u, int e) {   // the same with its two bytes swapped
+  const uint32_t w = e < 2 ? u.x : e < 4 ? u.y : e < 6 ? u.z : u.w;
+  return __byte_perm(w, 0u, (e & 1) ? 0x4423 : 0x4401);
 }
 
 // two values that E4M3 / E2M1 holds exactly, or rounded to nearest even -> codes, `lo` in the low byte / nibble

@@ -41,8 +41,8 @@ __device__ __forceinline__ uint32_t encode_e2m1(const float (&x)[8], float inv, 
   for (int k = 0; k < 4; ++k) {
     float a = x[2 * k] * inv, b = x[2 * k + 1] * inv;
     if (SR) {
-      a = copysignf(round_stochastic<1, 0>(fabsf(a), half_word(u, 2 * k)), a);
-      b = copysignf(round_stochastic<1, 0>(fabsf(b), half_word(u, 2 * k + 1)), b);
+      a = round_stochastic<1, 0>(a, half_word(u, 2 * k));
+      b = round_stochastic<1, 0>(b, half_word(u, 2 * k + 1));
     }
     w |= to_e2m1x2(a, b) << (8 * k);
   }

@@ -1,4 +1,5 @@
 // C entry points of the AdamW step over a list of tensors (adamw_kernel.cuh): argument checks, tables, launches.
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <new>
@@ -11,7 +12,7 @@ using namespace ssim;
 
 namespace {
 
-struct Group { int pt, gt; uint32_t first, count; };   // chunks of tensors with the same parameter and gradient types
+struct Group { int pt, gt; uint32_t first, count, grid; };   // chunks of tensors with the same parameter and gradient types
 
 struct DeviceGuard {   // the handle's device for the duration of a call
   int before = -1;
@@ -23,32 +24,20 @@ struct DeviceGuard {   // the handle's device for the duration of a call
   ~DeviceGuard() { if (before >= 0) cudaSetDevice(before); }
 };
 
-template <int PT, int GT, int BITS>
-cudaError_t launch(const AdamwArgs& a, cudaStream_t st) {
-  // as many blocks as the machine holds at once, chunks dealt round-robin
-  int per_sm = 0, dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, adamw_kernel<PT, GT, BITS>, ADAMW_THREADS, 0);
-  if (e != cudaSuccess) return e;
-  const uint32_t full = (uint32_t)(per_sm > 0 ? per_sm : 1) * (uint32_t)sms;
-  adamw_kernel<PT, GT, BITS><<<a.n_chunks < full ? a.n_chunks : full, ADAMW_THREADS, 0, st>>>(a);
-  return cudaGetLastError();
-}
+using Kernel = void (*)(AdamwArgs);
 
 template <int PT, int BITS>
-cudaError_t launch_g(int gt, const AdamwArgs& a, cudaStream_t st) {
+Kernel pick_g(int gt) {
   switch (gt) {
-    case T_F32: return launch<PT, T_F32, BITS>(a, st);
-    case T_BF16: return launch<PT, T_BF16, BITS>(a, st);
-    case T_F16: return launch<PT, T_F16, BITS>(a, st);
-    default: return launch<PT, T_MXFP4, BITS>(a, st);
+    case T_F32: return adamw_kernel<PT, T_F32, BITS>;
+    case T_BF16: return adamw_kernel<PT, T_BF16, BITS>;
+    case T_F16: return adamw_kernel<PT, T_F16, BITS>;
+    default: return adamw_kernel<PT, T_MXFP4, BITS>;
   }
 }
-
-cudaError_t launch_any(int bits, int pt, int gt, const AdamwArgs& a, cudaStream_t st) {
-  if (bits == 32) return pt == T_F32 ? launch_g<T_F32, 32>(gt, a, st) : launch_g<T_BF16, 32>(gt, a, st);
-  return pt == T_F32 ? launch_g<T_F32, 8>(gt, a, st) : launch_g<T_BF16, 8>(gt, a, st);
+Kernel pick(int bits, int pt, int gt) {
+  if (bits == 32) return pt == T_F32 ? pick_g<T_F32, 32>(gt) : pick_g<T_BF16, 32>(gt);
+  return pt == T_F32 ? pick_g<T_F32, 8>(gt) : pick_g<T_BF16, 8>(gt);
 }
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -107,7 +96,7 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
   if (n_grads < 1 || n_grads > SIM_MAX_P) return record_error(SIM_ERR_ARG, "sim_adamw_create: n_grads must be in [1, SIM_MAX_P]");
   if (bits != 32 && bits != 8) return record_error(SIM_ERR_ARG, "sim_adamw_create: state_bits must be 32 or 8");
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return record_error(SIM_ERR_ARG, "sim_adamw_create: betas must be in [0, 1)");
-  if (!((float)eps > 0.f) || std::isinf((float)eps)) return record_error(SIM_ERR_ARG, "sim_adamw_create: eps must be finite and > 0 in fp32");
+  if (!((float)eps >= FLT_MIN) || std::isinf((float)eps)) return record_error(SIM_ERR_ARG, "sim_adamw_create: eps must be finite and at least 2^-126");
   long long total_chunks = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const sim_status st = check_tensor(ts[i], i, n_grads, bits);
@@ -131,11 +120,11 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
       if (t.g_type == SIM_MXFP4) gs[(size_t)l * n_tensors + i] = t.g_scale[l];
       vec = vec && aligned(t.g[l], gv);
     }
-    tensors[i] = AdamwTensor{t.p, t.m, t.v, t.m_scale, t.v_scale, static_cast<uint16_t*>(t.shadow), t.n, t.weight_decay, vec ? 1 : 0};
+    tensors[i] = AdamwTensor{t.p, t.m, t.v, t.m_scale, t.v_scale, static_cast<uint16_t*>(t.shadow), g[i], gs[i], t.n, t.weight_decay, vec ? 1 : 0};
   }
   for (int pt = 0; pt < 2; ++pt)
     for (int gt = 0; gt < 4; ++gt) {
-      Group grp{pt, gt, (uint32_t)chunks.size(), 0};
+      Group grp{pt, gt, (uint32_t)chunks.size(), 0, 0};
       for (int i = 0; i < n_tensors; ++i)
         if ((int)ts[i].p_type == pt && (int)ts[i].g_type == gt)
           for (long long c = 0; c < (ts[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK; ++c) chunks.push_back(AdamwChunk{(uint32_t)i, (uint32_t)c});
@@ -145,10 +134,18 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
 
   sim_adamw* h = new sim_adamw();
   h->n_tensors = n_tensors; h->n_grads = n_grads; h->bits = bits; h->beta1 = beta1; h->beta2 = beta2; h->eps = (float)eps; h->seed = seed;
-  h->groups.swap(groups);
   const size_t nb_t = tensors.size() * sizeof(AdamwTensor), nb_c = chunks.size() * sizeof(AdamwChunk), nb_g = g.size() * sizeof(void*);
   char* d = nullptr;
   cudaError_t e = cudaGetDevice(&h->device);
+  int sms = 0;
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
+  for (Group& grp : groups) {     // 8-bit states: as many blocks as the machine holds at once; 32-bit: one for each chunk
+    int per_sm = 0;
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, pick(bits, grp.pt, grp.gt), ADAMW_THREADS, 0);
+    const uint32_t full = (uint32_t)(per_sm > 0 ? per_sm : 1) * (uint32_t)sms;
+    grp.grid = bits == 32 || grp.count < full ? grp.count : full;
+  }
+  h->groups.swap(groups);
   if (e == cudaSuccess) e = cudaMalloc(&h->tables, nb_t + nb_c + 2 * nb_g);
   if (e == cudaSuccess) {
     d = static_cast<char*>(h->tables);
@@ -181,12 +178,14 @@ sim_status step(const sim_adamw* h, int64_t t, const int64_t* t_dev, float lr, c
   if (guard.err != cudaSuccess) return cuda_failed("sim_adamw_step", guard.err);
   AdamwArgs a{};
   a.tensors = h->tensors; a.g = h->g; a.g_scale = h->g_scale; a.n_tensors = h->n_tensors; a.K = K;
-  a.beta1 = h->beta1; a.beta2 = h->beta2; a.eps = h->eps; a.grad_scale = (float)((double)grad_scale / K);
-  a.lr = lr; a.step = t; a.lr_dev = lr_dev; a.step_dev = reinterpret_cast<const long long*>(t_dev); a.seed = h->seed;
+  a.beta1 = h->beta1; a.beta2 = h->beta2; a.mean = (double)grad_scale / K;
+  a.coef = adamw_coef(h->beta1, h->beta2, h->eps, a.mean, lr, t_dev ? 1 : t);
+  a.step32 = (uint32_t)t; a.lr_dev = lr_dev; a.step_dev = reinterpret_cast<const long long*>(t_dev); a.keys = philox_keys(h->seed);
   for (const Group& grp : h->groups) {
     a.chunks = h->chunks + grp.first;
     a.n_chunks = grp.count;
-    const cudaError_t e = launch_any(h->bits, grp.pt, grp.gt, a, static_cast<cudaStream_t>(stream));
+    pick(h->bits, grp.pt, grp.gt)<<<grp.grid, ADAMW_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_failed("sim_adamw_step", e);
   }
   return SIM_OK;
