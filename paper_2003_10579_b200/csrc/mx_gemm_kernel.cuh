@@ -79,6 +79,69 @@ __device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
 template <int T>
 __device__ __forceinline__ void mxg_store(void* d, long long i, float v) { Elem<T>::put(d, i, v); }
 
+// A warp's 32 rows x 128 bytes of D: each lane leaves its row in the warp's 4 KB of shared memory, the eight 16-byte pieces XOR-swizzled
+// with the row, and the rows leave as whole 128-byte lines (or as pairs or single elements where D's alignment allows no more).
+__device__ __forceinline__ void mxg_stage(unsigned char* st, int lane, const uint32_t* w) {
+#pragma unroll
+  for (int p = 0; p < 8; ++p)
+    *reinterpret_cast<uint4*>(st + lane * 128 + ((p ^ (lane & 7)) << 4)) = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+}
+// n accumulators as the words of D's type, in place
+template <int T, int N>
+__device__ __forceinline__ void mxg_pack(const uint32_t* v, uint32_t* w) {
+#pragma unroll
+  for (int j = 0; j < N * Elem<T>::bytes / 4; ++j) w[j] = T == T_F32 ? v[j] : float_to_bf16x2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+}
+template <int T>
+__device__ __forceinline__ void mxg_write_rows(const unsigned char* st, int lane, void* d, long long ldd, long long row0, int rows, long long col0, int cols, int vec) {
+  constexpr int EB = Elem<T>::bytes;
+  if (rows <= 0 || cols <= 0) return;
+  char* out = static_cast<char*>(d) + (row0 * ldd + col0) * EB;
+  const long long pitch = ldd * EB;
+  if (vec && cols * EB >= 128) {
+    const int r0 = lane >> 3, piece = lane & 7;
+    char* at = out + r0 * pitch + piece * 16;
+#pragma unroll
+    for (int it = 0; it < 8; ++it, at += 4 * pitch) {
+      const int r = it * 4 + r0;
+      if (r < rows) *reinterpret_cast<uint4*>(at) = *reinterpret_cast<const uint4*>(st + r * 128 + ((piece ^ (r & 7)) << 4));
+    }
+    return;
+  }
+  const bool pairs = EB == 2 && ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)pitch) & 3) == 0;
+#pragma unroll 4
+  for (int r = 0; r < 32; ++r, out += pitch) {
+    if (r >= rows) break;
+    const unsigned char* row = st + r * 128;
+    const int sw = r & 7;
+    if (EB == 4) {
+      if (lane < cols) reinterpret_cast<uint32_t*>(out)[lane] = *reinterpret_cast<const uint32_t*>(row + (((lane >> 2) ^ sw) << 4) + (lane & 3) * 4);
+    } else if (pairs) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(row + (((lane >> 2) ^ sw) << 4) + (lane & 3) * 4);
+      if (2 * lane + 1 < cols) reinterpret_cast<uint32_t*>(out)[lane] = w;
+      else if (2 * lane < cols) reinterpret_cast<uint16_t*>(out)[2 * lane] = (uint16_t)w;
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int e = lane + 32 * h;
+        if (e < cols) reinterpret_cast<uint16_t*>(out)[e] = *reinterpret_cast<const uint16_t*>(row + (((e >> 3) ^ sw) << 4) + (e & 7) * 2);
+      }
+    }
+  }
+}
+// 32 columns of the accumulators, without waiting for them
+__device__ __forceinline__ void mxg_ld32(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]),
+        "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
+        "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void mxg_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
 template <int BN, int T, bool SWAP, bool SPLIT>
 __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, MxgArgs g) {
   using S = MxgShape<BN>;
@@ -187,16 +250,39 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
         for (int j = 0; j < CH; ++j)
           if (b0 + ch * CH + j < g.rows_b && a0 + row < g.rows_a) mxg_store<T>(g.d, (long long)(b0 + ch * CH + j) * g.ldd + a0 + row, __uint_as_float(v[j]));
       } else {
-        // 32 x CH values through the warp's own patch of shared memory: rows leave as consecutive elements
-        float* patch = part + q * 32 * (CH + 1);
-        __syncwarp();
+        // rows leave through the warp's patch of shared memory; 16-bit results gather two loads of 32 columns for a line
+        constexpr int EB = Elem<T>::bytes, CC = 128 / EB;
+        if constexpr (CH == 32 && BN * EB >= 128) {
+          if constexpr (EB == 2) {
+            if (ch & 1) continue;
+            uint32_t w[64];
 #pragma unroll
-        for (int j = 0; j < CH; ++j) patch[lane * (CH + 1) + j] = __uint_as_float(v[j]);
-        __syncwarp();
-        const int col = b0 + ch * CH + lane;
-        if (lane < CH && col < g.rows_b)
-          for (int r = 0; r < 32; ++r)
-            if (a0 + 32 * q + r < g.rows_a) mxg_store<T>(g.d, (long long)(a0 + 32 * q + r) * g.ldd + col, patch[r * (CH + 1) + lane]);
+            for (int j = 0; j < 32; ++j) w[j] = v[j];
+            mxg_ld32(trow + (ch + 1) * 32, w + 32);
+            mxg_ld_wait();
+            if (failed) {
+#pragma unroll
+              for (int j = 32; j < 64; ++j) w[j] = 0x7FC00000u;
+            }
+            unsigned char* st = base_p + q * 4096;
+            __syncwarp();
+            uint32_t packed[32];
+            mxg_pack<T, 64>(w, packed);
+            mxg_stage(st, lane, packed);
+            __syncwarp();
+            mxg_write_rows<T>(st, lane, g.d, g.ldd, a0 + 32 * q, (int)min(32ll, g.rows_a - a0 - 32 * q), b0 + ch * 32, (int)min((long long)CC, g.rows_b - b0 - ch * 32), g.vec);
+          } else {
+            unsigned char* st = base_p + q * 4096;
+            __syncwarp();
+            mxg_stage(st, lane, v);
+            __syncwarp();
+            mxg_write_rows<T>(st, lane, g.d, g.ldd, a0 + 32 * q, (int)min(32ll, g.rows_a - a0 - 32 * q), b0 + ch * 32, (int)min(32ll, g.rows_b - b0 - ch * 32), g.vec);
+          }
+        } else {     // fewer columns than a line
+#pragma unroll
+          for (int j = 0; j < CH; ++j)
+            if (b0 + ch * CH + j < g.rows_b && a0 + row < g.rows_a) mxg_store<T>(g.d, (long long)(a0 + row) * g.ldd + b0 + ch * CH + j, __uint_as_float(v[j]));
+        }
       }
     }
   }
@@ -229,6 +315,324 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
   tc_fence_before();
   __syncthreads();
   if (warp == 1) tc_dealloc(tmem, S::TMEM_COLS);
+}
+
+// ---- two multiprocessors on one tile ---------------------------------------------------------------------------------------
+// Large products.  A 128 x 256 tile a multiprocessor needs 51 KB of operands for 512 cycles of MMA, more than L2 delivers to all of
+// them at once (measured: 35 KB in 523 cycles); the pair of a cluster works on 256 x 256 with cta_group::2, each block holding its 128
+// rows of A and half of B's rows.  Both load their own parts and count them on the leader's barrier; the leader issues the MMAs for
+// both; its commits release the slots of both.  Each block keeps its 128 x 256 accumulators and the scales of all 256 rows of B.
+//
+// What bounds it is the time from a slot's release to its refill, about 1.4 us of L2 latency, over the slots that shared memory
+// holds; so the scales, whose way is longer, have rings of their own that run further ahead, and nothing else sits in the codes' ring.
+//
+//   warp 0      codes: TMA loads (leader's barrier)
+//   warp 1      tensor memory; in the leader one lane issues the MMAs
+//   warps 2-5   scales from shared to tensor memory with plain stores.  (tcgen05.cp by the issuing lane puts
+//               their latency into the codes' ring: 1190 cycles a stage instead of 784 without copies.)
+//   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers, frees the accumulators, and writes while the next
+//               tile's MMAs run: 32 bytes a lane, or through a kilobyte of shared memory where D's rows are not 32-byte aligned
+//   warp 14     scales: TMA loads (own barrier), eight stages deep
+// Persistent: the producers run ahead of the epilogue into the next tile.
+constexpr int MXP_THREADS = 480;
+constexpr int MXP_STAGES = 6;                                         // codes: 256 elements of k
+constexpr int MXP_SF_STAGES = 4, MXP_SFT_STAGES = 4;                  // scales of 512 elements of k: in shared memory, in tensor memory
+constexpr int MXP_HALF = 128 * 128;                                   // 128 rows x 128 bytes: A's rows, and this block's half of B's
+constexpr int MXP_SF_BYTES = 3 * 2048;                                // of 128 rows of A and 256 of B: four tiles of each 128 rows
+constexpr int MXP_OFF_SF = MXP_STAGES * 2 * MXP_HALF;
+constexpr int MXP_OFF_STORE = MXP_OFF_SF + MXP_SF_STAGES * MXP_SF_BYTES;    // 1 KB for each epilogue warp
+constexpr int MXP_OFF_BARS = MXP_OFF_STORE + 8 * 1024;
+constexpr int MXP_BARS = 2 * (MXP_STAGES + MXP_SF_STAGES + MXP_SFT_STAGES) + 2;
+constexpr int MXP_SMEM = MXP_OFF_BARS + 8 * MXP_BARS + 16 + 1024;
+constexpr int MXP_SCALE_COLS = 48;                                    // four tiles: 16 columns of A's scales, 32 of B's
+constexpr int MXP_TMEM_COLS = 512;
+static_assert(256 + MXP_SFT_STAGES * MXP_SCALE_COLS <= MXP_TMEM_COLS && MXP_SMEM <= 227 * 1024, "accumulators, scales and rings must fit");
+
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
+  uint32_t p;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(addr), "r"(rank));
+  return p;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+// Issued by one elected lane of a converged warp: with the whole warp in step the operands stay in uniform registers, where the
+// instruction wants them (a loop of one lane alone moved them there one by one: 890 cycles a stage instead of 620).
+__device__ __forceinline__ void mxp_commit(uint32_t bar) {            // to the barrier at this address in both blocks
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mxp_mma(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ uint32_t mxp_idesc(uint32_t id) {          // M = 256, N = 256
+  return (id << 4) | (1u << 7) | (1u << 10) | ((256u >> 3) << 17) | (1u << 23) | (2u << 27) | (id << 29);
+}
+__device__ __forceinline__ void mxp_st8(uint32_t taddr, const uint4 a, const uint4 b) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // a look, without waiting
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+
+// The warp's wait: one lane polls.  (A warp-wide poll is 32 accesses of the barrier, and with a dozen warps waiting those got in the way of
+// the copies' own arrivals.)
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+  bool ok = false;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
+  return __any_sync(0xFFFFFFFFu, ok);
+}
+// The same for a wait of microseconds: a look every 200 ns leaves the issue slots to the others (4096 x 8192 x 8192: 128 -> 122 us).
+__device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
+  int ok = 0;
+  if ((threadIdx.x & 31) == 0)
+    for (int i = 0; i < (1 << 23) && !ok; ++i) {
+      ok = mbar_test(bar, parity);
+      if (!ok) __nanosleep(200);
+    }
+  return __any_sync(0xFFFFFFFFu, ok);
+}
+
+// slot and parity of a ring, stepped
+struct MxpRing {
+  int s = 0;
+  uint32_t phase;
+  __device__ __forceinline__ explicit MxpRing(uint32_t first) : phase(first) {}
+  template <int N> __device__ __forceinline__ void step() { if (++s == N) { s = 0; phase ^= 1u; } }
+};
+
+template <int T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MXP_THREADS, 1)
+mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
+                    const __grid_constant__ CUtensorMap map_sb, MxgArgs g) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;      // the same offset in both blocks
+  unsigned char* base_p = smem_raw + (base - raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = cluster_rank();
+  const uint32_t bars = base + MXP_OFF_BARS;
+  constexpr int B_SF = 2 * MXP_STAGES, B_SFT = B_SF + 2 * MXP_SF_STAGES, B_ACC = B_SFT + 2 * MXP_SFT_STAGES;
+  auto full = [&](int s) { return bars + 8u * s; };                             // codes of both blocks have landed: the leader's count
+  auto empty = [&](int s) { return bars + 8u * (MXP_STAGES + s); };
+  auto sf_full = [&](int s) { return bars + 8u * (B_SF + s); };                 // this block's scales have landed in shared memory
+  auto sf_empty = [&](int s) { return bars + 8u * (B_SF + MXP_SF_STAGES + s); };
+  auto sft_full = [&](int s) { return bars + 8u * (B_SFT + s); };               // both blocks' scales are in tensor memory: the leader's count
+  auto sft_empty = [&](int s) { return bars + 8u * (B_SFT + MXP_SFT_STAGES + s); };
+  const uint32_t acc_full = bars + 8u * B_ACC, acc_empty = acc_full + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_p + MXP_OFF_BARS + 8 * MXP_BARS);
+
+  if (tid == 0) {
+    for (int s = 0; s < MXP_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < MXP_SF_STAGES; ++s) { mbar_init(sf_full(s), 1); mbar_init(sf_empty(s), 4); }
+    for (int s = 0; s < MXP_SFT_STAGES; ++s) { mbar_init(sft_full(s), 8); mbar_init(sft_empty(s), 1); }
+    mbar_init(acc_full, 1);
+    mbar_init(acc_empty, 16);                                                   // eight epilogue warps of each block
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_slot)), "r"(MXP_TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                                           // barriers of both blocks are set up
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot, sf_cols = tmem + 256;
+  const int stages = (g.kb + 1) / 2, sf_stages = (g.kb + 3) / 4, n_tiles = g.tiles_a * g.tiles_b, pairs = (int)gridDim.x >> 1;
+  bool failed = false;
+
+  // tiles in bands of eight of A: pairs that run together share rows of both operands in L2
+  auto tile_at = [&](int tile, int& a0, int& b0) {
+    const int band = tile / (8 * g.tiles_b), in_band = tile % (8 * g.tiles_b), band_rows = min(8, g.tiles_a - band * 8);
+    a0 = (band * 8 + in_band % band_rows) * 256 + (int)rank * 128;
+    b0 = in_band / band_rows * 256;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      MxpRing r(1);
+      for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
+        int a0, b0;
+        tile_at(tile, a0, b0);
+        for (int it = 0; it < stages; ++it, r.step<MXP_STAGES>()) {
+          if (!mbar_wait(empty(r.s), r.phase)) { failed = true; break; }
+          const uint32_t at = base + (uint32_t)r.s * (2 * MXP_HALF), bar = cluster_addr(full(r.s), 0);
+          if (rank == 0) mbar_arrive_expect_tx(full(r.s), 4u * MXP_HALF);
+          tma_load_2d_pair(at, &map_a, it * 128, a0, bar);
+          tma_load_2d_pair(at + MXP_HALF, &map_b, it * 128, b0 + (int)rank * 128, bar);
+        }
+      }
+      if (failed)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);                       // let what is in flight land
+    }
+    __syncwarp();
+  } else if (warp == 14) {
+    if (lane == 0) {
+      MxpRing r(1);
+      for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
+        int a0, b0;
+        tile_at(tile, a0, b0);
+        const int sa_row = (a0 >> 7) * g.kb, sb_row = (b0 >> 7) * g.kb;         // rows of the scales' tensors: tiles (zeros outside)
+        for (int it = 0; it < sf_stages; ++it, r.step<MXP_SF_STAGES>()) {
+          if (!mbar_wait(sf_empty(r.s), r.phase)) { failed = true; break; }
+          const uint32_t sc = base + MXP_OFF_SF + (uint32_t)r.s * MXP_SF_BYTES;
+          mbar_arrive_expect_tx(sf_full(r.s), MXP_SF_BYTES);
+          tma_load_2d(sc, &map_sa, 0, sa_row + 4 * it, sf_full(r.s));
+          tma_load_2d(sc + 2048, &map_sb, 0, sb_row + 4 * it, sf_full(r.s));
+          tma_load_2d(sc + 4096, &map_sb, 0, sb_row + g.kb + 4 * it, sf_full(r.s));
+        }
+      }
+      if (failed)
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (rank == 0) {
+      // The MMA pipe queues about two instructions, 270 cycles of work.  What the thread does between the last MMA of a stage and the
+      // first of the next has to be shorter, so the next stage's barriers are looked at while this one's MMAs are queued.
+      const uint64_t adesc0 = tc_desc_kmajor(base), bdesc0 = tc_desc_kmajor(base + MXP_HALF);
+      MxpRing r(0), rs(0);
+      uint32_t acc_phase = 1;
+      bool codes = false, scales = false;                                       // known to be there
+      for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs, acc_phase ^= 1u) {
+        if (!mbar_wait_warp(acc_empty, acc_phase)) { failed = true; break; }    // both blocks have read the last tile's accumulators
+        for (int it = 0; it < stages; ++it) {
+          const bool first = (it & 1) == 0, last = !first || it == stages - 1;  // of the two stages that share a slot of scales
+          if (first && !scales && !mbar_wait_warp(sft_full(rs.s), rs.phase)) { failed = true; break; }
+          if (!codes && !mbar_wait_warp(full(r.s), r.phase)) { failed = true; break; }
+          tc_fence_after();
+          const uint64_t ad = adesc0 + (uint32_t)(r.s * (2 * MXP_HALF / 16)), bd = bdesc0 + (uint32_t)(r.s * (2 * MXP_HALF / 16));
+          const uint32_t sf = sf_cols + (uint32_t)(rs.s * MXP_SCALE_COLS), sfa = sf + (first ? 0u : 8u), sfb = sf + (first ? 16u : 32u);
+          mxp_mma(tmem, ad, bd, mxp_idesc(0), sfa, sfb, it > 0 ? 1u : 0u);
+          mxp_mma(tmem, ad + 2, bd + 2, mxp_idesc(2), sfa, sfb, 1u);
+          const int s_now = r.s, rs_now = rs.s;
+          r.step<MXP_STAGES>();
+          codes = __all_sync(0xFFFFFFFFu, mbar_test(full(r.s), r.phase));
+          if (last) {
+            rs.step<MXP_SFT_STAGES>();
+            scales = __all_sync(0xFFFFFFFFu, mbar_test(sft_full(rs.s), rs.phase));
+          }
+          if (2 * it + 1 < g.kb) {
+            mxp_mma(tmem, ad + 4, bd + 4, mxp_idesc(0), sfa + 4, sfb + 8, 1u);
+            mxp_mma(tmem, ad + 6, bd + 6, mxp_idesc(2), sfa + 4, sfb + 8, 1u);
+          }
+          mxp_commit(empty(s_now));
+          if (last) mxp_commit(sft_empty(rs_now));
+          if (it == stages - 1) mxp_commit(acc_full);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp < 6) {
+    // a lane holds rows l, 32 + l, 64 + l, 96 + l of each 512-byte tile: four columns of its tensor-memory lane; the four warps
+    // write the same to their quarters of the lanes
+    const uint32_t trow = sf_cols + ((uint32_t)(32 * (warp & 3)) << 16);
+    MxpRing r(0), rs(1);
+    for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
+      for (int it = 0; it < sf_stages; ++it, r.step<MXP_SF_STAGES>(), rs.step<MXP_SFT_STAGES>()) {
+        if (!mbar_wait_warp(sf_full(r.s), r.phase)) { failed = true; break; }
+        const uint4* t = reinterpret_cast<const uint4*>(base_p + MXP_OFF_SF + r.s * MXP_SF_BYTES) + lane;
+        uint4 a[4], b[2][4];                                                    // [128 rows of B][k]
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { a[k] = t[32 * k]; b[0][k] = t[128 + 32 * k]; b[1][k] = t[256 + 32 * k]; }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sf_empty(r.s));
+        if (!mbar_wait_warp(sft_empty(rs.s), rs.phase)) { failed = true; break; }
+        tc_fence_after();
+        const uint32_t at = trow + (uint32_t)(rs.s * MXP_SCALE_COLS);
+        mxp_st8(at, a[0], a[1]);
+        mxp_st8(at + 8, a[2], a[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mxp_st8(at + 16 + 8 * k, b[0][k], b[1][k]);
+        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_addr(sft_full(rs.s), 0));
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 6) >> 2;
+    const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16) + 128 * half, done = cluster_addr(acc_empty, 0);
+    unsigned char* st = base_p + MXP_OFF_STORE + (warp - 6) * 1024;
+    uint32_t phase = 0;
+    for (int tile = (int)blockIdx.x >> 1; tile < n_tiles; tile += pairs, phase ^= 1u) {
+      int a0, b0;
+      tile_at(tile, a0, b0);
+      a0 += 32 * q;
+      b0 += 128 * half;
+      if (!failed && !mbar_wait_warp_long(acc_full, phase)) failed = true;                // from then on every tile of this block is NaN
+      tc_fence_after();
+      const int rows = (int)max(0ll, min(32ll, g.rows_a - a0));
+      constexpr int EB = Elem<T>::bytes, CC = 128 / EB;                         // columns of a 128-byte line
+      constexpr int GROUP = EB == 2 ? 128 : 64;                                 // columns taken into registers at a time
+#pragma unroll
+      for (int c0 = 0; c0 < 128; c0 += GROUP) {
+        uint32_t w[64];
+        if constexpr (EB == 2) {
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            uint32_t v[32];
+            mxg_ld32(trow + 32 * h, v);
+            mxg_ld_wait();
+            mxg_pack<T, 32>(v, w + 16 * h);
+          }
+        } else {
+          mxg_ld32(trow + c0, w);
+          mxg_ld32(trow + c0 + 32, w + 32);
+          mxg_ld_wait();
+        }
+        if (c0 + GROUP == 128) {                                                // the accumulators are read: the next tile may start
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive_cluster(done);
+        }
+        if (failed) {
+#pragma unroll
+          for (int j = 0; j < 64; ++j) w[j] = EB == 2 ? 0x7FC07FC0u : 0x7FC00000u;
+        }
+        const long long cols = g.rows_b - b0 - c0;                              // columns that exist from here on
+        if (g.vec && cols >= GROUP) {
+          // a lane writes its row, 32 bytes at a time
+          char* out = static_cast<char*>(g.d) + ((long long)(a0 + lane) * g.ldd + b0 + c0) * EB;
+          if (lane < rows) {
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 32 * p), "r"(w[8 * p]), "r"(w[8 * p + 1]), "r"(w[8 * p + 2]),
+                           "r"(w[8 * p + 3]), "r"(w[8 * p + 4]), "r"(w[8 * p + 5]), "r"(w[8 * p + 6]), "r"(w[8 * p + 7]) : "memory");
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < GROUP; c += CC) {
+            // eight rows at a time through the warp's kilobyte
+#pragma unroll 1
+            for (int r8 = 0; r8 < 4; ++r8) {
+              __syncwarp();
+              if ((lane >> 3) == r8) mxg_stage(st, lane & 7, w + c * EB / 4);
+              __syncwarp();
+              mxg_write_rows<T>(st, lane, g.d, g.ldd, a0 + 8 * r8, min(8, rows - 8 * r8), b0 + c0 + c, (int)max(0ll, min((long long)CC, cols - c)), 0);
+            }
+          }
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                        // nobody leaves while the other may still load, commit or arrive here
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(MXP_TMEM_COLS) : "memory");
 }
 
 }  // namespace ssim

@@ -55,6 +55,26 @@ bool make_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t cols
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// scale tiles as a 2-D tensor of 512-byte rows; box: four tiles that follow one another along k
+bool make_scale_map(CUtensorMap* map, const uint8_t* scales, int64_t rows, int64_t kb) {
+  PFN_encodeTiled fn = tc_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[2] = {128, (cuuint64_t)((rows + 127) / 128 * kb)};
+  const cuuint64_t strides[1] = {512};
+  const cuuint32_t box[2] = {128, 4}, one[2] = {1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(scales), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int T>
+cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& msa, const CUtensorMap& msb, const MxgArgs& g, int sms, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(mx_gemm_pair_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXP_SMEM);
+  if (e != cudaSuccess) return e;
+  const long long tiles = (long long)g.tiles_a * g.tiles_b, pairs = sms / 2;
+  mx_gemm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MXP_THREADS, MXP_SMEM, st>>>(ma, mb, msa, msb, g);
+  return cudaGetLastError();
+}
+
 template <int BN, int T, bool SWAP, bool SPLIT>
 cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
   auto kern = mx_gemm_kernel<BN, T, SWAP, SPLIT>;
@@ -87,7 +107,7 @@ cudaError_t launch_bn(int bn, const CUtensorMap& ma, const CUtensorMap& mb, cons
     case 32: return launch_split<32, T, SWAP>(ma, mb, g, split, st);
     case 64: return launch_split<64, T, SWAP>(ma, mb, g, split, st);
     case 128: return launch_split<128, T, SWAP>(ma, mb, g, split, st);
-    default: return launch<256, T, SWAP, false>(ma, mb, g, 1, st);
+    default: return cudaErrorInvalidValue;
   }
 }
 
@@ -155,11 +175,11 @@ sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const 
   const int kb = (int)((K + 127) / 128), sms = sm_count();
   const int64_t tiles_a = (ra + 127) / 128;
   int bn = rb <= 16 ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
-  if (rb > 128 && tiles_a * ((rb + 255) / 256) >= sms) bn = 256;
+  const bool pair = ra > 128 && rb > 128 && (ra + 255) / 256 * ((rb + 255) / 256) >= sms / 4;
   const int64_t tiles_b = (rb + bn - 1) / bn;
   if (tiles_a * tiles_b > (int64_t)1 << 30) return record_error(SIM_ERR_ARG, "sim_mx_matmul: the result has too many tiles");
   int split = 1;
-  if (bn < 256)     // fewer tiles than two a multiprocessor: split k over a cluster, four 128-element blocks each at least
+  if (!pair)     // fewer tiles than two a multiprocessor: split k over a cluster, four 128-element blocks each at least
     while (split < 8 && tiles_a * tiles_b * split * 2 <= 2 * sms && kb >= split * 2 * 4) split *= 2;
   MxgArgs g{};
   g.a_scales = swap ? b_scales : a_scales; g.b_scales = swap ? a_scales : b_scales;
@@ -170,10 +190,20 @@ sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const 
   g.d = c; g.ldd = ldc;
   g.vec = aligned(c, 16) && ldc * elem_bytes(type) % 16 == 0 ? 1 : 0;
   CUtensorMap ma, mb;
-  if (!make_map(&ma, swap ? b_codes : a_codes, ra, K, 128) || !make_map(&mb, swap ? a_codes : b_codes, rb, K, (uint32_t)bn))
-    return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
+  if (pair) {
+    CUtensorMap msa, msb;
+    g.vec = aligned(c, 32) && ldc * elem_bytes(type) % 32 == 0 ? 1 : 0;
+    g.a_scales = a_scales; g.b_scales = b_scales; g.rows_a = M; g.rows_b = N;
+    g.tiles_a = (int)((M + 255) / 256); g.tiles_b = (int)((N + 255) / 256);
+    if (!make_map(&ma, a_codes, M, K, 128) || !make_map(&mb, b_codes, N, K, 128) || !make_scale_map(&msa, a_scales, M, kb) || !make_scale_map(&msb, b_scales, N, kb))
+      return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
+    e = type == SIM_F32 ? launch_pair<T_F32>(ma, mb, msa, msb, g, sms, st) : launch_pair<T_BF16>(ma, mb, msa, msb, g, sms, st);
+    return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_matmul", e);
+  }
+  if (!make_map(&ma, swap ? b_codes : a_codes, ra, K, 128) || !make_map(&mb, swap ? a_codes : b_codes, rb, K, (uint32_t)bn))
+    return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
   if (type == SIM_F32) e = swap ? launch_bn<T_F32, true>(bn, ma, mb, g, split, st) : launch_bn<T_F32, false>(bn, ma, mb, g, split, st);
   else e = swap ? launch_bn<T_BF16, true>(bn, ma, mb, g, split, st) : launch_bn<T_BF16, false>(bn, ma, mb, g, split, st);
   return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_matmul", e);

@@ -178,7 +178,7 @@ def product_case(B, M, N, K, dtype, seed=0, out=None):
 # all widths of B's tile (16, 32, 64, 128, 256), both roles, ragged and tiny sizes, k of one block to many, split and whole
 PRODUCTS = [(1, 1, 1), (1, 128, 32), (1, 1000, 4096), (2, 300, 500), (16, 256, 256), (17, 129, 1000), (31, 500, 130), (33, 1000, 700), (64, 640, 2048),
             (65, 100, 300), (100, 65, 260), (128, 128, 128), (129, 257, 385), (300, 7, 900), (500, 40, 1500), (1000, 64, 64), (257, 129, 33),
-            (1500, 3000, 128), (2050, 2047, 515), (5000, 1, 200), (1, 20000, 160)]
+            (1500, 3000, 128), (2050, 2047, 515), (2500, 2600, 200), (2561, 5130, 140), (5000, 1, 200), (1, 20000, 160)]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
