@@ -188,6 +188,60 @@ template <> struct Elem<T_F16> {
   }
 };
 
+// ---- eight consecutive elements as they are stored: their largest magnitude without unpacking 16-bit types ----------------
+template <int T> struct Raw8;
+template <> struct Raw8<T_F32> {
+  uint32_t w[8];
+  __device__ __forceinline__ void load(const void* p, long long i) {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + i);
+    const uint4 a = q[0], b = q[1];
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+  }
+  __device__ __forceinline__ void load_some(const void* p, long long i, int n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = e < n ? static_cast<const uint32_t*>(p)[i + e] : 0u;
+  }
+  __device__ __forceinline__ float value(int e) const { return __uint_as_float(w[e]); }
+  __device__ __forceinline__ uint32_t amax() const {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(w[e]);
+    return amax8(v);
+  }
+};
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int T> struct Raw16 {      // bf16 and fp16: two elements a word
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const void* p, long long i) {
+    const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i);
+    w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+  }
+  __device__ __forceinline__ void load_some(const void* p, long long i, int n) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t lo = 2 * k < n ? static_cast<const uint16_t*>(p)[i + 2 * k] : 0u, hi = 2 * k + 1 < n ? static_cast<const uint16_t*>(p)[i + 2 * k + 1] : 0u;
+      w[k] = lo | hi << 16;
+    }
+  }
+  __device__ __forceinline__ float value(int e) const {
+    const uint32_t x = w[e >> 1];
+    if (T == T_BF16) return __uint_as_float((e & 1) ? x & 0xFFFF0000u : x << 16);
+    return f16_to_float((e & 1) ? x >> 16 : x & 0xFFFFu);
+  }
+  // magnitudes compare as the integers that their bits are (an infinity or a NaN above every number)
+  __device__ __forceinline__ uint32_t amax() const {
+    const uint32_t m = max_u16x2(max_u16x2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), max_u16x2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+    return widen(max(m >> 16, m & 0xFFFFu));
+  }
+  static __device__ __forceinline__ uint32_t widen(uint32_t h) { return T == T_BF16 ? h << 16 : __float_as_uint(f16_to_float(h)); }
+};
+template <> struct Raw8<T_BF16> : Raw16<T_BF16> {};
+template <> struct Raw8<T_F16> : Raw16<T_F16> {};
+
 // eight MXFP4 codes of one word -> values in units of the scale
 __device__ __forceinline__ void e2m1x8(uint32_t w, float (&v)[8]) {
 #pragma unroll

@@ -2,10 +2,10 @@
 //
 // tcgen05.mma kind::mxf4 multiplies 4-bit operands with a scale per 32 elements of k; one instruction takes 128 rows of A, BN rows
 // of B and 64 elements of k.  A stage holds 256 elements of k: 128 bytes a row, one swizzle atom, loaded by TMA; the rows'
-// scales come as whole 512-byte tiles (128 rows x 128 elements of k, mx_kernel.cuh) by bulk copies and go from shared into tensor
+// scales come as whole 512-byte tiles (128 rows x 128 elements of k, mx_kernel.cuh), two to a TMA box, and go from shared into tensor
 // memory with tcgen05.cp, into columns of their own for each stage of the ring, so that a stage's release also frees them.
 //
-//   warp 0     producer: TMA loads and bulk copies into the ring
+//   warp 0     producer: TMA loads into the ring
 //   warp 1     allocates tensor memory; one lane issues the copies of the scales and the MMAs
 //   warps 2-5  epilogue: accumulators from tensor memory to D
 //
@@ -23,23 +23,20 @@ namespace ssim {
 constexpr int MXG_THREADS = 192;
 constexpr int MXG_A_BYTES = 128 * 128;
 
-template <int BN>
+template <int BN>      // 16, 32, 64 or 128 rows of B
 struct MxgShape {
-  static constexpr int NT = BN > 128 ? BN / 128 : 1;                 // scale tiles of B
   static constexpr int B_BYTES = BN * 128;
-  static constexpr int SCALE_BYTES = 1024 * (1 + NT);                // two tiles of A, two of each 128 rows of B
+  static constexpr int SCALE_BYTES = 2 * 1024;                       // two tiles of A's scales, two of B's
   static constexpr int STAGE_BYTES = MXG_A_BYTES + B_BYTES + SCALE_BYTES;
-  static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 3 : BN == 16 ? 5 : 4;
-  static constexpr int SCALE_COLS = 8 + 8 * NT;                      // tensor-memory columns of a stage's scales
+  static constexpr int STAGES = BN == 128 ? 3 : BN == 16 ? 5 : 4;    // about 100 KB: two blocks to a multiprocessor
+  static constexpr int SCALE_COLS = 16;                              // tensor-memory columns of a stage's scales
   static constexpr int USED_COLS = BN + STAGES * SCALE_COLS;
-  static constexpr int TMEM_COLS = USED_COLS <= 128 ? 128 : USED_COLS <= 256 ? 256 : 512;
+  static constexpr int TMEM_COLS = USED_COLS <= 128 ? 128 : 256;
   static constexpr int OFF_BARS = STAGES * STAGE_BYTES;
   static constexpr int SMEM = OFF_BARS + 8 * (2 * STAGES + 1) + 16 + 1024;   // slack for the alignment to 1024 bytes
 };
 
 struct MxgArgs {
-  const uint8_t* a_scales;
-  const uint8_t* b_scales;
   long long rows_a, rows_b;
   int kb;                  // 128-element blocks of k
   int kb_split;            // of them for each block of the cluster (even)
@@ -49,16 +46,30 @@ struct MxgArgs {
   int vec;                 // D's rows allow 16-byte stores
 };
 
+// Issued by one elected lane of a converged warp: with the whole warp in step the operands stay in uniform registers, where the
+// instruction wants them.
 __device__ __forceinline__ void mxg_mma(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mxg_commit(uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 // 512 bytes of shared memory, 32 rows of 16, to four tensor-memory columns of every quarter of the lanes
 __device__ __forceinline__ void mxg_copy_scales(uint32_t taddr, uint32_t saddr) {
   const uint64_t desc = (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);   // 8-row groups 128 B apart, no swizzle
-  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+// The warp's wait: one lane polls.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
+  bool ok = false;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
+  return __any_sync(0xFFFFFFFFu, ok);
 }
 // A and B E2M1, scales E8M0, M = 128, N = n; id: which half of a column's four scale bytes (0 or 2)
 __device__ __forceinline__ uint32_t mxg_idesc(int n, uint32_t id) {
@@ -68,11 +79,14 @@ __device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("m
 __device__ __forceinline__ void cluster_sync_all() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
   uint32_t p;
-  float v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(p) : "memory");
+  return p;
+}
+__device__ __forceinline__ float4 ld_cluster4(uint32_t cluster_ptr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_ptr) : "memory");
   return v;
 }
 
@@ -143,7 +157,8 @@ __device__ __forceinline__ void mxg_ld32(uint32_t taddr, uint32_t* v) {
 __device__ __forceinline__ void mxg_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 template <int BN, int T, bool SWAP, bool SPLIT>
-__global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, MxgArgs g) {
+__global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                              const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb, MxgArgs g) {
   using S = MxgShape<BN>;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -167,6 +182,7 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
     for (int s = 0; s < S::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(acc_bar, 1);
     mbar_fence_init();
+    prefetch_map(&map_a); prefetch_map(&map_b); prefetch_map(&map_sa); prefetch_map(&map_sb);
   }
   if (warp == 1) tc_alloc(smem_addr(tmem_slot), S::TMEM_COLS);
   tc_fence_before();
@@ -177,18 +193,17 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 
   if (warp == 0) {
     if (lane == 0) {
-      const int b_tile0 = b0 >> 7, b_tiles = min(S::NT, (int)((g.rows_b + 127) >> 7) - b_tile0);
+      const int sa_row = (a0 >> 7) * g.kb, sb_row = (b0 >> 7) * g.kb;      // rows of the scales' tensors: tiles (zeros outside)
       int issued = 0;
       for (int it = 0; it < stages; ++it) {
-        const int s = it % S::STAGES, k0 = k_begin + 2 * it, nk = min(2, k_end - k0);
+        const int s = it % S::STAGES, k0 = k_begin + 2 * it;
         if (!mbar_wait(empty(s), (uint32_t)(((it / S::STAGES) & 1) ^ 1))) { failed = true; break; }
         const uint32_t at = base + (uint32_t)s * S::STAGE_BYTES, sc = at + MXG_A_BYTES + S::B_BYTES;
-        mbar_arrive_expect_tx(full(s), (uint32_t)(MXG_A_BYTES + S::B_BYTES + 512 * nk * (1 + b_tiles)));
+        mbar_arrive_expect_tx(full(s), (uint32_t)S::STAGE_BYTES);
         tma_load_2d(at, &map_a, k0 * 64, a0, full(s));
         tma_load_2d(at + MXG_A_BYTES, &map_b, k0 * 64, b0, full(s));
-        bulk_g2s(sc, g.a_scales + ((long long)(a0 >> 7) * g.kb + k0) * 512, (uint32_t)(512 * nk), full(s));
-        for (int t = 0; t < b_tiles; ++t)
-          bulk_g2s(sc + 1024u * (1 + t), g.b_scales + ((long long)(b_tile0 + t) * g.kb + k0) * 512, (uint32_t)(512 * nk), full(s));
+        tma_load_2d(sc, &map_sa, 0, sa_row + k0, full(s));
+        tma_load_2d(sc + 1024, &map_sb, 0, sb_row + k0, full(s));
         issued = it + 1;
       }
       if (failed)     // let what is in flight land (a bounded time) before the block gives up its shared memory
@@ -197,31 +212,30 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
     __syncwarp();
   } else if (warp == 1) {
     const uint32_t sf_base = tmem + BN, b_col = (uint32_t)((b0 & 127) >> 5);
+    const uint64_t adesc0 = tc_desc_kmajor(base), bdesc0 = tc_desc_kmajor(base + MXG_A_BYTES);
+    int s = 0;
+    uint32_t phase = 0;
     for (int it = 0; it < stages; ++it) {
-      const int s = it % S::STAGES, nk = min(2, k_end - (k_begin + 2 * it));
-      if (!mbar_wait(full(s), (uint32_t)((it / S::STAGES) & 1))) { failed = true; break; }
+      const int nk = min(2, k_end - (k_begin + 2 * it));
+      if (!mbar_wait_warp(full(s), phase)) { failed = true; break; }
       tc_fence_after();
-      if (lane == 0) {
-        const uint32_t at = base + (uint32_t)s * S::STAGE_BYTES, bt = at + MXG_A_BYTES, sc = bt + S::B_BYTES;
-        const uint32_t sfa = sf_base + (uint32_t)(s * S::SCALE_COLS), sfb = sfa + 8;
-        for (int k = 0; k < nk; ++k) {
-          mxg_copy_scales(sfa + 4 * k, sc + 512 * k);
-#pragma unroll
-          for (int t = 0; t < S::NT; ++t) mxg_copy_scales(sfb + 4 * (S::NT * k + t), sc + 1024 * (1 + t) + 512 * k);
-        }
-        for (int k = 0; k < nk; ++k) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            mxg_mma(tmem, tc_desc_kmajor(at + 64 * k + 32 * h), tc_desc_kmajor(bt + 64 * k + 32 * h), mxg_idesc(BN, 2 * h), sfa + 4 * k,
-                    sfb + 4 * S::NT * k + b_col, (it > 0 || k > 0 || h > 0) ? 1u : 0u);
-        }
-        tc_commit(empty(s));
-        if (it == stages - 1) tc_commit(acc_bar);
+      const uint32_t sc = base + (uint32_t)s * S::STAGE_BYTES + MXG_A_BYTES + S::B_BYTES;
+      const uint32_t sfa = sf_base + (uint32_t)(s * S::SCALE_COLS), sfb = sfa + 8;
+      const uint64_t ad = adesc0 + (uint32_t)(s * (S::STAGE_BYTES / 16)), bd = bdesc0 + (uint32_t)(s * (S::STAGE_BYTES / 16));
+      for (int k = 0; k < nk; ++k) {
+        mxg_copy_scales(sfa + 4 * k, sc + 512 * k);
+        mxg_copy_scales(sfb + 4 * k, sc + 1024 + 512 * k);
       }
-      __syncwarp();
+      for (int k = 0; k < nk; ++k) {
+        mxg_mma(tmem, ad + 4 * k, bd + 4 * k, mxg_idesc(BN, 0), sfa + 4 * k, sfb + 4 * k + b_col, (it > 0 || k > 0) ? 1u : 0u);
+        mxg_mma(tmem, ad + 4 * k + 2, bd + 4 * k + 2, mxg_idesc(BN, 2), sfa + 4 * k, sfb + 4 * k + b_col, 1u);
+      }
+      mxg_commit(empty(s));
+      if (it == stages - 1) mxg_commit(acc_bar);
+      if (++s == S::STAGES) { s = 0; phase ^= 1u; }
     }
   } else {
-    if (!mbar_wait(acc_bar, 0)) failed = true;
+    if (!mbar_wait_warp(acc_bar, 0)) failed = true;
     tc_fence_after();
     const int q = warp & 3, row = 32 * q + lane;
     const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16);
@@ -243,8 +257,14 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
         for (int j = 0; j < CH; ++j) v[j] = 0x7FC00000u;
       }
       if (SPLIT) {
+        if (SWAP) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) part[SWAP ? (ch * CH + j) * 128 + row : row * (BN + 1) + ch * CH + j] = __uint_as_float(v[j]);
+          for (int j = 0; j < CH; ++j) part[(ch * CH + j) * 128 + row] = __uint_as_float(v[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < CH; j += 4)
+            *reinterpret_cast<uint4*>(part + row * (BN + 4) + ch * CH + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        }
       } else if (SWAP) {
 #pragma unroll
         for (int j = 0; j < CH; ++j)
@@ -290,24 +310,32 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
   if (SPLIT) {
     __syncthreads();
     cluster_sync_all();
-    const uint32_t rank = cluster_rank(), n = gridDim.y;
-    const uint32_t part = base;
-    constexpr int W = BN + 1;
-    if (SWAP) {      // columns of A's rows side by side: block `rank` adds columns rank, rank + n, ... of B's rows
-      for (int i = tid; i < 128 * BN; i += MXG_THREADS) {
-        const int j = i >> 7, row = i & 127;
-        if (j % (int)n != (int)rank || b0 + j >= g.rows_b || a0 + row >= g.rows_a) continue;
-        float s = 0.f;
-        for (uint32_t r = 0; r < n; ++r) s += ld_cluster(part + 4u * (uint32_t)(j * 128 + row), r);
-        mxg_store<T>(g.d, (long long)(b0 + j) * g.ldd + a0 + row, s);
-      }
-    } else {
-      for (int i = tid; i < 128 * BN; i += MXG_THREADS) {
-        const int row = i / BN, j = i % BN;
-        if (row % (int)n != (int)rank || b0 + j >= g.rows_b || a0 + row >= g.rows_a) continue;
-        float s = 0.f;
-        for (uint32_t r = 0; r < n; ++r) s += ld_cluster(part + 4u * (uint32_t)(row * W + j), r);
-        mxg_store<T>(g.d, (long long)(a0 + row) * g.ldd + b0 + j, s);
+    // the block of rank r adds the r-th part of the tile, four neighbours of a line at a time, over the blocks in their order
+    const int rank = (int)cluster_rank(), n = (int)gridDim.y;
+    constexpr int ITEMS = 128 * BN / 4, LINE = SWAP ? 32 : BN / 4, PITCH = SWAP ? 128 : BN + 4;
+    for (int i = ITEMS * rank / n + tid; i < ITEMS * (rank + 1) / n; i += MXG_THREADS) {
+      const int line = i / LINE, at = i % LINE * 4;
+      const uint32_t where = base + 4u * (uint32_t)(line * PITCH + at);
+      float4 v[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
+        if (r < n) v[r] = ld_cluster4(cluster_addr(where, (uint32_t)r));
+      float4 t = v[0];
+#pragma unroll
+      for (int r = 1; r < 8; ++r)
+        if (r < n) { t.x += v[r].x; t.y += v[r].y; t.z += v[r].z; t.w += v[r].w; }
+      const long long out_row = SWAP ? b0 + line : a0 + line, out_col = SWAP ? a0 + at : b0 + at;
+      const long long rows = SWAP ? g.rows_b : g.rows_a, cols = SWAP ? g.rows_a : g.rows_b;
+      if (out_row >= rows) continue;
+      const long long to = out_row * g.ldd + out_col;
+      if (g.vec && out_col + 4 <= cols) {
+        if (T == T_F32) *reinterpret_cast<float4*>(static_cast<float*>(g.d) + to) = t;
+        else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(g.d) + to) = make_uint2(float_to_bf16x2(t.x, t.y), float_to_bf16x2(t.z, t.w));
+      } else {
+        const float e[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (out_col + j < cols) mxg_store<T>(g.d, to + j, e[j]);
       }
     }
     cluster_sync_all();          // nobody leaves while its partial sums may still be read
@@ -348,11 +376,6 @@ constexpr int MXP_SCALE_COLS = 48;                                    // four ti
 constexpr int MXP_TMEM_COLS = 512;
 static_assert(256 + MXP_SFT_STAGES * MXP_SCALE_COLS <= MXP_TMEM_COLS && MXP_SMEM <= 227 * 1024, "accumulators, scales and rings must fit");
 
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
-  uint32_t p;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(addr), "r"(rank));
-  return p;
-}
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
@@ -388,14 +411,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
   return ok != 0;
 }
 
-// The warp's wait: one lane polls.  (A warp-wide poll is 32 accesses of the barrier, and with a dozen warps waiting those got in the way of
-// the copies' own arrivals.)
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
-  bool ok = false;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
-  return __any_sync(0xFFFFFFFFu, ok);
-}
-// The same for a wait of microseconds: a look every 200 ns leaves the issue slots to the others (4096 x 8192 x 8192: 128 -> 122 us).
+// The warp's wait of microseconds: a look every 200 ns leaves the issue slots to the others (4096 x 8192 x 8192: 128 -> 122 us).
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
   int ok = 0;
   if ((threadIdx.x & 31) == 0)

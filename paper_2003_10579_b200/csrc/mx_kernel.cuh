@@ -26,59 +26,78 @@ struct MxQuantArgs {
   uint8_t* codes_t;      // of the columns (the transpose's rows), or null
   uint8_t* scales_t;
   int tiles, stochastic, vec;
-  uint64_t seed;
+  PhiloxKeys keys;
 };
 
-__device__ __forceinline__ U4 mx_random(uint64_t seed, uint32_t tag, unsigned long long group, unsigned long long row) {
-  return philox4x32_10((uint32_t)seed, (uint32_t)(seed >> 32), (uint32_t)group, (tag << 24) | (uint32_t)(group >> 32), (uint32_t)row, (uint32_t)(row >> 32));
+__device__ __forceinline__ U4 mx_random(const PhiloxKeys& keys, uint32_t tag, unsigned long long group, unsigned long long row) {
+  return philox_keyed(keys, (uint32_t)group, (tag << 24) | (uint32_t)(group >> 32), (uint32_t)row, (uint32_t)(row >> 32));
 }
 
-// eight values -> eight codes; inv = 1 / scale
+// eight values times inv = 1 / scale -> eight codes
 template <bool SR>
-__device__ __forceinline__ uint32_t encode_e2m1(const float (&x)[8], float inv, const U4& u) {
-  uint32_t w = 0;
+__device__ __forceinline__ uint32_t encode_e2m1(float (&x)[8], float inv, const U4& u) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    float a = x[2 * k] * inv, b = x[2 * k + 1] * inv;
-    if (SR) {
-      a = round_stochastic<1, 0>(a, half_word(u, 2 * k));
-      b = round_stochastic<1, 0>(b, half_word(u, 2 * k + 1));
-    }
-    w |= to_e2m1x2(a, b) << (8 * k);
-  }
-  return w;
-}
-
-// Rows only.  A thread takes eight elements, four neighbouring lanes a block; rows are padded to 128 elements, so a block of lanes
-// never spans two rows.
-template <int T, bool SR>
-__global__ void __launch_bounds__(256) mx_quantize_rows_kernel(MxQuantArgs a) {
-  const long long kb = (a.cols + 127) / 128, groups = kb * 16, blocks = (a.cols + 31) / 32, pitch = kb * 64;
-  const long long step = (long long)gridDim.x * blockDim.x, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long drow = step / groups, dgrp = step % groups;
-  long long row = first / groups, grp = first % groups;
-  // all four lanes of a block run the same number of rounds: their groups differ only in the last two bits
-  for (; row < a.rows; row += drow, grp += dgrp, row += grp >= groups, grp -= grp >= groups ? groups : 0) {
-    const long long c = grp * 8;
-    const char* src = static_cast<const char*>(a.x) + (row * a.ld) * Elem<T>::bytes;
-    float x[8];
-    if (a.vec && c + 8 <= a.cols) {
-      Elem<T>::get8(src, c, x);
+  for (int e = 0; e < 8; ++e) x[e] *= inv;
+  if (SR) {
+    if (amin8(x) >= 1.f) {                                      // all normal in E2M1
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = round_normal<1>(x[e], half_word(u, e));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = c + e < a.cols ? Elem<T>::get(src, c + e) : 0.f;
+      for (int e = 0; e < 8; ++e) x[e] = round_stochastic<1, 0>(x[e], half_word(u, e));
     }
-    uint32_t amax = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[e]) & ABS_MASK);
-    const uint32_t team = 0xFu << (threadIdx.x & 28);
-    amax = max(amax, __shfl_xor_sync(team, amax, 1));
-    amax = max(amax, __shfl_xor_sync(team, amax, 2));
+  }
+  const uint32_t lo = __byte_perm(to_e2m1x2(x[0], x[1]), to_e2m1x2(x[2], x[3]), 0x0040), hi = __byte_perm(to_e2m1x2(x[4], x[5]), to_e2m1x2(x[6], x[7]), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
+}
+
+// Where a thread stands in a matrix whose rows are `units` pieces long, stepped by the size of the grid without a division each time
+struct RowWalk {
+  long long row, drow;
+  uint32_t unit, dunit, units;
+  __device__ __forceinline__ RowWalk(long long units_) : units((uint32_t)units_) {
+    const long long step = (long long)gridDim.x * blockDim.x, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
+    row = first / units_; unit = (uint32_t)(first % units_);
+    drow = step / units_; dunit = (uint32_t)(step % units_);
+  }
+  __device__ __forceinline__ void next() {
+    row += drow;
+    unit += dunit;
+    if (unit >= units) { unit -= units; ++row; }
+  }
+};
+
+// Rows only.  A thread takes sixteen elements, two neighbouring lanes a block; rows are padded to 128 elements, so the lanes of a
+// block never stand in two rows.
+template <int T, bool SR>
+__global__ void __launch_bounds__(256) mx_quantize_rows_kernel(const __grid_constant__ MxQuantArgs a) {
+  const long long kb = (a.cols + 127) / 128, blocks = (a.cols + 31) / 32, pitch = kb * 64;
+  for (RowWalk w(kb * 8); w.row < a.rows; w.next()) {
+    const long long c = (long long)w.unit * 16;
+    const char* src = static_cast<const char*>(a.x) + w.row * a.ld * Elem<T>::bytes;
+    Raw8<T> x[2];
+    if (a.vec && c + 16 <= a.cols) {
+      x[0].load(src, c);
+      x[1].load(src, c + 8);
+    } else {
+      x[0].load_some(src, c, (int)min(8ll, a.cols - c));
+      x[1].load_some(src, c + 8, (int)min(8ll, a.cols - c - 8));
+    }
+    uint32_t amax = max(x[0].amax(), x[1].amax());
+    amax = max(amax, __shfl_xor_sync(3u << (threadIdx.x & 30), amax, 1));
     const uint32_t code = scale_code_e2m1(amax);
-    const uint32_t w = encode_e2m1<SR>(x, scale_inverse(code), SR ? mx_random(a.seed, MX_TAG_ROWS, grp, row) : U4{0, 0, 0, 0});
-    *reinterpret_cast<uint32_t*>(a.codes + row * pitch + grp * 4) = w;
-    const long long block = grp >> 2;
-    if ((threadIdx.x & 3) == 0 && (a.tiles || block < blocks)) a.scales[mx_scale_at(row, block, blocks, kb, a.tiles)] = (uint8_t)code;
+    const float inv = scale_inverse(code);
+    uint32_t q[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = x[h].value(e);
+      q[h] = encode_e2m1<SR>(v, inv, SR ? mx_random(a.keys, MX_TAG_ROWS, 2 * w.unit + h, w.row) : U4{0, 0, 0, 0});
+    }
+    *reinterpret_cast<uint2*>(a.codes + w.row * pitch + w.unit * 8) = make_uint2(q[0], q[1]);
+    const long long block = w.unit >> 1;
+    if ((threadIdx.x & 1) == 0 && (a.tiles || block < blocks)) a.scales[mx_scale_at(w.row, block, blocks, kb, a.tiles)] = (uint8_t)code;
   }
 }
 
@@ -87,7 +106,7 @@ __global__ void __launch_bounds__(256) mx_quantize_rows_kernel(MxQuantArgs a) {
 // columns of 16-bit elements: one word a row) - whole blocks of the transpose, no exchange between lanes.  Codes of the
 // transpose leave through shared memory, 64 consecutive bytes a column, scales as whole 512-byte tiles.
 template <int T, bool SR>
-__global__ void __launch_bounds__(256) mx_quantize_tile_kernel(MxQuantArgs a) {
+__global__ void __launch_bounds__(256, 3) mx_quantize_tile_kernel(const __grid_constant__ MxQuantArgs a) {
   constexpr int EB = Elem<T>::bytes, CT = EB == 2 ? 2 : 1;     // columns a thread reads with one word
   extern __shared__ __align__(16) unsigned char tile[];        // [128][128] raw elements | codes_t [128][80] | scales [512] | scales_t [512]
   unsigned char* ct_s = tile + 128 * 128 * EB;
@@ -98,66 +117,93 @@ __global__ void __launch_bounds__(256) mx_quantize_tile_kernel(MxQuantArgs a) {
   const long long blocks = (a.cols + 31) / 32, blocks_t = (a.rows + 31) / 32;
   for (long long t = blockIdx.x; t < row_tiles * col_tiles; t += gridDim.x) {
     const long long rt = t / col_tiles, c_t = t % col_tiles, r0 = rt * 128, c0 = c_t * 128;
+    const int r_first = tid >> 4, g = tid & 15;
+    const long long c = c0 + 8 * g;
+    const bool wide = a.vec && c + 8 <= a.cols;
+    const char* src = static_cast<const char*>(a.x) + (r0 + r_first) * a.ld * EB;
 #pragma unroll
-    for (int it = 0; it < 8; ++it) {
-      const int r = it * 16 + (tid >> 4), g = tid & 15;
-      const long long row = r0 + r, c = c0 + 8 * g;
-      const char* src = static_cast<const char*>(a.x) + row * a.ld * EB;
-      float x[8];
-      if (row < a.rows && a.vec && c + 8 <= a.cols) {
-        Elem<T>::get8(src, c, x);
-      } else {
+    for (int batch = 0; batch < 2; ++batch) {
+      Raw8<T> x[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = row < a.rows && c + e < a.cols ? Elem<T>::get(src, c + e) : 0.f;
+      for (int i = 0; i < 4; ++i) {
+        const int r = (4 * batch + i) * 16 + r_first;
+        const char* from = src + (long long)(4 * batch + i) * 16 * a.ld * EB;
+        if (r0 + r < a.rows && wide) x[i].load(from, c);
+        else x[i].load_some(from, c, r0 + r < a.rows ? (int)max(0ll, min(8ll, a.cols - c)) : 0);
       }
-      Elem<T>::put8(tile, r * 128 + 8 * g, x);                  // exact: the values came from this type
-      if (a.codes) {
-        uint32_t amax = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[e]) & ABS_MASK);
-        amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-        amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-        const uint32_t code = scale_code_e2m1(amax);
-        const uint32_t w = encode_e2m1<SR>(x, scale_inverse(code), SR ? mx_random(a.seed, MX_TAG_ROWS, (c0 >> 3) + g, row) : U4{0, 0, 0, 0});
-        if (row < a.rows) *reinterpret_cast<uint32_t*>(a.codes + row * (col_tiles * 64) + c0 / 2 + g * 4) = w;
-        if ((g & 3) == 0) {
-          if (a.tiles) sc_s[(r & 31) * 16 + (r >> 5) * 4 + (g >> 2)] = (unsigned char)code;
-          else if (row < a.rows && (c0 >> 5) + (g >> 2) < blocks) a.scales[row * blocks + (c0 >> 5) + (g >> 2)] = (uint8_t)code;
+      for (int i = 0; i < 4; ++i) {
+        const int r = (4 * batch + i) * 16 + r_first;
+        uint4* to = reinterpret_cast<uint4*>(tile + (r * 128 + 8 * g) * EB);
+        to[0] = make_uint4(x[i].w[0], x[i].w[1], x[i].w[2], x[i].w[3]);
+        if constexpr (EB == 4) to[1] = make_uint4(x[i].w[4], x[i].w[5], x[i].w[6], x[i].w[7]);
+        if (a.codes) {
+          uint32_t amax = x[i].amax();
+          amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+          amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+          const uint32_t code = scale_code_e2m1(amax);
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = x[i].value(e);
+          const uint32_t w = encode_e2m1<SR>(v, scale_inverse(code), SR ? mx_random(a.keys, MX_TAG_ROWS, (c0 >> 3) + g, r0 + r) : U4{0, 0, 0, 0});
+          if (r0 + r < a.rows) *reinterpret_cast<uint32_t*>(a.codes + (r0 + r) * (col_tiles * 64) + c0 / 2 + g * 4) = w;
+          if ((g & 3) == 0) {
+            if (a.tiles) sc_s[(r & 31) * 16 + (r >> 5) * 4 + (g >> 2)] = (unsigned char)code;
+            else if (r0 + r < a.rows && (c0 >> 5) + (g >> 2) < blocks) a.scales[(r0 + r) * blocks + (c0 >> 5) + (g >> 2)] = (uint8_t)code;
+          }
         }
       }
     }
     __syncthreads();
     if (a.codes && a.tiles && tid < 128)
       reinterpret_cast<uint32_t*>(a.scales + (rt * col_tiles + c_t) * 512)[tid] = reinterpret_cast<const uint32_t*>(sc_s)[tid];
+#pragma unroll 1
     for (int task = tid; task < 4 * 128 / CT; task += 256) {
       const int cp = task % (128 / CT), rb = task / (128 / CT);
-      uint32_t raw[32];
+      const unsigned char* col_s = tile + (rb * 32 * 128 + cp * CT) * EB;
+      // largest magnitudes of the column (of both columns side by side)
+      uint32_t top = 0;
+      float topf = 0.f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(tile + ((rb * 32 + i) * 128 + cp * CT) * EB);
+      for (int i = 0; i < 32; i += 2) {
+        const uint32_t p = *reinterpret_cast<const uint32_t*>(col_s + i * 128 * EB), q = *reinterpret_cast<const uint32_t*>(col_s + (i + 1) * 128 * EB);
+        if (EB == 2) top = max_u16x2(top, max_u16x2(p & 0x7FFF7FFFu, q & 0x7FFF7FFFu));
+        else topf = max3_abs(topf, __uint_as_float(p), __uint_as_float(q));
+      }
+      uint32_t code[CT];
+      float inv[CT];
+#pragma unroll
+      for (int h = 0; h < CT; ++h) {
+        uint32_t amax;
+        if constexpr (EB == 2) amax = Raw8<T>::widen(h ? top >> 16 : top & 0xFFFFu);
+        else amax = __float_as_uint(topf) & ABS_MASK;
+        code[h] = scale_code_e2m1(amax);
+        inv[h] = scale_inverse(code[h]);
+      }
+      uint32_t w[CT][4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t raw[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(col_s + (8 * q + i) * 128 * EB);
+#pragma unroll
+        for (int h = 0; h < CT; ++h) {
+          float v[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (T == T_F32) v[i] = __uint_as_float(raw[i]);
+            else if (T == T_BF16) v[i] = __uint_as_float(h ? raw[i] & 0xFFFF0000u : raw[i] << 16);
+            else v[i] = f16_to_float(h ? raw[i] >> 16 : raw[i] & 0xFFFFu);
+          }
+          w[h][q] = encode_e2m1<SR>(v, inv[h], SR ? mx_random(a.keys, MX_TAG_COLS, (r0 >> 3) + rb * 4 + q, c0 + cp * CT + h) : U4{0, 0, 0, 0});
+        }
+      }
 #pragma unroll
       for (int h = 0; h < CT; ++h) {
         const int col = cp * CT + h;
-        auto value = [&](int i) -> float {
-          if (T == T_F32) return __uint_as_float(raw[i]);
-          if (T == T_BF16) return h ? __uint_as_float(raw[i] & 0xFFFF0000u) : __uint_as_float(raw[i] << 16);
-          return f16_to_float(h ? raw[i] >> 16 : raw[i] & 0xFFFFu);
-        };
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) amax = max(amax, __float_as_uint(value(i)) & ABS_MASK);
-        const uint32_t code = scale_code_e2m1(amax);
-        const float inv = scale_inverse(code);
-        uint32_t w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = value(8 * q + e);
-          w[q] = encode_e2m1<SR>(x, inv, SR ? mx_random(a.seed, MX_TAG_COLS, (r0 >> 3) + rb * 4 + q, c0 + col) : U4{0, 0, 0, 0});
-        }
-        *reinterpret_cast<uint4*>(ct_s + col * 80 + rb * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-        if (a.tiles) sct_s[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)code;
-        else if (c0 + col < a.cols && (r0 >> 5) + rb < blocks_t) a.scales_t[(c0 + col) * blocks_t + (r0 >> 5) + rb] = (uint8_t)code;
+        *reinterpret_cast<uint4*>(ct_s + col * 80 + rb * 16) = make_uint4(w[h][0], w[h][1], w[h][2], w[h][3]);
+        if (a.tiles) sct_s[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)code[h];
+        else if (c0 + col < a.cols && (r0 >> 5) + rb < blocks_t) a.scales_t[(c0 + col) * blocks_t + (r0 >> 5) + rb] = (uint8_t)code[h];
       }
     }
     __syncthreads();
@@ -180,37 +226,39 @@ struct MxReadArgs {
   long long rows, cols, ld;
   void* out;
   int tiles, vec;
-  int word;            // codes rows may be read as words (a single row of a pushed gradient may end in mid-word)
+  int word;            // rows of codes may be read eight bytes at a time
 };
 
+// sixteen codes -> sixteen stored elements: 16-bit types take 32 bytes, one aligned sector a lane
 template <int T>
-__global__ void __launch_bounds__(256) mx_dequantize_kernel(MxReadArgs a) {
-  const long long kb = (a.cols + 127) / 128, groups = (a.cols + 7) / 8, blocks = (a.cols + 31) / 32, pitch = kb * 64;
-  const long long step = (long long)gridDim.x * blockDim.x, first = (long long)blockIdx.x * blockDim.x + threadIdx.x;
-  const long long drow = step / groups, dgrp = step % groups;
-  long long row = first / groups, grp = first % groups;
-  for (; row < a.rows; row += drow, grp += dgrp, row += grp >= groups, grp -= grp >= groups ? groups : 0) {
-    const long long c = grp * 8;
-    const int n8 = (int)min(8ll, a.cols - c);
-    const uint8_t* src = a.codes + row * pitch + grp * 4;
-    uint32_t w = 0;
-    if (a.word && n8 == 8) {
-      w = *reinterpret_cast<const uint32_t*>(src);
+__global__ void __launch_bounds__(256) mx_dequantize_kernel(const __grid_constant__ MxReadArgs a) {
+  const long long kb = (a.cols + 127) / 128, blocks = (a.cols + 31) / 32, pitch = kb * 64;
+  for (RowWalk w((a.cols + 15) / 16); w.row < a.rows; w.next()) {
+    const long long c = (long long)w.unit * 16;
+    const int n = (int)min(16ll, a.cols - c);
+    const uint8_t* src = a.codes + w.row * pitch + w.unit * 8;
+    uint32_t q[2] = {0u, 0u};
+    if (a.word && n == 16) {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      q[0] = x.x; q[1] = x.y;
     } else {
-      for (int b = 0; 2 * b < n8; ++b) w |= (uint32_t)src[b] << (8 * b);
+      for (int b = 0; 2 * b < n; ++b) q[b >> 2] |= (uint32_t)src[b] << (8 * (b & 3));
     }
-    const float s = scale_value(a.scales[mx_scale_at(row, grp >> 2, blocks, kb, a.tiles)]);
-    float x[8];
-    e2m1x8(w, x);
+    const float s = scale_value(a.scales[mx_scale_at(w.row, w.unit >> 1, blocks, kb, a.tiles)]);
+    char* dst = static_cast<char*>(a.out) + w.row * a.ld * Elem<T>::bytes;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] *= s;
-    char* dst = static_cast<char*>(a.out) + row * a.ld * Elem<T>::bytes;
-    if (a.vec && n8 == 8) {
-      Elem<T>::put8(dst, c, x);
-    } else {
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+      e2m1x8(q[h], x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n8) Elem<T>::put(dst, c + e, x[e]);
+      for (int e = 0; e < 8; ++e) x[e] *= s;
+      if (a.vec && n == 16) {
+        Elem<T>::put8(dst, c + 8 * h, x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * h + e < n) Elem<T>::put(dst, c + 8 * h + e, x[e]);
+      }
     }
   }
 }

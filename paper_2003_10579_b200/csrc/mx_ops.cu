@@ -31,13 +31,13 @@ unsigned grid_for(long long threads) {
 template <int T, bool SR>
 cudaError_t quantize(const MxQuantArgs& a, cudaStream_t st) {
   if (!a.codes_t) {
-    mx_quantize_rows_kernel<T, SR><<<grid_for(a.rows * ((a.cols + 127) / 128) * 16), 256, 0, st>>>(a);
+    mx_quantize_rows_kernel<T, SR><<<grid_for(a.rows * ((a.cols + 127) / 128) * 8), 256, 0, st>>>(a);
     return cudaGetLastError();
   }
   constexpr int smem = mx_tile_smem<T>();
   cudaError_t e = cudaFuncSetAttribute(mx_quantize_tile_kernel<T, SR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  const long long tiles = ((a.rows + 127) / 128) * ((a.cols + 127) / 128), full = (long long)(227 * 1024 / smem) * sm_count();
+  const long long tiles = ((a.rows + 127) / 128) * ((a.cols + 127) / 128), full = 3ll * sm_count();     // three blocks fit (fp32 tiles: two or three)
   mx_quantize_tile_kernel<T, SR><<<(unsigned)(tiles < full ? tiles : full), 256, smem, st>>>(a);
   return cudaGetLastError();
 }
@@ -55,31 +55,33 @@ bool make_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t cols
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// scale tiles as a 2-D tensor of 512-byte rows; box: four tiles that follow one another along k
-bool make_scale_map(CUtensorMap* map, const uint8_t* scales, int64_t rows, int64_t kb) {
+// scale tiles as a 2-D tensor of 512-byte rows; box: `tiles` that follow one another along k
+bool make_scale_map(CUtensorMap* map, const uint8_t* scales, int64_t rows, int64_t kb, uint32_t tiles) {
   PFN_encodeTiled fn = tc_encode_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {128, (cuuint64_t)((rows + 127) / 128 * kb)};
   const cuuint64_t strides[1] = {512};
-  const cuuint32_t box[2] = {128, 4}, one[2] = {1, 1};
+  const cuuint32_t box[2] = {128, tiles}, one[2] = {1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(scales), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+struct MxgMaps { CUtensorMap a, b, sa, sb; };
+
 template <int T>
-cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const CUtensorMap& msa, const CUtensorMap& msb, const MxgArgs& g, int sms, cudaStream_t st) {
+cudaError_t launch_pair(const MxgMaps& m, const MxgArgs& g, int sms, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(mx_gemm_pair_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXP_SMEM);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)g.tiles_a * g.tiles_b, pairs = sms / 2;
-  mx_gemm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MXP_THREADS, MXP_SMEM, st>>>(ma, mb, msa, msb, g);
+  mx_gemm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MXP_THREADS, MXP_SMEM, st>>>(m.a, m.b, m.sa, m.sb, g);
   return cudaGetLastError();
 }
 
 template <int BN, int T, bool SWAP, bool SPLIT>
-cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
+cudaError_t launch(const MxgMaps& m, const MxgArgs& g, int split, cudaStream_t st) {
   auto kern = mx_gemm_kernel<BN, T, SWAP, SPLIT>;
   // partial sums of a split tile lie in the ring's bytes
-  static_assert(!SPLIT || 128 * (BN + 1) * 4 <= MxgShape<BN>::OFF_BARS, "the partial sums must fit the ring");
+  static_assert(!SPLIT || 128 * (BN + 4) * 4 <= MxgShape<BN>::OFF_BARS, "the partial sums must fit the ring");
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MxgShape<BN>::SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
@@ -94,19 +96,19 @@ cudaError_t launch(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& 
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
   }
-  return cudaLaunchKernelEx(&cfg, kern, ma, mb, g);
+  return cudaLaunchKernelEx(&cfg, kern, m.a, m.b, m.sa, m.sb, g);
 }
 template <int BN, int T, bool SWAP>
-cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
-  return split > 1 ? launch<BN, T, SWAP, true>(ma, mb, g, split, st) : launch<BN, T, SWAP, false>(ma, mb, g, split, st);
+cudaError_t launch_split(const MxgMaps& m, const MxgArgs& g, int split, cudaStream_t st) {
+  return split > 1 ? launch<BN, T, SWAP, true>(m, g, split, st) : launch<BN, T, SWAP, false>(m, g, split, st);
 }
 template <int T, bool SWAP>
-cudaError_t launch_bn(int bn, const CUtensorMap& ma, const CUtensorMap& mb, const MxgArgs& g, int split, cudaStream_t st) {
+cudaError_t launch_bn(int bn, const MxgMaps& m, const MxgArgs& g, int split, cudaStream_t st) {
   switch (bn) {
-    case 16: return launch_split<16, T, SWAP>(ma, mb, g, split, st);
-    case 32: return launch_split<32, T, SWAP>(ma, mb, g, split, st);
-    case 64: return launch_split<64, T, SWAP>(ma, mb, g, split, st);
-    case 128: return launch_split<128, T, SWAP>(ma, mb, g, split, st);
+    case 16: return launch_split<16, T, SWAP>(m, g, split, st);
+    case 32: return launch_split<32, T, SWAP>(m, g, split, st);
+    case 64: return launch_split<64, T, SWAP>(m, g, split, st);
+    case 128: return launch_split<128, T, SWAP>(m, g, split, st);
     default: return cudaErrorInvalidValue;
   }
 }
@@ -133,7 +135,7 @@ sim_status sim_mx_quantize(const void* x, sim_dtype type, int64_t rows, int64_t 
     return record_error(SIM_ERR_ARG, "sim_mx_quantize: codes and tiled scales must be 16-byte aligned");
   MxQuantArgs a{};
   a.x = x; a.rows = rows; a.cols = cols; a.ld = ld; a.codes = codes; a.scales = scales; a.codes_t = codes_t; a.scales_t = scales_t;
-  a.tiles = tiles ? 1 : 0; a.stochastic = stochastic ? 1 : 0; a.seed = seed;
+  a.tiles = tiles ? 1 : 0; a.stochastic = stochastic ? 1 : 0; a.keys = philox_keys(seed);
   a.vec = aligned(x, 16) && (rows == 1 || ld * elem_bytes(type) % 16 == 0) ? 1 : 0;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const cudaError_t e = type == SIM_F32 ? quantize_sr<T_F32>(a, st) : type == SIM_BF16 ? quantize_sr<T_BF16>(a, st) : quantize_sr<T_F16>(a, st);
@@ -149,9 +151,9 @@ sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
   MxReadArgs a{};
   a.codes = codes; a.scales = scales; a.rows = rows; a.cols = cols; a.ld = ld; a.out = out; a.tiles = tiles ? 1 : 0;
   a.vec = aligned(out, 16) && (rows == 1 || ld * elem_bytes(type) % 16 == 0) ? 1 : 0;
-  a.word = aligned(codes, 4) ? 1 : 0;
+  a.word = aligned(codes, 8) ? 1 : 0;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const unsigned grid = grid_for(rows * ((cols + 7) / 8));
+  const unsigned grid = grid_for(rows * ((cols + 15) / 16));
   if (type == SIM_F32) mx_dequantize_kernel<T_F32><<<grid, 256, 0, st>>>(a);
   else if (type == SIM_BF16) mx_dequantize_kernel<T_BF16><<<grid, 256, 0, st>>>(a);
   else mx_dequantize_kernel<T_F16><<<grid, 256, 0, st>>>(a);
@@ -175,37 +177,40 @@ sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const 
   const int kb = (int)((K + 127) / 128), sms = sm_count();
   const int64_t tiles_a = (ra + 127) / 128;
   int bn = rb <= 16 ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
+  // pairs of multiprocessors on 256 x 256 tiles once there is a tile for every second pair (256 x 4096 x 4096, 16 tiles: 15.8 us against 12.5)
   const bool pair = ra > 128 && rb > 128 && (ra + 255) / 256 * ((rb + 255) / 256) >= sms / 4;
   const int64_t tiles_b = (rb + bn - 1) / bn;
   if (tiles_a * tiles_b > (int64_t)1 << 30) return record_error(SIM_ERR_ARG, "sim_mx_matmul: the result has too many tiles");
+  // Few tiles: k is split over a cluster.  Narrow tiles add little to the end of the kernel, so down to 512 elements of k a block and up to
+  // two blocks a multiprocessor (1 x 4096 x 4096: 12.5 -> 8.4 us); 128 x 128 partial sums cost as much as 2048 elements of k
+  // (512 x 512 x 8192: 20.7 -> 12.5 us, but 1024 x 1024 x 1024: 7.4 -> 10.4 us).
   int split = 1;
-  if (!pair)     // fewer tiles than two a multiprocessor: split k over a cluster, four 128-element blocks each at least
-    while (split < 8 && tiles_a * tiles_b * split * 2 <= 2 * sms && kb >= split * 2 * 4) split *= 2;
+  const int least = bn < 128 ? 4 : 16, blocks = bn < 128 ? 2 * sms : sms;
+  while (!pair && split < 8 && tiles_a * tiles_b * split * 2 <= blocks && kb >= split * 2 * least) split *= 2;
   MxgArgs g{};
-  g.a_scales = swap ? b_scales : a_scales; g.b_scales = swap ? a_scales : b_scales;
   g.rows_a = ra; g.rows_b = rb; g.kb = kb;
   g.kb_split = ((kb + split - 1) / split + 1) / 2 * 2;
   split = (kb + g.kb_split - 1) / g.kb_split;          // every block of a cluster has a part
   g.tiles_a = (int)tiles_a; g.tiles_b = (int)tiles_b;
   g.d = c; g.ldd = ldc;
   g.vec = aligned(c, 16) && ldc * elem_bytes(type) % 16 == 0 ? 1 : 0;
-  CUtensorMap ma, mb;
+  MxgMaps m;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
   if (pair) {
-    CUtensorMap msa, msb;
     g.vec = aligned(c, 32) && ldc * elem_bytes(type) % 32 == 0 ? 1 : 0;
-    g.a_scales = a_scales; g.b_scales = b_scales; g.rows_a = M; g.rows_b = N;
+    g.rows_a = M; g.rows_b = N;
     g.tiles_a = (int)((M + 255) / 256); g.tiles_b = (int)((N + 255) / 256);
-    if (!make_map(&ma, a_codes, M, K, 128) || !make_map(&mb, b_codes, N, K, 128) || !make_scale_map(&msa, a_scales, M, kb) || !make_scale_map(&msb, b_scales, N, kb))
+    if (!make_map(&m.a, a_codes, M, K, 128) || !make_map(&m.b, b_codes, N, K, 128) || !make_scale_map(&m.sa, a_scales, M, kb, 4) || !make_scale_map(&m.sb, b_scales, N, kb, 4))
       return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
-    e = type == SIM_F32 ? launch_pair<T_F32>(ma, mb, msa, msb, g, sms, st) : launch_pair<T_BF16>(ma, mb, msa, msb, g, sms, st);
+    e = type == SIM_F32 ? launch_pair<T_F32>(m, g, sms, st) : launch_pair<T_BF16>(m, g, sms, st);
     return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_matmul", e);
   }
-  if (!make_map(&ma, swap ? b_codes : a_codes, ra, K, 128) || !make_map(&mb, swap ? a_codes : b_codes, rb, K, (uint32_t)bn))
+  if (!make_map(&m.a, swap ? b_codes : a_codes, ra, K, 128) || !make_map(&m.b, swap ? a_codes : b_codes, rb, K, (uint32_t)bn) ||
+      !make_scale_map(&m.sa, swap ? b_scales : a_scales, ra, kb, 2) || !make_scale_map(&m.sb, swap ? a_scales : b_scales, rb, kb, 2))
     return record_error(SIM_ERR_CUDA, "sim_mx_matmul: the driver refused a tensor map");
-  if (type == SIM_F32) e = swap ? launch_bn<T_F32, true>(bn, ma, mb, g, split, st) : launch_bn<T_F32, false>(bn, ma, mb, g, split, st);
-  else e = swap ? launch_bn<T_BF16, true>(bn, ma, mb, g, split, st) : launch_bn<T_BF16, false>(bn, ma, mb, g, split, st);
+  if (type == SIM_F32) e = swap ? launch_bn<T_F32, true>(bn, m, g, split, st) : launch_bn<T_F32, false>(bn, m, g, split, st);
+  else e = swap ? launch_bn<T_BF16, true>(bn, m, g, split, st) : launch_bn<T_BF16, false>(bn, m, g, split, st);
   return e == cudaSuccess ? SIM_OK : cuda_failed("sim_mx_matmul", e);
 }
 
