@@ -359,17 +359,17 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 //   warps 2-5   scales from shared to tensor memory with plain stores.  (tcgen05.cp by the issuing lane puts
 //               their latency into the codes' ring: 1190 cycles a stage instead of 784 without copies.)
 //   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers, frees the accumulators, and writes while the next
-//               tile's MMAs run: 32 bytes a lane, or through a kilobyte of shared memory where D's rows are not 32-byte aligned
+//               tile's MMAs run: 32 bytes a lane, or through shared memory where D's rows are not 32-byte aligned
 //   warp 14     scales: TMA loads (own barrier), eight stages deep
 // Persistent: the producers run ahead of the epilogue into the next tile.
 constexpr int MXP_THREADS = 480;
-constexpr int MXP_STAGES = 6;                                         // codes: 256 elements of k
+constexpr int MXP_STAGES = 5;                                         // codes: 256 elements of k (six: the same time)
 constexpr int MXP_SF_STAGES = 4, MXP_SFT_STAGES = 4;                  // scales of 512 elements of k: in shared memory, in tensor memory
 constexpr int MXP_HALF = 128 * 128;                                   // 128 rows x 128 bytes: A's rows, and this block's half of B's
 constexpr int MXP_SF_BYTES = 3 * 2048;                                // of 128 rows of A and 256 of B: four tiles of each 128 rows
 constexpr int MXP_OFF_SF = MXP_STAGES * 2 * MXP_HALF;
-constexpr int MXP_OFF_STORE = MXP_OFF_SF + MXP_SF_STAGES * MXP_SF_BYTES;    // 1 KB for each epilogue warp
-constexpr int MXP_OFF_BARS = MXP_OFF_STORE + 8 * 1024;
+constexpr int MXP_OFF_STORE = MXP_OFF_SF + MXP_SF_STAGES * MXP_SF_BYTES;    // 4 KB for each epilogue warp
+constexpr int MXP_OFF_BARS = MXP_OFF_STORE + 8 * 4096;
 constexpr int MXP_BARS = 2 * (MXP_STAGES + MXP_SF_STAGES + MXP_SFT_STAGES) + 2;
 constexpr int MXP_SMEM = MXP_OFF_BARS + 8 * MXP_BARS + 16 + 1024;
 constexpr int MXP_SCALE_COLS = 48;                                    // four tiles: 16 columns of A's scales, 32 of B's
@@ -429,6 +429,45 @@ struct MxpRing {
   __device__ __forceinline__ explicit MxpRing(uint32_t first) : phase(first) {}
   template <int N> __device__ __forceinline__ void step() { if (++s == N) { s = 0; phase ^= 1u; } }
 };
+
+// Up to sixteen rows of 256 bytes from shared memory (16-byte pieces XOR-swizzled with the row) to rows of D at any alignment of the
+// element type: a lane writes an aligned 16-byte piece of its row, put together from five words of shared memory, and at most one of the
+// elements before the first or behind the last such piece.
+template <int EB>
+__device__ __forceinline__ void mxp_write_rows(const unsigned char* st, int lane, void* d, long long ldd, long long row0, int rows, long long col0, int cols) {
+  if (rows <= 0 || cols <= 0) return;
+  const int j = lane & 15, bytes = cols * EB;
+  char* out = static_cast<char*>(d) + ((row0 + (lane >> 4)) * ldd + col0) * EB;
+  const long long pitch2 = 2 * ldd * EB;
+#pragma unroll
+  for (int it = 0; it < 8; ++it, out += pitch2) {
+    const int r = 2 * it + (lane >> 4);
+    if (r >= rows) continue;
+    const unsigned char* row = st + r * 256;
+    const int sw = r & 7;
+    const int head = min(bytes, (int)(-(intptr_t)out & 15)), pieces = (bytes - head) >> 4, tail = head + 16 * pieces;
+    if (j < pieces) {
+      const int o = head + 16 * j, first = o >> 2, shift = (o & 3) * 8;          // EB == 4: shift is 0
+      uint32_t w[5];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) {
+        const int wi = min(first + k, 63);
+        if (k < 4 || EB == 2) w[k] = *reinterpret_cast<const uint32_t*>(row + (((wi >> 2) ^ sw) << 4) + (wi & 3) * 4);
+      }
+      if (EB == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __funnelshift_r(w[k], w[k + 1], shift);
+      }
+      *reinterpret_cast<uint4*>(out + o) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    const int e = j < 8 ? j * EB : tail + (j - 8) * EB;                          // before the first piece, behind the last
+    if (j < 8 ? e < head : e < bytes) {
+      const unsigned char* at = row + (((e >> 4) ^ sw) << 4) + (e & 15);
+      if (EB == 2) *reinterpret_cast<uint16_t*>(out + e) = *reinterpret_cast<const uint16_t*>(at);
+      else *reinterpret_cast<uint32_t*>(out + e) = *reinterpret_cast<const uint32_t*>(at);
+    }
+  }
+}
 
 template <int T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MXP_THREADS, 1)
@@ -582,7 +621,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
   } else {
     const int q = warp & 3, half = (warp - 6) >> 2;
     const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16) + 128 * half, done = cluster_addr(acc_empty, 0);
-    unsigned char* st = base_p + MXP_OFF_STORE + (warp - 6) * 1024;
+    unsigned char* st = base_p + MXP_OFF_STORE + (warp - 6) * 4096;
     uint32_t phase = 0;
     for (int tile = (int)blockIdx.x >> 1; tile < n_tiles; tile += pairs, phase ^= 1u) {
       int a0, b0;
@@ -592,8 +631,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
       if (!failed && !mbar_wait_warp_long(acc_full, phase)) failed = true;                // from then on every tile of this block is NaN
       tc_fence_after();
       const int rows = (int)max(0ll, min(32ll, g.rows_a - a0));
-      constexpr int EB = Elem<T>::bytes, CC = 128 / EB;                         // columns of a 128-byte line
-      constexpr int GROUP = EB == 2 ? 128 : 64;                                 // columns taken into registers at a time
+      constexpr int EB = Elem<T>::bytes, GROUP = 256 / EB;                      // columns taken into registers at a time: 256 bytes of a row
 #pragma unroll
       for (int c0 = 0; c0 < 128; c0 += GROUP) {
         uint32_t w[64];
@@ -630,16 +668,18 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                            "r"(w[8 * p + 3]), "r"(w[8 * p + 4]), "r"(w[8 * p + 5]), "r"(w[8 * p + 6]), "r"(w[8 * p + 7]) : "memory");
           }
         } else {
-#pragma unroll
-          for (int c = 0; c < GROUP; c += CC) {
-            // eight rows at a time through the warp's kilobyte
+          // sixteen rows at a time through the warp's 4 KB
 #pragma unroll 1
-            for (int r8 = 0; r8 < 4; ++r8) {
-              __syncwarp();
-              if ((lane >> 3) == r8) mxg_stage(st, lane & 7, w + c * EB / 4);
-              __syncwarp();
-              mxg_write_rows<T>(st, lane, g.d, g.ldd, a0 + 8 * r8, min(8, rows - 8 * r8), b0 + c0 + c, (int)max(0ll, min((long long)CC, cols - c)), 0);
+          for (int h = 0; h < 2; ++h) {
+            __syncwarp();
+            if ((lane >> 4) == h) {
+              const int r = lane & 15;
+#pragma unroll
+              for (int p = 0; p < 16; ++p)
+                *reinterpret_cast<uint4*>(st + r * 256 + ((p ^ (r & 7)) << 4)) = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
             }
+            __syncwarp();
+            mxp_write_rows<EB>(st, lane, g.d, g.ldd, a0 + 16 * h, min(16, rows - 16 * h), b0 + c0, (int)max(0ll, min((long long)GROUP, cols)));
           }
         }
       }

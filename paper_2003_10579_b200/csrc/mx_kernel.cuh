@@ -246,19 +246,32 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const __grid_constan
     }
     const float s = scale_value(a.scales[mx_scale_at(w.row, w.unit >> 1, blocks, kb, a.tiles)]);
     char* dst = static_cast<char*>(a.out) + w.row * a.ld * Elem<T>::bytes;
+    float x[2][8];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      float x[8];
-      e2m1x8(q[h], x);
+      e2m1x8(q[h], x[h]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= s;
-      if (a.vec && n == 16) {
-        Elem<T>::put8(dst, c + 8 * h, x);
+      for (int e = 0; e < 8; ++e) x[h][e] *= s;
+    }
+    if (a.vec && n == 16) {                     // 32-byte aligned rows: whole sectors
+      if constexpr (T == T_F32) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(x[h][e]);
+          store32(dst + (c + 8 * h) * 4, o);
+        }
       } else {
+        uint32_t o[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (8 * h + e < n) Elem<T>::put(dst, c + 8 * h + e, x[e]);
+        for (int k = 0; k < 8; ++k) o[k] = T == T_BF16 ? float_to_bf16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]) : float_to_f16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]);
+        store32(dst + c * 2, o);
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (e < n) Elem<T>::put(dst, c + e, x[e >> 3][e & 7]);
     }
   }
 }

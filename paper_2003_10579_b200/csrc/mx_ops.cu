@@ -150,7 +150,7 @@ sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
   if (!codes || !scales || !out || !aligned(out, elem_bytes(type))) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: codes, scales and out (aligned to its type) are required");
   MxReadArgs a{};
   a.codes = codes; a.scales = scales; a.rows = rows; a.cols = cols; a.ld = ld; a.out = out; a.tiles = tiles ? 1 : 0;
-  a.vec = aligned(out, 16) && (rows == 1 || ld * elem_bytes(type) % 16 == 0) ? 1 : 0;
+  a.vec = aligned(out, 32) && (rows == 1 || ld * elem_bytes(type) % 32 == 0) ? 1 : 0;
   a.word = aligned(codes, 8) ? 1 : 0;
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const unsigned grid = grid_for(rows * ((cols + 15) / 16));
