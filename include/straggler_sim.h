@@ -120,6 +120,15 @@ sim_status sim_set_adasync(sim_handle* h, int32_t K0, double t_interval);
  */
 sim_status sim_set_adasync_loss(sim_handle* h, int32_t K0, double t_interval);
 
+/*
+ * AdamW instead of Eq. 2 / Eq. 3 as the server's update (same formulas as sim_adamw_step below, fp32 moments): the mean of the K
+ * gradients - possibly taken at stale parameters - updates the moments, and w_{j+1} = w_j (1 - eta weight_decay) - eta
+ * (m / (1 - beta1^(j+1))) / (sqrt(v / (1 - beta2^(j+1))) + eps).  Everything else (arrivals, clock, minibatches, trace) is
+ * unchanged.  LSQ and LOGISTIC; only before sim_reserve / sim_run.  SIM_ERR_ARG for other models, betas outside [0, 1), eps not finite
+ * or below 2^-126, weight_decay < 0, a handle with eta < 0.
+ */
+sim_status sim_set_adamw(sim_handle* h, double beta1, double beta2, double eps, float weight_decay);
+
 /* Optional performance knobs of the linear-model kernels (0 = chosen from d): depth of the
  * shared-memory ring that stages sample rows ahead of the arithmetic (2..8), rows per tile (2 or
  * 4) and threads per replica (256 or 512) where the kernel for that d offers the choice.
@@ -167,6 +176,14 @@ sim_status sim_get_params(const sim_handle* h, float* w);
  * fixed order.  SIM_ERR_ARG for SIM_NONE.  Enqueued on the handle's stream; does not wait.
  */
 sim_status sim_eval_loss(sim_handle* h, float* loss);
+
+/*
+ * The same risk with the data set and the parameters rounded to MXFP4 along the features (blocks of 32, nearest even; see
+ * sim_mx_quantize) and the logits from the 4-bit product sim_mx_matmul: what a replica's parameters lose when they are served in 4
+ * bits.  Parameters themselves stay as they are.  LSQ, LOGISTIC and SOFTMAX (SIM_ERR_ARG otherwise).  The first call of a handle allocates
+ * the 4-bit form of the data set (17/32 of a byte an element), which it keeps, and room for logits.  Enqueued; does not wait.
+ */
+sim_status sim_eval_loss_mxfp4(sim_handle* h, float* loss);
 
 /*
  * Error against wall clock, the two metrics of Section 2.3 recorded together inside sim_run: with every > 0 the

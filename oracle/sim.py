@@ -61,7 +61,7 @@ def adasync_next_K(variant, K0, P, K_prev, F0, F):
 
 class OracleReplica:
     def __init__(self, *, model, X, y, w0, P, K, variant, delay_kind, mu, shift=0.0, eta, m, seed,
-                 replica, n_classes=1, hidden=0, w_ref=None, K0=0, t_interval=0.0, bf16=True, k_rule="doubling"):
+                 replica, n_classes=1, hidden=0, w_ref=None, K0=0, t_interval=0.0, bf16=True, k_rule="doubling", adamw=None):
         assert variant in core.VARIANTS and 1 <= P and 1 <= m
         self.model, self.X, self.y = model, X, y
         self.n = 0 if X is None else X.shape[0]
@@ -75,6 +75,8 @@ class OracleReplica:
         self.k_events = []               # (update index, F(w_start), new K) at every recomputation
         self.w_ref = None if w_ref is None else np.asarray(w_ref, np.float64)
         self.w = None if w0 is None else np.array(w0, dtype=np.float32)   # w_j
+        self.adamw = adamw               # (beta1, beta2, eps, weight decay) of an AdamW server, its moments in fp64
+        self.moments = None if adamw is None else [np.zeros(self.w.shape[0]), np.zeros(self.w.shape[0])]
         self.j = 0
         self.t = 0.0
         self.s = [0] * P                 # tasks launched so far by worker i
@@ -134,7 +136,15 @@ class OracleReplica:
                 f_sum, g = self._gradient(w_at, i, seq)
                 total += g
                 loss += f_sum
-            self.w = (self.w.astype(np.float64) - (self.eta / K) * total).astype(np.float32)
+            if self.adamw is None:
+                self.w = (self.w.astype(np.float64) - (self.eta / K) * total).astype(np.float32)
+            else:
+                b1, b2, eps, decay = self.adamw
+                mean, t, w = total / K, self.j + 1, self.w.astype(np.float64)
+                self.moments[0] = m = b1 * self.moments[0] + (1.0 - b1) * mean
+                self.moments[1] = v = b2 * self.moments[1] + (1.0 - b2) * mean * mean
+                step = (m / (1.0 - b1 ** t)) / (np.sqrt(v / (1.0 - b2 ** t)) + eps)
+                self.w = (w * (1.0 - self.eta * decay) - self.eta * step).astype(np.float32)
             tr["loss"].append(np.float32(loss / (K * self.m)))
             tr["gnorm"].append(float(np.linalg.norm(total)) / K)     # |averaged gradient| of this update
             if self.w_ref is not None:

@@ -24,7 +24,7 @@ EXPORTS = ["sim_create", "sim_set_params", "sim_set_adasync", "sim_set_adasync_l
            "sim_get_risk_trace", "sim_risk_curve", "sim_risk_envelope", "sim_selftest_wait_timeout", "sim_n_params", "sim_last_error",
            "sim_destroy", "sim_draw_delays", "sim_draw_indices", "sim_simulate_host", "sim_sweep_host", "sim_schedule_noalloc",
            "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy",
-           "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul"]
+           "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul", "sim_set_adamw", "sim_eval_loss_mxfp4"]
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # SIM_F32, SIM_BF16, SIM_F16
 MXFP4 = 3
 
@@ -96,6 +96,8 @@ def _load():
     L.sim_adamw_step_device.argtypes = [vp, vp, vp, C.c_float, i32, vp]
     L.sim_adamw_destroy.argtypes = [vp]
     L.sim_adamw_destroy.restype = None
+    L.sim_set_adamw.argtypes = [vp, dbl, dbl, dbl, C.c_float]
+    L.sim_eval_loss_mxfp4.argtypes = [vp, vp]
     L.sim_mx_codes_bytes.argtypes = [i64, i64]
     L.sim_mx_scales_bytes.argtypes = [i64, i64, i32]
     L.sim_mx_quantize.argtypes = [vp, C.c_int, i64, i64, i64, i32, i32, u64, vp, vp, vp, vp, vp]
@@ -174,6 +176,10 @@ class Simulation:
         """Algorithm 1 as printed: K follows the full-data risk at interval boundaries."""
         _check(lib.sim_set_adasync_loss(self._h, K0, t_interval), self._h)
 
+    def set_adamw(self, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0):
+        """AdamW with step size eta instead of the plain step as the server's update (least squares and logistic)."""
+        _check(lib.sim_set_adamw(self._h, betas[0], betas[1], eps, weight_decay), self._h)
+
     def set_tuning(self, stages=0, tile_rows=0, threads=0):
         _check(lib.sim_set_tuning(self._h, stages, tile_rows, threads), self._h)
 
@@ -211,10 +217,10 @@ class Simulation:
         _check(lib.sim_get_params(self._h, _ptr(w)), self._h)
         return w.cpu().numpy() if to_numpy else w
 
-    def eval_loss(self, to_numpy=True):
-        """Full-data risk F(w_j) of every replica's current parameters."""
+    def eval_loss(self, to_numpy=True, mxfp4=False):
+        """Full-data risk F(w_j) of every replica's current parameters; mxfp4: with data and parameters in 4 bits."""
         out = torch.empty((self.R,), dtype=torch.float32, device=self.device)
-        _check(lib.sim_eval_loss(self._h, _ptr(out)), self._h)
+        _check((lib.sim_eval_loss_mxfp4 if mxfp4 else lib.sim_eval_loss)(self._h, _ptr(out)), self._h)
         if self.stream is not None:
             self.stream.synchronize()
         else:

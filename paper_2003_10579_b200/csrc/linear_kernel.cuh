@@ -9,10 +9,12 @@
 //         a_q = dl/dz(z_q, y_q)    (x.w - y, or sigmoid(x.w) - b)
 //         g  += sum_q a_q x_q      (column owner accumulates, no reduction needed)
 // and at the end of the update  w_{j+1} = w_j - (eta / (K m)) g   (Eq. 2 / Eq. 3), the minibatch
-// loss and |w_{j+1} - w_ref|^2 are recorded.  w_j, w_tau and g live in registers; for the
+// loss and |w_{j+1} - w_ref|^2 are recorded.  With ADAM the same averaged gradient goes through AdamW instead, whose moments
+// are read and written once per update.  w_j, w_tau and g live in registers; for the
 // asynchronous variants every version is also written to the replica's version pool, from
 // which stale snapshots w_tau are read back.
 #pragma once
+#include "adamw_math.cuh"
 #include "ptx_util.cuh"
 #include "schedule_kernel.cuh"
 
@@ -50,6 +52,12 @@ struct NumericArgs {
   float* pool;               // asynchronous variants: [R][n_slots][n_params]
   int stages;                // shared-memory ring depth
   int* err;
+  // AdamW as the server's update: moments [R][n_params], coefficients for a mean of one gradient, and for each update j
+  // (eta / (1 - beta1^(j+1)), 1 / sqrt(1 - beta2^(j+1)))
+  float* adam_m; float* adam_v;
+  const float2* adam_bias;
+  AdamwCoef adam;
+  float adam_keep;           // 1 - eta * weight_decay
 };
 
 // Where the MLP keeps element (k, n) of W1 inside a version of the pool.  The update kernel moves W1
@@ -118,7 +126,7 @@ struct ScheduleWalk {
   }
 };
 
-template <int NT, int CHUNKS, int T, bool ASYNC>
+template <int NT, int CHUNKS, int T, bool ASYNC, bool ADAM>
 __global__ void __launch_bounds__(NT) linear1_kernel(NumericArgs a) {
   constexpr int NW = NT / 32;
   constexpr int E = 4 * CHUNKS;
@@ -355,13 +363,36 @@ __global__ void __launch_bounds__(NT) linear1_kernel(NumericArgs a) {
     if (ti.flags & TILE_LAST_OF_UPDATE) {
       // w_{j+1} = w_j - (eta / (K m)) sum of the K m per-sample gradients
       const float scale = (float)((double)a.eta / ((double)ti.K * (double)m));
+      AdamwCoef ac = a.adam;
+      if (ADAM) {
+        const float mean = (float)(1.0 / ((double)ti.K * (double)m));
+        const float2 bias = a.adam_bias[j];
+        ac.c1 *= mean; ac.s2 *= mean; ac.lr_bc1 = bias.x; ac.rbc2 = bias.y;
+      }
       float dd = 0.f;
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
         const int ci = tid + NT * c;
         if (ci < d4) {
+          if constexpr (ADAM) {
+            float4* mp = reinterpret_cast<float4*>(a.adam_m + (size_t)r * d) + ci;
+            float4* vp = reinterpret_cast<float4*>(a.adam_v + (size_t)r * d) + ci;
+            const float4 m4 = *mp, v4 = *vp;
+            float mo[4] = {m4.x, m4.y, m4.z, m4.w}, vo[4] = {v4.x, v4.y, v4.z, v4.w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { w_cur[4 * c + e] = fmaf(-scale, g[4 * c + e], w_cur[4 * c + e]); g[4 * c + e] = 0.f; }
+            for (int e = 0; e < 4; ++e) {
+              const float s2 = ac.s2 * g[4 * c + e];
+              mo[e] = fmaf(ac.b1, mo[e], ac.c1 * g[4 * c + e]);
+              vo[e] = fmaf(ac.b2, vo[e], s2 * s2);
+              w_cur[4 * c + e] = adamw_param(ac, a.adam_keep, w_cur[4 * c + e], mo[e], sqrt_fast(vo[e]));
+              g[4 * c + e] = 0.f;
+            }
+            *mp = make_float4(mo[0], mo[1], mo[2], mo[3]);
+            *vp = make_float4(vo[0], vo[1], vo[2], vo[3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { w_cur[4 * c + e] = fmaf(-scale, g[4 * c + e], w_cur[4 * c + e]); g[4 * c + e] = 0.f; }
+          }
           if (ASYNC) {
             float4* dst = reinterpret_cast<float4*>(a.pool + ((size_t)r * a.n_slots + ti.fresh) * (size_t)d);
             dst[ci] = make_float4(w_cur[4 * c], w_cur[4 * c + 1], w_cur[4 * c + 2], w_cur[4 * c + 3]);

@@ -2,6 +2,7 @@
 // See include/straggler_sim.h for the contract of every entry point.
 #include "../../include/straggler_sim.h"
 
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -15,6 +16,7 @@
 #include "softmax_ws_kernel.cuh"
 #include "mlp_tc_kernel.cuh"
 #include "eval_kernel.cuh"
+#include "mx_eval_kernel.cuh"
 
 using namespace ssim;
 
@@ -85,6 +87,15 @@ struct sim_handle {
   long long eval_every = 0, n_evals = 0, risk_cap = 0;
   float* risk = nullptr;            // [risk_cap][R]
   float* mlp_eval_part = nullptr;   // MLP: per 32-row group partial loss sums of one evaluation
+  // AdamW as the server's update: moments [R][n_params], bias corrections of every update there is trace for
+  bool adam = false;
+  double adam_b1 = 0.0, adam_b2 = 0.0;
+  float adam_eps = 0.f, adam_decay = 0.f;
+  float* adam_m = nullptr; float* adam_v = nullptr; float2* adam_bias = nullptr;
+  // risk with data and parameters in MXFP4: the data's codes and scales (made on the first call), the parameters', logits, sums
+  uint8_t* mx_x = nullptr; uint8_t* mx_xs = nullptr; uint8_t* mx_w = nullptr; uint8_t* mx_ws = nullptr;
+  float* mx_params = nullptr; float* mx_z = nullptr; double* mx_partial = nullptr;
+  long long mx_chunk = 0;
   TraceBuffers tr;
   bool poisoned = false;
   bool in_arena = false;      // buffers come from the creating thread's DeviceArena and are not freed one by one
@@ -192,6 +203,13 @@ __global__ void gather_params_kernel(const float* pool, const uint8_t* cur_slot,
   }
 }
 
+__global__ void adam_bias_kernel(double beta1, double beta2, float eta, float2* bias, long long n) {
+  for (long long j = blockIdx.x * (long long)blockDim.x + threadIdx.x; j < n; j += (long long)gridDim.x * blockDim.x) {
+    const AdamwCoef c = adamw_coef(beta1, beta2, 0.f, 1.0, eta, j + 1);
+    bias[j] = make_float2(c.lr_bc1, c.rbc2);
+  }
+}
+
 template <typename T>
 sim_status regrow(sim_handle* h, T** buf, size_t per_update, long long new_cap, bool zero) {
   T* nb = nullptr;
@@ -223,6 +241,14 @@ sim_status ensure_capacity(sim_handle* h, long long need) {
     if ((st = regrow(h, &h->tr.snap_slot, Ks, nc, false)) != SIM_OK) return st;
     if ((st = regrow(h, &h->tr.new_slot, 1, nc, false)) != SIM_OK) return st;
   }
+  if (h->adam) {
+    float2* nb = nullptr;
+    CUDA_TRY(h, dev_alloc(&nb, (size_t)nc, h->stream, false));
+    adam_bias_kernel<<<296, 256, 0, h->stream>>>(h->adam_b1, h->adam_b2, h->eta, nb, nc);
+    CUDA_TRY(h, cudaGetLastError());
+    if (h->adam_bias && !h->in_arena) { CUDA_TRY(h, cudaStreamSynchronize(h->stream)); cudaFree(h->adam_bias); }
+    h->adam_bias = nb;
+  }
   h->cap = nc;
   return SIM_OK;
 }
@@ -252,7 +278,8 @@ sim_status launch_linear1(sim_handle* h, NumericArgs& a) {
   if (smem > (size_t)(226 << 10))
     return fail(h, SIM_ERR_ARG, "the row staging buffers (d) and the minibatch index table (m) do not fit in shared memory with this tuning");
   a.stages = S;
-  auto kern = a.is_async ? linear1_kernel<NT, CHUNKS, T, true> : linear1_kernel<NT, CHUNKS, T, false>;
+  auto kern = h->adam ? (a.is_async ? linear1_kernel<NT, CHUNKS, T, true, true> : linear1_kernel<NT, CHUNKS, T, false, true>)
+                      : (a.is_async ? linear1_kernel<NT, CHUNKS, T, true, false> : linear1_kernel<NT, CHUNKS, T, false, false>);
   CUDA_TRY(h, cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
   kern<<<a.R, NT, smem, h->stream>>>(a);
   CUDA_TRY(h, cudaGetLastError());
@@ -327,6 +354,8 @@ void free_all(sim_handle* h) {
   cudaFree(h->tr.t); cudaFree(h->tr.loss); cudaFree(h->tr.dist2); cudaFree(h->tr.K_used);
   cudaFree(h->tr.worker); cudaFree(h->tr.stale); cudaFree(h->tr.seq); cudaFree(h->tr.snap_slot);
   cudaFree(h->tr.new_slot); cudaFree(h->risk); cudaFree(h->mlp_eval_part);
+  cudaFree(h->adam_m); cudaFree(h->adam_v); cudaFree(h->adam_bias); cudaFree(h->mx_x); cudaFree(h->mx_xs); cudaFree(h->mx_w); cudaFree(h->mx_ws);
+  cudaFree(h->mx_params); cudaFree(h->mx_z); cudaFree(h->mx_partial);
 }
 
 // MLP: bf16 copy of the data, per-update scratch and the bf16 shadow of the initial W1, made on first use
@@ -486,6 +515,11 @@ static sim_status run_span(sim_handle* h, int64_t iters) {
     a.K_used = h->tr.K_used; a.worker = h->tr.worker; a.seq = h->tr.seq; a.snap_slot = h->tr.snap_slot;
     a.new_slot = h->tr.new_slot; a.begin_slot = h->begin_slot; a.loss = h->tr.loss; a.dist2 = h->tr.dist2;
     a.w_state = h->w_state; a.pool = h->pool; a.err = h->err;
+    if (h->adam) {
+      a.adam_m = h->adam_m; a.adam_v = h->adam_v; a.adam_bias = h->adam_bias;
+      a.adam = adamw_coef(h->adam_b1, h->adam_b2, h->adam_eps, 1.0, h->eta, 1);
+      a.adam_keep = (float)(1.0 - (double)h->eta * (double)h->adam_decay);
+    }
     const char* why = nullptr;
     cudaError_t ce = cudaSuccess;
     switch (h->prob.model) {
@@ -751,6 +785,81 @@ sim_status sim_eval_loss(sim_handle* h, float* loss) {
   if (!loss) return fail(h, SIM_ERR_ARG, "loss is NULL");
   if (h->poisoned) return fail(h, SIM_ERR_STATE, "the handle failed earlier");
   return eval_into(h, loss);
+}
+
+// Risk with data and parameters in MXFP4: logits of all replicas over a stretch of rows are one product of the parameters (a replica's
+// classes are its rows) and the data, both quantised along the features.
+static sim_status eval_mxfp4(sim_handle* h, float* loss) {
+  const sim_model mdl = h->prob.model;
+  const long long n = h->prob.n, d = h->prob.d, C = mdl == SIM_SOFTMAX ? h->prob.n_classes : 1, rows_w = (long long)h->R * C;
+  const long long seg_total = (n + MXE_SEG - 1) / MXE_SEG;
+  if (seg_total > (1ll << 30) / (h->R > 0 ? h->R : 1)) return fail(h, SIM_ERR_ARG, "too many replicas for this data set");
+  auto mx_failed = [&](sim_status st) { return fail(h, st, sim_last_error(nullptr)); };
+  sim_status st;
+  if (!h->mx_x) {                       // the data set does not change while the handle lives: its 4-bit form is made once
+    uint8_t *xc = nullptr, *xs = nullptr;
+    long long chunk = ((256ll << 20) / 4 / rows_w) / MXE_SEG * MXE_SEG;      // rows of logits in 256 MB, whole segments
+    chunk = chunk < MXE_SEG ? MXE_SEG : chunk > 65536 ? 65536 : chunk;
+    CUDA_TRY(h, dev_alloc(&h->mx_w, (size_t)sim_mx_codes_bytes(rows_w, d), h->stream, false));
+    CUDA_TRY(h, dev_alloc(&h->mx_ws, (size_t)sim_mx_scales_bytes(rows_w, d, 1), h->stream, false));
+    if (h->uses_pool) CUDA_TRY(h, dev_alloc(&h->mx_params, (size_t)h->R * h->n_params, h->stream, false));
+    CUDA_TRY(h, dev_alloc(&h->mx_z, (size_t)rows_w * chunk, h->stream, false));
+    CUDA_TRY(h, dev_alloc(&h->mx_partial, (size_t)h->R * seg_total, h->stream, false));
+    CUDA_TRY(h, dev_alloc(&h->mx_xs, (size_t)sim_mx_scales_bytes(n, d, 1), h->stream, false));
+    CUDA_TRY(h, dev_alloc(&xc, (size_t)sim_mx_codes_bytes(n, d), h->stream, false));
+    xs = h->mx_xs;
+    if ((st = sim_mx_quantize(h->prob.X, SIM_F32, n, d, d, 1, 0, 0, xc, xs, nullptr, nullptr, h->stream)) != SIM_OK) { if (!h->in_arena) cudaFree(xc); return mx_failed(st); }
+    h->mx_x = xc;
+    h->mx_chunk = chunk;
+  }
+  const float* w = h->w_state;
+  if (h->uses_pool) {
+    gather_params_kernel<<<1184, 256, 0, h->stream>>>(h->pool, h->cur_slot, h->mx_params, h->n_params, h->slot_stride, h->n_slots, h->R, 0, 1);
+    CUDA_TRY(h, cudaGetLastError());
+    w = h->mx_params;
+  }
+  if ((st = sim_mx_quantize(w, SIM_F32, rows_w, d, d, 1, 0, 0, h->mx_w, h->mx_ws, nullptr, nullptr, h->stream)) != SIM_OK) return mx_failed(st);
+  const long long pitch = sim_mx_codes_bytes(1, d), tile_row = sim_mx_scales_bytes(128, d, 1);
+  const void* y = mdl == SIM_LSQ ? static_cast<const void*>(h->prob.y) : static_cast<const void*>(h->prob.label);
+  for (long long row0 = 0; row0 < n; row0 += h->mx_chunk) {
+    const long long rows = n - row0 < h->mx_chunk ? n - row0 : h->mx_chunk;
+    st = sim_mx_matmul(h->mx_w, h->mx_ws, h->mx_x + row0 * pitch, h->mx_xs + row0 / 128 * tile_row, rows_w, rows, d, SIM_F32, h->mx_z, h->mx_chunk, h->stream);
+    if (st != SIM_OK) return mx_failed(st);
+    const unsigned segs = (unsigned)((rows + MXE_SEG - 1) / MXE_SEG);
+    for (int r0 = 0; r0 < h->R; r0 += 65535) {        // the grid's second dimension
+      const int part = h->R - r0 < 65535 ? h->R - r0 : 65535;
+      mx_loss_kernel<<<dim3(segs, (unsigned)part), 256, 0, h->stream>>>(h->mx_z + (long long)r0 * C * h->mx_chunk, h->mx_chunk, y, (int)mdl, (int)C, row0, (int)rows,
+                                                                        h->mx_partial + (long long)r0 * seg_total, (int)seg_total, (int)(row0 / MXE_SEG));
+      CUDA_TRY(h, cudaGetLastError());
+    }
+  }
+  mx_loss_finish_kernel<<<(h->R + 127) / 128, 128, 0, h->stream>>>(h->mx_partial, (int)seg_total, n, h->R, loss);
+  CUDA_TRY(h, cudaGetLastError());
+  return SIM_OK;
+}
+
+sim_status sim_eval_loss_mxfp4(sim_handle* h, float* loss) {
+  if (!h) return fail(nullptr, SIM_ERR_ARG, "handle is NULL");
+  if (!loss) return fail(h, SIM_ERR_ARG, "loss is NULL");
+  if (h->poisoned) return fail(h, SIM_ERR_STATE, "the handle failed earlier");
+  const sim_model mdl = h->prob.model;
+  if (mdl != SIM_LSQ && mdl != SIM_LOGISTIC && mdl != SIM_SOFTMAX) return fail(h, SIM_ERR_ARG, "the risk in MXFP4 needs a linear model (LSQ, logistic or softmax)");
+  return eval_mxfp4(h, loss);
+}
+
+sim_status sim_set_adamw(sim_handle* h, double beta1, double beta2, double eps, float weight_decay) {
+  if (!h) return fail(nullptr, SIM_ERR_ARG, "handle is NULL");
+  if (h->n_updates > 0 || h->cap > 0) return fail(h, SIM_ERR_STATE, "sim_set_adamw is only allowed before sim_reserve / sim_run");
+  if (h->prob.model != SIM_LSQ && h->prob.model != SIM_LOGISTIC) return fail(h, SIM_ERR_ARG, "AdamW as the server's update needs a least-squares or logistic model");
+  if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(h, SIM_ERR_ARG, "betas must be in [0, 1)");
+  if (!((float)eps >= FLT_MIN) || std::isinf((float)eps)) return fail(h, SIM_ERR_ARG, "eps must be finite and at least 2^-126");
+  if (!(weight_decay >= 0.f) || std::isinf(weight_decay)) return fail(h, SIM_ERR_ARG, "weight_decay must be finite and >= 0");
+  if (!(h->eta >= 0.f)) return fail(h, SIM_ERR_ARG, "AdamW needs a step size eta >= 0");
+  const size_t np = (size_t)h->R * h->n_params;
+  if (!h->adam_m) CUDA_TRY(h, dev_alloc(&h->adam_m, np, h->stream));
+  if (!h->adam_v) CUDA_TRY(h, dev_alloc(&h->adam_v, np, h->stream));
+  h->adam = true; h->adam_b1 = beta1; h->adam_b2 = beta2; h->adam_eps = (float)eps; h->adam_decay = weight_decay;
+  return SIM_OK;
 }
 
 sim_status sim_set_adasync_loss(sim_handle* h, int32_t K0, double t_interval) {
