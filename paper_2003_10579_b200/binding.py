@@ -410,20 +410,66 @@ class MxTensor:
     """A matrix [rows, cols] in MXFP4: E2M1 codes (two a byte, even element in the low half, rows padded to 128 elements) and
     a power-of-two scale byte per block of 32 elements of a row.  layout "linear": scale bytes [rows, ceil(cols / 32)]; a
     single row is also the form of a pushed gradient.  layout "tiles": the order the products read, 512 bytes per 128 rows x
-    4 blocks (row r of a tile at byte 16 (r % 32) + 4 (r / 32))."""
+    4 blocks (row r of a tile at byte 16 (r % 32) + 4 (r / 32)).  codes and scales are flat uint8 tensors."""
 
-    __slots__ = ("codes", "scales", "rows", "cols", "layout")
+    __slots__ = ("rows", "cols", "layout", "device", "codes_ptr", "scales_ptr", "_codes", "_scales", "_buffer")
 
     def __init__(self, codes, scales, rows, cols, layout):
         if layout not in ("linear", "tiles"):
             raise ValueError("layout must be 'linear' or 'tiles'")
-        blocks, pitch = -(-cols // 32), 64 * -(-cols // 128)
-        need_c = -(-cols // 2) if rows == 1 and layout == "linear" else rows * pitch
-        need_s = rows * blocks if layout == "linear" else 512 * -(-rows // 128) * -(-cols // 128)
+        need_c, need_s = _mx_bytes(rows, cols, layout)
+        if rows == 1 and layout == "linear":
+            need_c = -(-cols // 2)
         for name, t, need in (("codes", codes, need_c), ("scales", scales, need_s)):
-            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < need:
-                raise ValueError("%s must be a contiguous CUDA uint8 tensor of at least %d bytes" % (name, need))
-        self.codes, self.scales, self.rows, self.cols, self.layout = codes, scales, rows, cols, layout
+            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < need or t.device != codes.device:
+                raise ValueError("%s must be a contiguous CUDA uint8 tensor of at least %d bytes, on one device" % (name, need))
+        self._codes, self._scales, self._buffer = codes, scales, None
+        self.rows, self.cols, self.layout, self.device = rows, cols, layout, codes.device
+        self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def empty(cls, rows, cols, layout, device):
+        """Uninitialised, codes and scales in one buffer."""
+        self = cls.__new__(cls)
+        nc, ns = _mx_bytes(rows, cols, layout)
+        self._buffer = buf = torch.empty(nc + ns, dtype=torch.uint8, device=device)
+        self._codes = self._scales = None
+        self.rows, self.cols, self.layout, self.device = rows, cols, layout, buf.device
+        self.codes_ptr = buf.data_ptr()
+        self.scales_ptr = self.codes_ptr + nc
+        return self
+
+    @property
+    def codes(self):
+        if self._codes is None:
+            self._codes = self._buffer[:self.scales_ptr - self.codes_ptr]
+        return self._codes
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._scales = self._buffer[self.scales_ptr - self.codes_ptr:]
+        return self._scales
+
+
+def _mx_bytes(rows, cols, layout):
+    """Bytes of codes (a multiple of 64) and of scales, as sim_mx_codes_bytes and sim_mx_scales_bytes give them."""
+    kb = (cols + 127) // 128
+    return rows * 64 * kb, (rows + 127) // 128 * kb * 512 if layout == "tiles" else rows * ((cols + 31) // 32)
+
+
+# the raw stream of a device without a Stream object around it, where torch offers that (2 us a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _on(device, stream, call, *args):
+    """call(*args, stream) with `device` current; stream None: the device's current one."""
+    index = device.index
+    st = _raw_stream(index) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        return call(*args, st)
+    with torch.cuda.device(index):
+        return call(*args, st)
 
 
 def _ptr_array(pointers):
@@ -472,10 +518,10 @@ class AdamW:
             mine = [g[i] for g in grads]
             if isinstance(mine[0], MxTensor):
                 for q in mine:
-                    if not isinstance(q, MxTensor) or q.rows != 1 or q.cols != n or q.layout != "linear" or q.codes.device != self.device or q.scales.device != self.device:
+                    if not isinstance(q, MxTensor) or q.rows != 1 or q.cols != n or q.layout != "linear" or q.device != self.device:
                         raise ValueError("the gradients of parameter %d must all be MxTensor of one row of %d elements, linear layout, on %s" % (i, n, self.device))
                 r.g_type = MXFP4
-                arrays = _ptr_array([q.codes.data_ptr() for q in mine]), _ptr_array([q.scales.data_ptr() for q in mine])
+                arrays = _ptr_array([q.codes_ptr for q in mine]), _ptr_array([q.scales_ptr for q in mine])
                 r.g_scale = C.cast(arrays[1], C.POINTER(C.c_void_p))
             else:
                 if any(isinstance(g, MxTensor) or g.dtype != mine[0].dtype for g in mine):
@@ -499,15 +545,15 @@ class AdamW:
         """Step number `step` (1, 2, ...) with learning rate lr and the average of the first K pushes (default: all), on
         `stream` (default: the device's current one).  step and lr may both be CUDA tensors of one element (int64, float32):
         they are read when the step runs, for steps captured in a graph."""
-        st = torch.cuda.current_stream(self.device) if stream is None else stream
+        st = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
         K = self.n_grads if K is None else K
         if torch.is_tensor(step) or torch.is_tensor(lr):
             for t, dt in ((step, torch.int64), (lr, torch.float32)):
                 if not torch.is_tensor(t) or t.device != self.device or t.dtype != dt or t.numel() != 1:
                     raise ValueError("step and lr must both be numbers, or CUDA tensors of one int64 and one float32 on %s" % self.device)
-            _check(lib.sim_adamw_step_device(self._h, _ptr(step), _ptr(lr), grad_scale, K, _stream_ptr(st)))
+            _check(lib.sim_adamw_step_device(self._h, step.data_ptr(), lr.data_ptr(), grad_scale, K, st))
         else:
-            _check(lib.sim_adamw_step(self._h, step, lr, grad_scale, K, _stream_ptr(st)))
+            _check(lib.sim_adamw_step(self._h, step, lr, grad_scale, K, st))
 
     def close(self):
         if self._h:
@@ -531,25 +577,17 @@ def _matrix(x, what):
     return rows, cols, x.stride(0) if rows > 1 else cols
 
 
-def _mx_empty(rows, cols, layout, device):
-    tiles = layout == "tiles"
-    return MxTensor(torch.empty(lib.sim_mx_codes_bytes(rows, cols), dtype=torch.uint8, device=device),
-                    torch.empty(lib.sim_mx_scales_bytes(rows, cols, tiles), dtype=torch.uint8, device=device), rows, cols, layout)
-
-
 def mx_quantize(x, *, along="rows", rounding="nearest", seed=0, layout="tiles", stream=None):
     """MXFP4 form of a matrix (or vector: one row).  along "rows" -> MxTensor [rows, cols]; "cols" -> MxTensor [cols, rows] with
     blocks along x's columns; "both" -> the two from one read.  rounding "nearest" (even) or "stochastic" (from `seed`)."""
     if along not in ("rows", "cols", "both") or rounding not in ("nearest", "stochastic") or layout not in ("linear", "tiles"):
         raise ValueError("along: rows, cols or both; rounding: nearest or stochastic; layout: linear or tiles")
     rows, cols, ld = _matrix(x, "x")
-    with torch.cuda.device(x.device):
-        st = torch.cuda.current_stream() if stream is None else stream
-        q = _mx_empty(rows, cols, layout, x.device) if along != "cols" else None
-        qt = _mx_empty(cols, rows, layout, x.device) if along != "rows" else None
-        ptrs = [None if t is None else _ptr(b) for t in (q, qt) for b in ((t.codes, t.scales) if t is not None else (None, None))]
-        _check(lib.sim_mx_quantize(_ptr(x), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed, *ptrs, _stream_ptr(st)))
-    return (q, qt) if along == "both" else q if q is not None else qt
+    q = MxTensor.empty(rows, cols, layout, x.device) if along != "cols" else None
+    qt = MxTensor.empty(cols, rows, layout, x.device) if along != "rows" else None
+    _check(_on(x.device, stream, lib.sim_mx_quantize, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed,
+               q and q.codes_ptr, q and q.scales_ptr, qt and qt.codes_ptr, qt and qt.scales_ptr))
+    return (q, qt) if along == "both" else q if qt is None else qt
 
 
 def mx_dequantize(q, dtype=torch.float32, *, out=None, stream=None):
@@ -557,29 +595,24 @@ def mx_dequantize(q, dtype=torch.float32, *, out=None, stream=None):
     if out is None:
         if dtype not in DTYPES:
             raise ValueError("dtype must be float32, bfloat16 or float16")
-        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.codes.device)
+        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
     rows, cols, ld = _matrix(out, "out")
-    if (rows, cols) != (q.rows, q.cols) or out.device != q.codes.device or q.scales.device != q.codes.device:
-        raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.codes.device))
-    with torch.cuda.device(out.device):
-        st = torch.cuda.current_stream() if stream is None else stream
-        _check(lib.sim_mx_dequantize(_ptr(q.codes), _ptr(q.scales), rows, cols, q.layout == "tiles", DTYPES[out.dtype], _ptr(out), ld, _stream_ptr(st)))
+    if (rows, cols) != (q.rows, q.cols) or out.device != q.device:
+        raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.device))
+    _check(_on(q.device, stream, lib.sim_mx_dequantize, q.codes_ptr, q.scales_ptr, rows, cols, q.layout == "tiles", DTYPES[out.dtype], out.data_ptr(), ld))
     return out
 
 
 def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
     """a b^T [a.rows, b.rows] of two MxTensors with as many columns, layout "tiles", as bfloat16 or float32, or into `out`."""
-    if a.cols != b.cols or a.layout != "tiles" or b.layout != "tiles" or len({t.device for t in (a.codes, a.scales, b.codes, b.scales)}) != 1:
+    if a.cols != b.cols or a.layout != "tiles" or b.layout != "tiles" or a.device != b.device:
         raise ValueError("both operands need the same number of columns, the layout 'tiles' and one device")
     if out is None:
         if dtype not in (torch.float32, torch.bfloat16):
             raise ValueError("dtype must be bfloat16 or float32")
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.codes.device)
+        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
     rows, cols, ld = _matrix(out, "out")
-    if (rows, cols) != (a.rows, b.rows) or out.device != a.codes.device or out.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.codes.device))
-    with torch.cuda.device(out.device):
-        st = torch.cuda.current_stream() if stream is None else stream
-        _check(lib.sim_mx_matmul(_ptr(a.codes), _ptr(a.scales), _ptr(b.codes), _ptr(b.scales), a.rows, b.rows, a.cols, DTYPES[out.dtype], _ptr(out), ld,
-                                 _stream_ptr(st)))
+    if (rows, cols) != (a.rows, b.rows) or out.device != a.device or out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.device))
+    _check(_on(a.device, stream, lib.sim_mx_matmul, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, a.rows, b.rows, a.cols, DTYPES[out.dtype], out.data_ptr(), ld))
     return out

@@ -1,4 +1,5 @@
 // C entry points of MXFP4 quantisation, reading back and products (mx_kernel.cuh, mx_gemm_kernel.cuh).
+#include <atomic>
 #include <cstdio>
 
 #include "error.cuh"
@@ -23,6 +24,16 @@ int sm_count() {
   if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   return sms;
 }
+// Dynamic shared memory of a kernel, asked for once a device (the call costs a microsecond)
+template <typename K>
+cudaError_t allow_smem(K kern, int bytes, std::atomic<unsigned long long>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || (dev < 64 && (done.load(std::memory_order_relaxed) >> dev & 1))) return e;
+  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return e;
+}
 unsigned grid_for(long long threads) {
   const long long blocks = (threads + 255) / 256, full = 8ll * sm_count();
   return (unsigned)(blocks < full ? blocks : full);
@@ -35,7 +46,8 @@ cudaError_t quantize(const MxQuantArgs& a, cudaStream_t st) {
     return cudaGetLastError();
   }
   constexpr int smem = mx_tile_smem<T>();
-  cudaError_t e = cudaFuncSetAttribute(mx_quantize_tile_kernel<T, SR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_smem(mx_quantize_tile_kernel<T, SR>, smem, done);
   if (e != cudaSuccess) return e;
   const long long tiles = ((a.rows + 127) / 128) * ((a.cols + 127) / 128), full = 3ll * sm_count();     // three blocks fit (fp32 tiles: two or three)
   mx_quantize_tile_kernel<T, SR><<<(unsigned)(tiles < full ? tiles : full), 256, smem, st>>>(a);
@@ -70,7 +82,8 @@ struct MxgMaps { CUtensorMap a, b, sa, sb; };
 
 template <int T>
 cudaError_t launch_pair(const MxgMaps& m, const MxgArgs& g, int sms, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(mx_gemm_pair_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, MXP_SMEM);
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_smem(mx_gemm_pair_kernel<T>, MXP_SMEM, done);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)g.tiles_a * g.tiles_b, pairs = sms / 2;
   mx_gemm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MXP_THREADS, MXP_SMEM, st>>>(m.a, m.b, m.sa, m.sb, g);
@@ -82,7 +95,8 @@ cudaError_t launch(const MxgMaps& m, const MxgArgs& g, int split, cudaStream_t s
   auto kern = mx_gemm_kernel<BN, T, SWAP, SPLIT>;
   // partial sums of a split tile lie in the ring's bytes
   static_assert(!SPLIT || 128 * (BN + 4) * 4 <= MxgShape<BN>::OFF_BARS, "the partial sums must fit the ring");
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, MxgShape<BN>::SMEM);
+  static std::atomic<unsigned long long> done{0};
+  cudaError_t e = allow_smem(kern, MxgShape<BN>::SMEM, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1);
