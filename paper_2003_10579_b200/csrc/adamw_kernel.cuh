@@ -127,15 +127,15 @@ __device__ __forceinline__ float push_element(const void* src, const uint8_t* sc
   }
 }
 
-// Tensors whose streams allow wide accesses: a thread owns eight consecutive elements at a time.
-template <int PT, int GT, int BITS>
+// Tensors whose streams allow wide accesses: a thread owns eight consecutive elements (FULL: the chunk ends inside the tensor, all exist).
+template <int PT, int GT, int BITS, bool MULTI, bool FULL>
 __device__ __forceinline__ void adamw_chunk_wide(const AdamwArgs& a, const AdamwCoef& c, uint32_t step32, const AdamwTensor& t, const AdamwChunk ch) {
   const float keep = fmaf(-c.lr, t.decay, 1.f);
   const long long i = (long long)ch.chunk * ADAMW_CHUNK + 8 * (int)threadIdx.x;
   float p[8], g[8], m[8], v[8];      // m, v: 32-bit states
   uint32_t cm[2], cv[2];             // 8-bit states
   float sm, sv;
-  const int n8 = (int)max(0ll, min(8ll, t.n - i));
+  const int n8 = FULL ? 8 : (int)max(0ll, min(8ll, t.n - i));
   add_push<GT, true>(t.g0, t.g0_scale, i, n8, g);
   if (n8 == 8) {
     Elem<PT>::get8(t.p, i, p);
@@ -166,7 +166,7 @@ __device__ __forceinline__ void adamw_chunk_wide(const AdamwArgs& a, const Adamw
     if (n8 > 0) { sm = scale_value(t.m_scale[i >> 5]); sv = scale_value(t.v_scale[i >> 5]); }
   }
 #pragma unroll 4
-  for (int l = 1; l < a.K; ++l) {
+  for (int l = 1; MULTI && l < a.K; ++l) {
     const void* src = a.g[(size_t)l * a.n_tensors + ch.tensor];
     const uint8_t* scale = GT == T_MXFP4 ? a.g_scale[(size_t)l * a.n_tensors + ch.tensor] : nullptr;
     add_push<GT, false>(src, scale, i, n8, g);
@@ -228,7 +228,7 @@ __device__ __forceinline__ void adamw_chunk_wide(const AdamwArgs& a, const Adamw
 }
 
 // Any other alignment: neighbouring lanes take neighbouring elements, a warp a block of 32.
-template <int PT, int GT, int BITS>
+template <int PT, int GT, int BITS, bool MULTI>
 __device__ __forceinline__ void adamw_chunk_narrow(const AdamwArgs& a, const AdamwCoef& c, uint32_t step32, const AdamwTensor& t, const AdamwChunk ch) {
   const float keep = fmaf(-c.lr, t.decay, 1.f);
   const long long first = (long long)ch.chunk * ADAMW_CHUNK + (int)threadIdx.x;
@@ -251,7 +251,7 @@ __device__ __forceinline__ void adamw_chunk_narrow(const AdamwArgs& a, const Ada
         v[k] = in ? from_e4m3x2(static_cast<const uint8_t*>(t.v)[i]).x * scale_value(t.v_scale[i >> 5]) : 0.f;
       }
     }
-    for (int l = 1; l < a.K; ++l) {
+    for (int l = 1; MULTI && l < a.K; ++l) {
       const void* src = a.g[(size_t)l * a.n_tensors + ch.tensor];
       const uint8_t* scale = GT == T_MXFP4 ? a.g_scale[(size_t)l * a.n_tensors + ch.tensor] : nullptr;
 #pragma unroll
@@ -306,10 +306,11 @@ __device__ __forceinline__ void adamw_chunk_narrow(const AdamwArgs& a, const Ada
   }
 }
 
-// Blocks of an SM: with 32-bit states four, and a block per chunk (the hardware deals them: 257 M elements 1.10 ms, a grid that
-// stays 1.30 ms); with 8-bit states, where the arithmetic counts, five, and a grid that stays.
-template <int PT, int GT, int BITS>
-__global__ void __launch_bounds__(ADAMW_THREADS, BITS == 32 ? 4 : 5) adamw_kernel(const __grid_constant__ AdamwArgs a) {
+// MULTI: more than one push.  With 32-bit states a block per chunk (the hardware deals them: 257 M elements 1.10 ms, a grid that stays 1.30
+// ms); with 8-bit states, where the arithmetic counts, a grid that fills the machine once and stays (205 M elements 0.49 ms, a block
+// per chunk 0.54 ms).
+template <int PT, int GT, int BITS, bool MULTI>
+__global__ void __launch_bounds__(ADAMW_THREADS, 4) adamw_kernel(const __grid_constant__ AdamwArgs a) {
   __shared__ AdamwCoef coef_s;
   AdamwCoef c = a.coef;
   uint32_t step32 = a.step32;
@@ -325,8 +326,9 @@ __global__ void __launch_bounds__(ADAMW_THREADS, BITS == 32 ? 4 : 5) adamw_kerne
     const AdamwChunk ch = next;
     if (k + gridDim.x < a.n_chunks) next = a.chunks[k + gridDim.x];
     const AdamwTensor t = a.tensors[ch.tensor];
-    if (t.vec) adamw_chunk_wide<PT, GT, BITS>(a, c, step32, t, ch);
-    else adamw_chunk_narrow<PT, GT, BITS>(a, c, step32, t, ch);
+    if (t.vec && (long long)(ch.chunk + 1ull) * ADAMW_CHUNK <= t.n) adamw_chunk_wide<PT, GT, BITS, MULTI, true>(a, c, step32, t, ch);
+    else if (t.vec) adamw_chunk_wide<PT, GT, BITS, MULTI, false>(a, c, step32, t, ch);
+    else adamw_chunk_narrow<PT, GT, BITS, MULTI>(a, c, step32, t, ch);
   }
 }
 

@@ -12,7 +12,7 @@ using namespace ssim;
 
 namespace {
 
-struct Group { int pt, gt; uint32_t first, count, grid; };   // chunks of tensors with the same parameter and gradient types
+struct Group { int pt, gt; uint32_t first, count, grid[2]; };   // chunks of tensors with the same parameter and gradient types
 
 struct DeviceGuard {   // the handle's device for the duration of a call
   int before = -1;
@@ -26,19 +26,21 @@ struct DeviceGuard {   // the handle's device for the duration of a call
 
 using Kernel = void (*)(AdamwArgs);
 
-template <int PT, int BITS>
+template <int PT, int BITS, bool MULTI>
 Kernel pick_g(int gt) {
   switch (gt) {
-    case T_F32: return adamw_kernel<PT, T_F32, BITS>;
-    case T_BF16: return adamw_kernel<PT, T_BF16, BITS>;
-    case T_F16: return adamw_kernel<PT, T_F16, BITS>;
-    default: return adamw_kernel<PT, T_MXFP4, BITS>;
+    case T_F32: return adamw_kernel<PT, T_F32, BITS, MULTI>;
+    case T_BF16: return adamw_kernel<PT, T_BF16, BITS, MULTI>;
+    case T_F16: return adamw_kernel<PT, T_F16, BITS, MULTI>;
+    default: return adamw_kernel<PT, T_MXFP4, BITS, MULTI>;
   }
 }
-Kernel pick(int bits, int pt, int gt) {
-  if (bits == 32) return pt == T_F32 ? pick_g<T_F32, 32>(gt) : pick_g<T_BF16, 32>(gt);
-  return pt == T_F32 ? pick_g<T_F32, 8>(gt) : pick_g<T_BF16, 8>(gt);
+template <bool MULTI>
+Kernel pick_p(int bits, int pt, int gt) {
+  if (bits == 32) return pt == T_F32 ? pick_g<T_F32, 32, MULTI>(gt) : pick_g<T_BF16, 32, MULTI>(gt);
+  return pt == T_F32 ? pick_g<T_F32, 8, MULTI>(gt) : pick_g<T_BF16, 8, MULTI>(gt);
 }
+Kernel pick(int bits, int pt, int gt, int K) { return K > 1 ? pick_p<true>(bits, pt, gt) : pick_p<false>(bits, pt, gt); }
 
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -124,7 +126,7 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
   }
   for (int pt = 0; pt < 2; ++pt)
     for (int gt = 0; gt < 4; ++gt) {
-      Group grp{pt, gt, (uint32_t)chunks.size(), 0, 0};
+      Group grp{pt, gt, (uint32_t)chunks.size(), 0, {0, 0}};
       for (int i = 0; i < n_tensors; ++i)
         if ((int)ts[i].p_type == pt && (int)ts[i].g_type == gt)
           for (long long c = 0; c < (ts[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK; ++c) chunks.push_back(AdamwChunk{(uint32_t)i, (uint32_t)c});
@@ -139,12 +141,13 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
   cudaError_t e = cudaGetDevice(&h->device);
   int sms = 0;
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device);
-  for (Group& grp : groups) {     // 8-bit states: as many blocks as the machine holds at once; 32-bit: one for each chunk
-    int per_sm = 0;
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, pick(bits, grp.pt, grp.gt), ADAMW_THREADS, 0);
-    const uint32_t full = (uint32_t)(per_sm > 0 ? per_sm : 1) * (uint32_t)sms;
-    grp.grid = bits == 32 || grp.count < full ? grp.count : full;
-  }
+  for (Group& grp : groups)       // 8-bit states: as many blocks as the machine holds at once; 32-bit: one for each chunk
+    for (int multi = 0; multi < 2; ++multi) {
+      int per_sm = 0;
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, pick(bits, grp.pt, grp.gt, 1 + multi), ADAMW_THREADS, 0);
+      const uint32_t full = (uint32_t)(per_sm > 0 ? per_sm : 1) * (uint32_t)sms;
+      grp.grid[multi] = bits == 32 || grp.count < full ? grp.count : full;
+    }
   h->groups.swap(groups);
   if (e == cudaSuccess) e = cudaMalloc(&h->tables, nb_t + nb_c + 2 * nb_g);
   if (e == cudaSuccess) {
@@ -184,7 +187,7 @@ sim_status step(const sim_adamw* h, int64_t t, const int64_t* t_dev, float lr, c
   for (const Group& grp : h->groups) {
     a.chunks = h->chunks + grp.first;
     a.n_chunks = grp.count;
-    pick(h->bits, grp.pt, grp.gt)<<<grp.grid, ADAMW_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a);
+    pick(h->bits, grp.pt, grp.gt, K)<<<grp.grid[K > 1], ADAMW_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a);
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return cuda_failed("sim_adamw_step", e);
   }
