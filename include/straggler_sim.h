@@ -336,7 +336,7 @@ typedef enum { SIM_F32 = 0, SIM_BF16 = 1, SIM_F16 = 2, SIM_MXFP4 = 3 } sim_dtype
  * One parameter tensor of n elements (any n >= 0; contiguous).  All pointers are DEVICE pointers except the arrays g and
  * g_scale themselves, which are HOST arrays of n_grads device pointers, one per push.  Pointers need only the alignment of
  * their element type; where all of a tensor's streams start on 16-byte boundaries (8-bit states: 8 bytes, MXFP4 pushes: 4)
- * the accesses are wide.  Tensors and their buffers must not overlap.
+ * the accesses are wide.  A buffer that a step writes must not overlap any other of the list (SIM_ERR_ARG).
  *   p       SIM_F32 or SIM_BF16, updated in place (bf16 parameters are rounded to nearest each step)
  *   g       SIM_F32, SIM_BF16, SIM_F16, or SIM_MXFP4: ceil(n / 2) bytes of codes with ceil(n / 32) scale bytes in g_scale
  *   m, v    32-bit states: fp32 [n] first and second moment.  8-bit states: E4M3 codes [n] of m and of sqrt(v), with
@@ -363,7 +363,7 @@ typedef struct sim_adamw sim_adamw;   /* opaque; holds tables only, no state: bu
  * Binds a list of tensors with n_grads push buffers each on the current device.  state_bits is 32 or 8.  Allocates and fills
  * the tables (waits for the copy); no later call allocates or waits.  Errors: SIM_ERR_ARG for an empty list, n_grads outside
  * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps not finite or below 2^-126, a tensor with missing or misaligned
- * pointers or unknown types; SIM_ERR_ALLOC / SIM_ERR_CUDA otherwise.  *out is NULL on failure.
+ * pointers or unknown types, overlapping buffers; SIM_ERR_ALLOC / SIM_ERR_CUDA otherwise.  *out is NULL on failure.
  */
 sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, int32_t n_grads, int32_t state_bits, double beta1,
                             double beta2, double eps, uint64_t seed, sim_adamw** out);
@@ -394,7 +394,7 @@ void sim_adamw_destroy(sim_adamw* h);
  *   tiles = 0   [rows][ceil(cols / 32)]; with rows = 1 the form of a pushed gradient (SIM_MXFP4 of sim_adamw_tensor)
  *   tiles = 1   the order sim_mx_matmul reads, 16-byte aligned: 512 bytes per 128 rows x 4 blocks, the tiles of one row group one
  *               behind the other; row r of a tile at byte 16 (r % 32) + 4 (r / 32), its four blocks side by side
- * The two calls give the sizes of the buffers (0 for sizes outside [1, 2^40] or 2^48 elements).
+ * The two calls give the sizes of the buffers (0 for sizes outside [1, 2^35] or more than 2^48 elements).
  */
 int64_t sim_mx_codes_bytes(int64_t rows, int64_t cols);
 int64_t sim_mx_scales_bytes(int64_t rows, int64_t cols, int32_t tiles);

@@ -75,7 +75,7 @@ __device__ __forceinline__ uint32_t encode_e4m3(const float (&x)[8], const U4& u
     }
   }
 #pragma unroll
-  for (int w = 0; w < 2; ++w) codes[w] = __byte_perm(to_e4m3x2(q[4 * w], q[4 * w + 1]), to_e4m3x2(q[4 * w + 2], q[4 * w + 3]), 0x5410);
+  for (int w = 0; w < 2; ++w) codes[w] = to_e4m3x4(q[4 * w], q[4 * w + 1], q[4 * w + 2], q[4 * w + 3]);
   return code;
 }
 

@@ -108,9 +108,19 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t codes) {
   asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(v.x), "=f"(v.y) : "r"(h));
   return v;
 }
-__device__ __forceinline__ uint32_t to_e2m1x2(float lo, float hi) {
+// eight values -> eight E2M1 codes, the first in the lowest nibble (one block of assembly: the conversions then write into place)
+__device__ __forceinline__ uint32_t to_e2m1x8(const float (&x)[8]) {
   uint32_t r;
-  asm("{\n\t.reg .b8 c;\n\tcvt.rn.satfinite.e2m1x2.f32 c, %1, %2;\n\tmov.b32 %0, {c, 0, 0, 0};\n\t}" : "=r"(r) : "f"(hi), "f"(lo));
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\tmov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(r) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return r;
+}
+__device__ __forceinline__ uint32_t to_e4m3x4(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+      : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
 __device__ __forceinline__ float2 from_e2m1x2(uint32_t codes) {
@@ -185,10 +195,6 @@ template <> struct Elem<T_F16> {
 #pragma unroll
     for (int k = 0; k < 4; ++k) { v[2 * k] = f16_to_float(w[k] & 0xFFFFu); v[2 * k + 1] = f16_to_float(w[k] >> 16); }
   }
-  static __device__ __forceinline__ void put8(void* p, long long i, const float (&v)[8]) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) =
-        make_uint4(float_to_f16x2(v[0], v[1]), float_to_f16x2(v[2], v[3]), float_to_f16x2(v[4], v[5]), float_to_f16x2(v[6], v[7]));
-  }
 };
 
 // ---- eight consecutive elements as they are stored: their largest magnitude without unpacking 16-bit types ----------------
@@ -247,12 +253,11 @@ template <> struct Raw8<T_F16> : Raw16<T_F16> {};
 
 // eight MXFP4 codes of one word -> values in units of the scale
 __device__ __forceinline__ void e2m1x8(uint32_t w, float (&v)[8]) {
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 t = from_e2m1x2((w >> (8 * k)) & 0xFFu);
-    v[2 * k] = t.x;
-    v[2 * k + 1] = t.y;
-  }
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t.reg .b32 p, q, r, s;\n\t.reg .b16 l, h;\n\tmov.b32 {a, b, c, d}, %8;\n\t"
+      "cvt.rn.f16x2.e2m1x2 p, a;\n\tcvt.rn.f16x2.e2m1x2 q, b;\n\tcvt.rn.f16x2.e2m1x2 r, c;\n\tcvt.rn.f16x2.e2m1x2 s, d;\n\t"
+      "mov.b32 {l, h}, p;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\tmov.b32 {l, h}, q;\n\tcvt.f32.f16 %2, l;\n\tcvt.f32.f16 %3, h;\n\t"
+      "mov.b32 {l, h}, r;\n\tcvt.f32.f16 %4, l;\n\tcvt.f32.f16 %5, h;\n\tmov.b32 {l, h}, s;\n\tcvt.f32.f16 %6, l;\n\tcvt.f32.f16 %7, h;\n\t}"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]) : "r"(w));
 }
 
 }  // namespace ssim

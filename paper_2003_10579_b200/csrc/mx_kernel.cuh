@@ -47,8 +47,7 @@ __device__ __forceinline__ uint32_t encode_e2m1(float (&x)[8], float inv, const 
       for (int e = 0; e < 8; ++e) x[e] = round_stochastic<1, 0>(x[e], half_word(u, e));
     }
   }
-  const uint32_t lo = __byte_perm(to_e2m1x2(x[0], x[1]), to_e2m1x2(x[2], x[3]), 0x0040), hi = __byte_perm(to_e2m1x2(x[4], x[5]), to_e2m1x2(x[6], x[7]), 0x0040);
-  return __byte_perm(lo, hi, 0x5410);
+  return to_e2m1x8(x);
 }
 
 // Where a thread stands in a matrix whose rows are `units` pieces long, stepped by the size of the grid without a division each time
@@ -93,9 +92,9 @@ __global__ void __launch_bounds__(256) mx_quantize_rows_kernel(const __grid_cons
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = x[h].value(e);
-      q[h] = encode_e2m1<SR>(v, inv, SR ? mx_random(a.keys, MX_TAG_ROWS, 2 * w.unit + h, w.row) : U4{0, 0, 0, 0});
+      q[h] = encode_e2m1<SR>(v, inv, SR ? mx_random(a.keys, MX_TAG_ROWS, 2ull * w.unit + h, w.row) : U4{0, 0, 0, 0});
     }
-    *reinterpret_cast<uint2*>(a.codes + w.row * pitch + w.unit * 8) = make_uint2(q[0], q[1]);
+    *reinterpret_cast<uint2*>(a.codes + w.row * pitch + 8ll * w.unit) = make_uint2(q[0], q[1]);
     const long long block = w.unit >> 1;
     if ((threadIdx.x & 1) == 0 && (a.tiles || block < blocks)) a.scales[mx_scale_at(w.row, block, blocks, kb, a.tiles)] = (uint8_t)code;
   }
@@ -236,7 +235,7 @@ __global__ void __launch_bounds__(256) mx_dequantize_kernel(const __grid_constan
   for (RowWalk w((a.cols + 15) / 16); w.row < a.rows; w.next()) {
     const long long c = (long long)w.unit * 16;
     const int n = (int)min(16ll, a.cols - c);
-    const uint8_t* src = a.codes + w.row * pitch + w.unit * 8;
+    const uint8_t* src = a.codes + w.row * pitch + 8ll * w.unit;
     uint32_t q[2] = {0u, 0u};
     if (a.word && n == 16) {
       const uint2 x = *reinterpret_cast<const uint2*>(src);

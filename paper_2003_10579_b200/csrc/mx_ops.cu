@@ -16,7 +16,7 @@ sim_status cuda_failed(const char* where, cudaError_t e) {
   return record_error(e == cudaErrorMemoryAllocation ? SIM_ERR_ALLOC : SIM_ERR_CUDA, msg);
 }
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
-bool bad_size(int64_t rows, int64_t cols) { return rows < 1 || cols < 1 || rows > (int64_t)1 << 40 || cols > (int64_t)1 << 40 || rows > ((int64_t)1 << 48) / cols; }
+bool bad_size(int64_t rows, int64_t cols) { return rows < 1 || cols < 1 || rows > (int64_t)1 << 35 || cols > (int64_t)1 << 35 || rows > ((int64_t)1 << 48) / cols; }
 int elem_bytes(sim_dtype t) { return t == SIM_F32 ? 4 : 2; }
 
 int sm_count() {
@@ -122,8 +122,9 @@ cudaError_t launch_bn(int bn, const MxgMaps& m, const MxgArgs& g, int split, cud
     case 16: return launch_split<16, T, SWAP>(m, g, split, st);
     case 32: return launch_split<32, T, SWAP>(m, g, split, st);
     case 64: return launch_split<64, T, SWAP>(m, g, split, st);
-    case 128: return launch_split<128, T, SWAP>(m, g, split, st);
-    default: return cudaErrorInvalidValue;
+    default:
+      if constexpr (!SWAP) return launch_split<128, T, false>(m, g, split, st);
+      return cudaErrorInvalidValue;      // at most 64 rows are swapped
   }
 }
 
@@ -139,7 +140,7 @@ int64_t sim_mx_scales_bytes(int64_t rows, int64_t cols, int32_t tiles) {
 
 sim_status sim_mx_quantize(const void* x, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, int32_t tiles, int32_t stochastic,
                            uint64_t seed, uint8_t* codes, uint8_t* scales, uint8_t* codes_t, uint8_t* scales_t, void* cuda_stream) {
-  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_quantize: rows and cols must be >= 1, below 2^40 each and 2^48 together");
+  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_quantize: rows and cols must be in [1, 2^35], and their product at most 2^48");
   if (type != SIM_F32 && type != SIM_BF16 && type != SIM_F16) return record_error(SIM_ERR_ARG, "sim_mx_quantize: type must be SIM_F32, SIM_BF16 or SIM_F16");
   if (ld < cols || ld > ((int64_t)1 << 50) / rows) return record_error(SIM_ERR_ARG, "sim_mx_quantize: ld must be at least cols");
   if (!x || !aligned(x, elem_bytes(type))) return record_error(SIM_ERR_ARG, "sim_mx_quantize: x must be aligned to its type");
@@ -158,7 +159,7 @@ sim_status sim_mx_quantize(const void* x, sim_dtype type, int64_t rows, int64_t 
 
 sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, int32_t tiles, sim_dtype type, void* out,
                              int64_t ld, void* cuda_stream) {
-  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: rows and cols must be >= 1, below 2^40 each and 2^48 together");
+  if (bad_size(rows, cols)) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: rows and cols must be in [1, 2^35], and their product at most 2^48");
   if (type != SIM_F32 && type != SIM_BF16 && type != SIM_F16) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: type must be SIM_F32, SIM_BF16 or SIM_F16");
   if (ld < cols || ld > ((int64_t)1 << 50) / rows) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: ld must be at least cols");
   if (!codes || !scales || !out || !aligned(out, elem_bytes(type))) return record_error(SIM_ERR_ARG, "sim_mx_dequantize: codes, scales and out (aligned to its type) are required");

@@ -1,4 +1,5 @@
 // C entry points of the AdamW step over a list of tensors (adamw_kernel.cuh): argument checks, tables, launches.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstdio>
@@ -92,6 +93,37 @@ sim_status check_tensor(const sim_adamw_tensor& t, int i, int n_grads, int bits)
   return SIM_OK;
 }
 
+// A buffer that a step writes must not overlap any other buffer of the list: blocks run in any order.
+bool overlaps(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bits) {
+  struct Range { uintptr_t begin, end; bool written; };
+  std::vector<Range> all;
+  auto add = [&](const void* p, int64_t bytes, bool written) {
+    if (p && bytes > 0) all.push_back(Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written});
+  };
+  for (int i = 0; i < n_tensors; ++i) {
+    const sim_adamw_tensor& t = ts[i];
+    if (t.n == 0) continue;
+    const int64_t blocks = (t.n + 31) / 32, state = bits == 32 ? 4 * t.n : t.n;
+    add(t.p, t.n * (t.p_type == SIM_F32 ? 4 : 2), true);
+    add(t.m, state, true);
+    add(t.v, state, true);
+    if (bits == 8) { add(t.m_scale, blocks, true); add(t.v_scale, blocks, true); }
+    add(t.shadow, 2 * t.n, true);
+    for (int l = 0; l < n_grads; ++l) {
+      add(t.g[l], t.g_type == SIM_MXFP4 ? (t.n + 1) / 2 : t.n * (t.g_type == SIM_F32 ? 4 : 2), false);
+      if (t.g_type == SIM_MXFP4) add(t.g_scale[l], blocks, false);
+    }
+  }
+  std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.begin < b.begin; });
+  uintptr_t end = 0, end_written = 0;
+  for (const Range& r : all) {
+    if (r.begin < (r.written ? end : end_written)) return true;
+    end = std::max(end, r.end);
+    if (r.written) end_written = std::max(end_written, r.end);
+  }
+  return false;
+}
+
 sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bits, double beta1, double beta2, double eps, uint64_t seed,
                   sim_adamw** out) {
   if (!ts || n_tensors < 1) return record_error(SIM_ERR_ARG, "sim_adamw_create: at least one tensor is required");
@@ -105,7 +137,8 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
     if (st != SIM_OK) return st;
     total_chunks += (ts[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
   }
-  if (total_chunks > (1ll << 31)) return record_error(SIM_ERR_ARG, "sim_adamw_create: more than 2^42 elements in all");
+  if (overlaps(ts, n_tensors, n_grads, bits)) return record_error(SIM_ERR_ARG, "sim_adamw_create: a buffer that the step writes overlaps another one");
+  if (total_chunks >= (1ll << 31)) return record_error(SIM_ERR_ARG, "sim_adamw_create: more than 2^42 elements in all");
 
   std::vector<AdamwTensor> tensors((size_t)n_tensors);
   std::vector<AdamwChunk> chunks;

@@ -93,7 +93,7 @@ struct sim_handle {
   float adam_eps = 0.f, adam_decay = 0.f;
   float* adam_m = nullptr; float* adam_v = nullptr; float2* adam_bias = nullptr;
   // risk with data and parameters in MXFP4: the data's codes and scales (made on the first call), the parameters', logits, sums
-  uint8_t* mx_x = nullptr; uint8_t* mx_xs = nullptr; uint8_t* mx_w = nullptr; uint8_t* mx_ws = nullptr;
+  uint8_t* mx_x = nullptr; uint8_t* mx_x_new = nullptr; uint8_t* mx_xs = nullptr; uint8_t* mx_w = nullptr; uint8_t* mx_ws = nullptr;
   float* mx_params = nullptr; float* mx_z = nullptr; double* mx_partial = nullptr;
   long long mx_chunk = 0;
   TraceBuffers tr;
@@ -354,7 +354,7 @@ void free_all(sim_handle* h) {
   cudaFree(h->tr.t); cudaFree(h->tr.loss); cudaFree(h->tr.dist2); cudaFree(h->tr.K_used);
   cudaFree(h->tr.worker); cudaFree(h->tr.stale); cudaFree(h->tr.seq); cudaFree(h->tr.snap_slot);
   cudaFree(h->tr.new_slot); cudaFree(h->risk); cudaFree(h->mlp_eval_part);
-  cudaFree(h->adam_m); cudaFree(h->adam_v); cudaFree(h->adam_bias); cudaFree(h->mx_x); cudaFree(h->mx_xs); cudaFree(h->mx_w); cudaFree(h->mx_ws);
+  cudaFree(h->adam_m); cudaFree(h->adam_v); cudaFree(h->adam_bias); cudaFree(h->mx_x_new); cudaFree(h->mx_xs); cudaFree(h->mx_w); cudaFree(h->mx_ws);
   cudaFree(h->mx_params); cudaFree(h->mx_z); cudaFree(h->mx_partial);
 }
 
@@ -797,19 +797,18 @@ static sim_status eval_mxfp4(sim_handle* h, float* loss) {
   auto mx_failed = [&](sim_status st) { return fail(h, st, sim_last_error(nullptr)); };
   sim_status st;
   if (!h->mx_x) {                       // the data set does not change while the handle lives: its 4-bit form is made once
-    uint8_t *xc = nullptr, *xs = nullptr;
     long long chunk = ((256ll << 20) / 4 / rows_w) / MXE_SEG * MXE_SEG;      // rows of logits in 256 MB, whole segments
     chunk = chunk < MXE_SEG ? MXE_SEG : chunk > 65536 ? 65536 : chunk;
-    CUDA_TRY(h, dev_alloc(&h->mx_w, (size_t)sim_mx_codes_bytes(rows_w, d), h->stream, false));
-    CUDA_TRY(h, dev_alloc(&h->mx_ws, (size_t)sim_mx_scales_bytes(rows_w, d, 1), h->stream, false));
-    if (h->uses_pool) CUDA_TRY(h, dev_alloc(&h->mx_params, (size_t)h->R * h->n_params, h->stream, false));
-    CUDA_TRY(h, dev_alloc(&h->mx_z, (size_t)rows_w * chunk, h->stream, false));
-    CUDA_TRY(h, dev_alloc(&h->mx_partial, (size_t)h->R * seg_total, h->stream, false));
-    CUDA_TRY(h, dev_alloc(&h->mx_xs, (size_t)sim_mx_scales_bytes(n, d, 1), h->stream, false));
-    CUDA_TRY(h, dev_alloc(&xc, (size_t)sim_mx_codes_bytes(n, d), h->stream, false));
-    xs = h->mx_xs;
-    if ((st = sim_mx_quantize(h->prob.X, SIM_F32, n, d, d, 1, 0, 0, xc, xs, nullptr, nullptr, h->stream)) != SIM_OK) { if (!h->in_arena) cudaFree(xc); return mx_failed(st); }
-    h->mx_x = xc;
+    auto room = [&](auto** p, size_t count) { return *p ? cudaSuccess : dev_alloc(p, count, h->stream, false); };   // what an earlier, failed call made stays
+    CUDA_TRY(h, room(&h->mx_w, (size_t)sim_mx_codes_bytes(rows_w, d)));
+    CUDA_TRY(h, room(&h->mx_ws, (size_t)sim_mx_scales_bytes(rows_w, d, 1)));
+    if (h->uses_pool) CUDA_TRY(h, room(&h->mx_params, (size_t)h->R * h->n_params));
+    CUDA_TRY(h, room(&h->mx_z, (size_t)rows_w * chunk));
+    CUDA_TRY(h, room(&h->mx_partial, (size_t)h->R * seg_total));
+    CUDA_TRY(h, room(&h->mx_xs, (size_t)sim_mx_scales_bytes(n, d, 1)));
+    CUDA_TRY(h, room(&h->mx_x_new, (size_t)sim_mx_codes_bytes(n, d)));
+    if ((st = sim_mx_quantize(h->prob.X, SIM_F32, n, d, d, 1, 0, 0, h->mx_x_new, h->mx_xs, nullptr, nullptr, h->stream)) != SIM_OK) return mx_failed(st);
+    h->mx_x = h->mx_x_new;
     h->mx_chunk = chunk;
   }
   const float* w = h->w_state;

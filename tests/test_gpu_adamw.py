@@ -295,3 +295,34 @@ def test_refusals_on_the_device(B):
         with pytest.raises(ValueError):
             B.AdamW(ps, gs, **kw)
     assert not p.any()
+
+
+def test_overlapping_buffers_are_refused(B):
+    """The same parameter twice, states shared by two parameters, a gradient inside another parameter; two pushes may be one buffer."""
+    p, g = torch.zeros(256, device="cuda"), torch.ones(256, device="cuda")
+    q = torch.zeros(256, device="cuda")
+    z = lambda: torch.zeros(256, device="cuda")  # noqa: E731
+    m = z()
+    for ps, gs, state in (([p, p], [g, g], None), ([p, q], [g, g], {"m": [m, m], "v": [z(), z()]}), ([p, q], [g, p], None), ([p[:200], p[199:]], [g[:200], g[199:]], None)):
+        with pytest.raises(B.SimError) as e:
+            B.AdamW(ps, [gs], state=state)
+        assert e.value.status == 1 and "overlaps" in str(e.value)
+    opt = B.AdamW([p], [[g], [g]], weight_decay=0.0)
+    opt.step(1, 0.5)
+    assert torch.allclose(p, torch.full_like(p, -0.5), rtol=2.0 ** -19)      # m / sqrt(v) = 1 up to eps
+
+
+def test_offsets_beyond_32_bits(B):
+    """2^31 + 5000 elements, bf16 parameters: the last elements, and those around element 2^31, move as the formulas say."""
+    n = (1 << 31) + 5000
+    p, g = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda"), torch.full((n,), 0.25, dtype=torch.bfloat16, device="cuda")
+    g[-1], g[1 << 31] = -0.125, 0.0
+    opt = B.AdamW([p], [[g]], state_bits=8, weight_decay=0.0, seed=1)
+    opt.step(1, 0.25)
+    # first step: m / (1 - b1) = g, sqrt(v / (1 - b2)) = |g|: p moves by the step size against the sign of g
+    at = torch.tensor([0, 12345, (1 << 31) - 1, 1 << 31, (1 << 31) + 1, n - 2, n - 1], device="cuda")
+    assert p[at].float().cpu().tolist() == [0.25, 0.25, 0.25, 0.5, 0.25, 0.25, 0.75]
+    blocks = opt.state["v_scale"][0]
+    assert blocks.numel() == (n + 31) // 32 and (blocks != 0).all()
+    del opt, p, g
+    torch.cuda.empty_cache()

@@ -133,7 +133,8 @@ def test_strided_rows_and_untouched_neighbours(B):
         out = torch.full((view.shape[0], view.shape[1] + 5), 9.0, device="cuda")
         B.mx_dequantize(q, out=out[:, 2: 2 + view.shape[1]])
         # in the type of `out`: the largest bf16 is rounded to 4 * 2^126 in MXFP4, which fp32 reads as infinity
-        assert np.array_equal(out[:, 2: 2 + view.shape[1]].cpu().numpy(), quantise(ref)[0].astype(np.float32))
+        with np.errstate(over="ignore"):
+            assert np.array_equal(out[:, 2: 2 + view.shape[1]].cpu().numpy(), quantise(ref)[0].astype(np.float32))
         assert (out[:, :2] == 9).all() and (out[:, 2 + view.shape[1]:] == 9).all()
     with pytest.raises(ValueError):
         B.mx_quantize(big.t())
@@ -272,3 +273,37 @@ def test_refusals(B):
                 lambda: B.MxTensor(q.codes, q.scales, 4, 200, "tiles"), lambda: B.MxTensor(q.codes, q.scales, 129, 64, "tiles"), lambda: B.MxTensor(q.codes, q.scales, 4, 64, "x")):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_offsets_beyond_32_bits(B):
+    """A flat vector and a matrix of more than 2^32 bytes and elements: their ends are those of a small call on the same values."""
+    n = (1 << 31) + 77
+    x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    tail = 64 * 40 + 77 - 64
+    x[-tail:] = torch.randn(tail, device="cuda").bfloat16()
+    q = B.mx_quantize(x, layout="linear")
+    small = B.mx_quantize(x[n - tail:].clone(), layout="linear")
+    assert (n - tail) % 32 == 0
+    got, want = B.mx_dequantize(q, torch.bfloat16)[0, n - tail:], B.mx_dequantize(small, torch.bfloat16)[0]
+    assert torch.equal(got, want) and want.any()
+    del x, q, got
+    torch.cuda.empty_cache()
+    rows, cols = 66000, 65600                    # 4.3e9 elements
+    x = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    x[-40:] = torch.randn(40, cols, device="cuda").bfloat16()
+    q, qt = B.mx_quantize(x, along="both")
+    back = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    B.mx_dequantize(q, out=back)
+    small = B.mx_dequantize(B.mx_quantize(x[-40:].clone()), torch.bfloat16)
+    assert torch.equal(back[-40:], small) and not back[-41].any()
+    # the transpose's last row: column cols - 1, whose only entries are the last 40 (blocks of 32 rows: 65984.., 65952..)
+    y = B.mx_matmul(q, B.mx_quantize(torch.ones(1, cols, device="cuda")), torch.float32)
+    want = small.double().sum(1)
+    size = small.double().abs().sum(1)
+    assert torch.all((y[-40:, 0].double() - want).abs() <= cols * 2.0 ** -23 * size) and not y[:-40].any()
+    del back
+    t = B.mx_dequantize(qt, torch.bfloat16)
+    ref = quantise(x[65952:, -1:].double().cpu().numpy().T)[0]
+    assert np.array_equal(t[-1, 65952:].double().cpu().numpy(), ref[0])
+    del x, q, qt, t, y
+    torch.cuda.empty_cache()

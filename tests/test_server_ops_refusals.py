@@ -39,6 +39,8 @@ def test_adamw_create_refuses_bad_arguments(B):
         assert create(good, b1=b) == 1 and create(good, b2=b) == 1
     for e in (0.0, -1.0, float("nan"), float("inf"), 1e-60):
         assert create(good, eps=e) == 1
+    # p, m and v in one place: the step would write them over one another
+    assert create(good) == 1 and b"overlaps" in B.lib.sim_last_error(None)
     for kw in (dict(n=-1), dict(n=(1 << 40) + 1), dict(p_type=2), dict(p_type=3), dict(g_type=4), dict(g_type=-1), dict(weight_decay=-1.0),
                dict(weight_decay=float("nan")), dict(p=None), dict(m=None), dict(v=None), dict(g=None), dict(p=0x10002), dict(m=0x10001),
                dict(g_type=3), dict(p_type=1, shadow=0x10000)):
@@ -74,7 +76,7 @@ def test_mx_calls_refuse_bad_arguments(B):
     def quant(x=f, type=0, rows=4, cols=64, ld=64, tiles=1, codes=f, scales=f, codes_t=None, scales_t=None):
         return L.sim_mx_quantize(x, type, rows, cols, ld, tiles, 0, 0, codes, scales, codes_t, scales_t, None)
 
-    for kw in (dict(x=None), dict(x=f + 2), dict(type=3), dict(type=-1), dict(rows=0), dict(cols=0), dict(cols=-5), dict(rows=1 << 41), dict(ld=63), dict(ld=1 << 50),
+    for kw in (dict(x=None), dict(x=f + 2), dict(type=3), dict(type=-1), dict(rows=0), dict(cols=0), dict(cols=-5), dict(rows=1 << 36), dict(ld=63), dict(ld=1 << 50),
                dict(codes=None), dict(scales=None), dict(codes=None, scales=None), dict(codes_t=f), dict(scales_t=f), dict(codes=f + 8), dict(scales=f + 4),
                dict(codes_t=f + 8, scales_t=f), dict(codes_t=f, scales_t=f + 8)):
         assert quant(**kw) == 1, kw
