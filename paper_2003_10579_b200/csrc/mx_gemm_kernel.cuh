@@ -69,7 +69,9 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volat
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
   bool ok = false;
   if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
-  return __any_sync(0xFFFFFFFFu, ok);
+  ok = __any_sync(0xFFFFFFFFu, ok);
+  __syncwarp();            // what the polling lane has seen is ordered before the others' accesses
+  return ok;
 }
 // A and B E2M1, scales E8M0, M = 128, N = n; id: which half of a column's four scale bytes (0 or 2)
 __device__ __forceinline__ uint32_t mxg_idesc(int n, uint32_t id) {
@@ -413,13 +415,15 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
 
 // The warp's wait of microseconds: a look every 200 ns leaves the issue slots to the others (4096 x 8192 x 8192: 128 -> 122 us).
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
-  int ok = 0;
+  bool ok = false;
   if ((threadIdx.x & 31) == 0)
     for (int i = 0; i < (1 << 23) && !ok; ++i) {
       ok = mbar_test(bar, parity);
       if (!ok) __nanosleep(200);
     }
-  return __any_sync(0xFFFFFFFFu, ok);
+  ok = __any_sync(0xFFFFFFFFu, ok);
+  __syncwarp();
+  return ok;
 }
 
 // slot and parity of a ring, stepped
@@ -598,15 +602,12 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     MxpRing r(0), rs(1);
     for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
       for (int it = 0; it < sf_stages; ++it, r.step<MXP_SF_STAGES>(), rs.step<MXP_SFT_STAGES>()) {
-        if (!mbar_wait_warp(sf_full(r.s), r.phase)) { failed = true; break; }
+        if (!mbar_wait_warp(sf_full(r.s), r.phase) || !mbar_wait_warp(sft_empty(rs.s), rs.phase)) { failed = true; break; }
+        tc_fence_after();
         const uint4* t = reinterpret_cast<const uint4*>(base_p + MXP_OFF_SF + r.s * MXP_SF_BYTES) + lane;
         uint4 a[4], b[2][4];                                                    // [128 rows of B][k]
 #pragma unroll
         for (int k = 0; k < 4; ++k) { a[k] = t[32 * k]; b[0][k] = t[128 + 32 * k]; b[1][k] = t[256 + 32 * k]; }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(sf_empty(r.s));
-        if (!mbar_wait_warp(sft_empty(rs.s), rs.phase)) { failed = true; break; }
-        tc_fence_after();
         const uint32_t at = trow + (uint32_t)(rs.s * MXP_SCALE_COLS);
         mxp_st8(at, a[0], a[1]);
         mxp_st8(at + 8, a[2], a[3]);
@@ -615,7 +616,12 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_addr(sft_full(rs.s), 0));
+        if (lane == 0) {
+          mbar_arrive_cluster(cluster_addr(sft_full(rs.s), 0));
+          // Only here may the slot in shared memory be refilled: the stores have taken the loads' values.  An arrival right after the
+          // loads let a slow warp read the next round's scales (the loads need not have been performed by then).
+          mbar_arrive(sf_empty(r.s));
+        }
       }
     }
   } else {

@@ -188,6 +188,25 @@ def test_products_match(B, M, N, K, dtype):
     product_case(B, M, N, K, dtype)
 
 
+@pytest.mark.parametrize("M,N,K", [(4096, 8192, 2048), (8192, 8192, 512), (2816, 5376, 4100)])
+def test_many_tiles_a_multiprocessor(B, M, N, K):
+    """Several rounds of tiles for every pair of multiprocessors, so that each role of the kernel runs into the next tile, with
+    block scales spread over 2^6 so that a scale of another block shows.  Reference in fp32 on the values read back (its own sums
+    are off by as much as the kernel's may be: twice the tolerance), four runs."""
+    g = torch.Generator(device="cuda").manual_seed(M + K)
+
+    def operand(rows):
+        spread = torch.exp2(torch.randint(-3, 4, (rows, -(-K // 32), 1), generator=g, device="cuda").float()).expand(-1, -1, 32).reshape(rows, -1)[:, :K]
+        return B.mx_quantize(torch.randn(rows, K, generator=g, device="cuda") * spread)
+
+    a, b = operand(M), operand(N)
+    va, vb = B.mx_dequantize(a), B.mx_dequantize(b)
+    want, tol = va @ vb.t(), 2 * K * 2.0 ** -23 * (va.abs() @ vb.abs().t())
+    for _ in range(4):
+        outs = [B.mx_matmul(a, b, torch.float32) for _ in range(3)]
+        assert all(bool(((o - want).abs() <= tol).all()) for o in outs)
+
+
 def test_product_into_strided_rows_leaves_the_rest(B):
     for M, N in ((3, 200), (130, 190), (200, 33)):
         out = torch.full((M, N + 11), 5.0, device="cuda")
@@ -213,6 +232,27 @@ def test_products_are_the_same_bits_each_time_and_from_a_graph(B):
     z = B.mx_matmul(B.mx_quantize(x, stream=side), qw, torch.float32, stream=side)
     side.synchronize()
     assert torch.equal(z, y)
+
+
+def test_products_on_two_streams_at_once(B):
+    """A large product (pairs of multiprocessors, all of their tensor memory), small ones and quantisations, interleaved on two
+    streams: nothing is shared, and each result is what it is alone."""
+    big = [B.mx_quantize(torch.randn(n, 1500, device="cuda")) for n in (2500, 2600)]
+    small = [B.mx_quantize(torch.randn(n, 3000, device="cuda")) for n in (20, 700)]
+    x = torch.randn(300, 1100, device="cuda")
+    calls = (lambda st: B.mx_matmul(*big, torch.float32, stream=st), lambda st: B.mx_matmul(*small, torch.float32, stream=st),
+             lambda st: B.mx_dequantize(B.mx_quantize(x, along="cols", stream=st), stream=st))
+    alone = [c(None).clone() for c in calls]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    got = [[], []]
+    for i in range(12):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[k].append(((i + k) % 3, calls[(i + k) % 3](None)))
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, alone[c]) for part in got for c, out in part)
 
 
 def test_zero_and_nan_rows_in_a_product(B):
