@@ -42,7 +42,10 @@ __device__ __forceinline__ float round_normal(float a, uint32_t k16) {
 template <int MBITS, int EMIN>
 __device__ __forceinline__ float round_stochastic(float a, uint32_t k16) {
   constexpr float NORMAL = EMIN == 0 ? 1.f : 1.f / (float)(1 << -EMIN);
-  const float mag = fabsf(a), base = mag < NORMAL ? NORMAL : 0.f;
+  const float mag = fabsf(a);
+  float base;                                                     // NORMAL or zero
+  if (EMIN == 0) asm("set.lt.f32.f32 %0, %1, %2;" : "=f"(base) : "f"(mag), "f"(1.f));
+  else base = mag < NORMAL ? NORMAL : 0.f;
   return copysignf(round_normal<MBITS>(__fadd_rz(mag, base), k16) - base, a);
 }
 

@@ -39,13 +39,8 @@ __device__ __forceinline__ uint32_t encode_e2m1(float (&x)[8], float inv, const 
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] *= inv;
   if (SR) {
-    if (amin8(x) >= 1.f) {                                      // all normal in E2M1
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = round_normal<1>(x[e], half_word(u, e));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = round_stochastic<1, 0>(x[e], half_word(u, e));
-    }
+    for (int e = 0; e < 8; ++e) x[e] = round_stochastic<1, 0>(x[e], half_word(u, e));
   }
   return to_e2m1x8(x);
 }
