@@ -157,6 +157,9 @@ __device__ __forceinline__ float f16_to_float(uint32_t h) {
 __device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {      // one aligned 32-byte sector
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
 }
+__device__ __forceinline__ void load32(const void* p, uint32_t (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+}
 template <int T> struct Elem;
 template <> struct Elem<T_F32> {
   static constexpr int bytes = 4;

@@ -61,37 +61,47 @@ struct RowWalk {
   }
 };
 
-// Rows only.  A thread takes sixteen elements, two neighbouring lanes a block; rows are padded to 128 elements, so the lanes of a
-// block never stand in two rows.
+// Rows only.  A thread takes a block of 32 elements, in whole 32-byte sectors where the rows allow it.
 template <int T, bool SR>
 __global__ void __launch_bounds__(256) mx_quantize_rows_kernel(const __grid_constant__ MxQuantArgs a) {
+  constexpr int EB = Elem<T>::bytes;
   const long long kb = (a.cols + 127) / 128, blocks = (a.cols + 31) / 32, pitch = kb * 64;
-  for (RowWalk w(kb * 8); w.row < a.rows; w.next()) {
-    const long long c = (long long)w.unit * 16;
-    const char* src = static_cast<const char*>(a.x) + w.row * a.ld * Elem<T>::bytes;
-    Raw8<T> x[2];
-    if (a.vec && c + 16 <= a.cols) {
-      x[0].load(src, c);
-      x[1].load(src, c + 8);
-    } else {
-      x[0].load_some(src, c, (int)min(8ll, a.cols - c));
-      x[1].load_some(src, c + 8, (int)min(8ll, a.cols - c - 8));
-    }
-    uint32_t amax = max(x[0].amax(), x[1].amax());
-    amax = max(amax, __shfl_xor_sync(3u << (threadIdx.x & 30), amax, 1));
-    const uint32_t code = scale_code_e2m1(amax);
-    const float inv = scale_inverse(code);
-    uint32_t q[2];
+  for (RowWalk w(kb * 4); w.row < a.rows; w.next()) {
+    const long long c = (long long)w.unit * 32;
+    const char* src = static_cast<const char*>(a.x) + w.row * a.ld * EB;
+    Raw8<T> x[4];
+    if (a.vec == 2 && c + 32 <= a.cols) {
+      if constexpr (EB == 4) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+        for (int q = 0; q < 4; ++q) load32(src + (c + 8 * q) * 4, x[q].w);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t t[8];
+          load32(src + (c + 16 * q) * 2, t);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) { x[2 * q].w[k] = t[k]; x[2 * q + 1].w[k] = t[4 + k]; }
+        }
+      }
+    } else if (a.vec && c + 32 <= a.cols) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q].load(src, c + 8 * q);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q].load_some(src, c + 8 * q, (int)max(0ll, min(8ll, a.cols - c - 8 * q)));
+    }
+    const uint32_t code = scale_code_e2m1(max(max(x[0].amax(), x[1].amax()), max(x[2].amax(), x[3].amax())));
+    const float inv = scale_inverse(code);
+    uint32_t o[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = x[h].value(e);
-      q[h] = encode_e2m1<SR>(v, inv, SR ? mx_random(a.keys, MX_TAG_ROWS, 2ull * w.unit + h, w.row) : U4{0, 0, 0, 0});
+      for (int e = 0; e < 8; ++e) v[e] = x[q].value(e);
+      o[q] = encode_e2m1<SR>(v, inv, SR ? mx_random(a.keys, MX_TAG_ROWS, 4ull * w.unit + q, w.row) : U4{0, 0, 0, 0});
     }
-    *reinterpret_cast<uint2*>(a.codes + w.row * pitch + 8ll * w.unit) = make_uint2(q[0], q[1]);
-    const long long block = w.unit >> 1;
-    if ((threadIdx.x & 1) == 0 && (a.tiles || block < blocks)) a.scales[mx_scale_at(w.row, block, blocks, kb, a.tiles)] = (uint8_t)code;
+    *reinterpret_cast<uint4*>(a.codes + w.row * pitch + 16ll * w.unit) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (a.tiles || w.unit < blocks) a.scales[mx_scale_at(w.row, w.unit, blocks, kb, a.tiles)] = (uint8_t)code;
   }
 }
 
@@ -100,7 +110,7 @@ __global__ void __launch_bounds__(256) mx_quantize_rows_kernel(const __grid_cons
 // columns of 16-bit elements: one word a row) - whole blocks of the transpose, no exchange between lanes.  Codes of the
 // transpose leave through shared memory, 64 consecutive bytes a column, scales as whole 512-byte tiles.
 template <int T, bool SR>
-__global__ void __launch_bounds__(256, 3) mx_quantize_tile_kernel(const __grid_constant__ MxQuantArgs a) {
+__global__ void __launch_bounds__(256, 4) mx_quantize_tile_kernel(const __grid_constant__ MxQuantArgs a) {
   constexpr int EB = Elem<T>::bytes, CT = EB == 2 ? 2 : 1;     // columns a thread reads with one word
   extern __shared__ __align__(16) unsigned char tile[];        // [128][128] raw elements | codes_t [128][80] | scales [512] | scales_t [512]
   unsigned char* ct_s = tile + 128 * 128 * EB;
@@ -109,7 +119,8 @@ __global__ void __launch_bounds__(256, 3) mx_quantize_tile_kernel(const __grid_c
   const int tid = threadIdx.x;
   const long long row_tiles = (a.rows + 127) / 128, col_tiles = (a.cols + 127) / 128;
   const long long blocks = (a.cols + 31) / 32, blocks_t = (a.rows + 31) / 32;
-  for (long long t = blockIdx.x; t < row_tiles * col_tiles; t += gridDim.x) {
+  {
+    const long long t = blockIdx.x;
     const long long rt = t / col_tiles, c_t = t % col_tiles, r0 = rt * 128, c0 = c_t * 128;
     const int r_first = tid >> 4, g = tid & 15;
     const long long c = c0 + 8 * g;
@@ -220,52 +231,63 @@ struct MxReadArgs {
   long long rows, cols, ld;
   void* out;
   int tiles, vec;
-  int word;            // rows of codes may be read eight bytes at a time
+  int word;            // rows of codes may be read sixteen bytes at a time
 };
 
-// sixteen codes -> sixteen stored elements: 16-bit types take 32 bytes, one aligned sector a lane
+// 64 bytes of stored elements a thread (32 of 16 bits, 16 of fp32: 128 bytes a thread took 31 us instead of 27 for 30 M), in whole
+// 32-byte sectors where the rows allow it
+template <int T>
+__host__ __device__ constexpr int mx_read_unit() { return 64 / Elem<T>::bytes; }
+
 template <int T>
 __global__ void __launch_bounds__(256) mx_dequantize_kernel(const __grid_constant__ MxReadArgs a) {
+  constexpr int EB = Elem<T>::bytes, UNIT = mx_read_unit<T>(), WORDS = UNIT / 8;
   const long long kb = (a.cols + 127) / 128, blocks = (a.cols + 31) / 32, pitch = kb * 64;
-  for (RowWalk w((a.cols + 15) / 16); w.row < a.rows; w.next()) {
-    const long long c = (long long)w.unit * 16;
-    const int n = (int)min(16ll, a.cols - c);
-    const uint8_t* src = a.codes + w.row * pitch + 8ll * w.unit;
-    uint32_t q[2] = {0u, 0u};
-    if (a.word && n == 16) {
-      const uint2 x = *reinterpret_cast<const uint2*>(src);
-      q[0] = x.x; q[1] = x.y;
-    } else {
-      for (int b = 0; 2 * b < n; ++b) q[b >> 2] |= (uint32_t)src[b] << (8 * (b & 3));
-    }
-    const float s = scale_value(a.scales[mx_scale_at(w.row, w.unit >> 1, blocks, kb, a.tiles)]);
-    char* dst = static_cast<char*>(a.out) + w.row * a.ld * Elem<T>::bytes;
-    float x[2][8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      e2m1x8(q[h], x[h]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[h][e] *= s;
-    }
-    if (a.vec && n == 16) {                     // 32-byte aligned rows: whole sectors
-      if constexpr (T == T_F32) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t o[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(x[h][e]);
-          store32(dst + (c + 8 * h) * 4, o);
-        }
+  for (RowWalk w((a.cols + UNIT - 1) / UNIT); w.row < a.rows; w.next()) {
+    const long long c = (long long)w.unit * UNIT;
+    const int n = (int)min((long long)UNIT, a.cols - c);
+    const uint8_t* src = a.codes + w.row * pitch + c / 2;
+    uint32_t q[WORDS];
+    if (a.word && n == UNIT) {
+      if constexpr (WORDS == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src);
+        q[0] = x.x; q[1] = x.y; q[2] = x.z; q[3] = x.w;
       } else {
-        uint32_t o[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = T == T_BF16 ? float_to_bf16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]) : float_to_f16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]);
-        store32(dst + c * 2, o);
+        const uint2 x = *reinterpret_cast<const uint2*>(src);
+        q[0] = x.x; q[1] = x.y;
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (e < n) Elem<T>::put(dst, c + e, x[e >> 3][e & 7]);
+      for (int k = 0; k < WORDS; ++k) q[k] = 0u;
+#pragma unroll
+      for (int b = 0; b < UNIT / 2; ++b)
+        if (2 * b < n) q[b >> 2] |= (uint32_t)src[b] << (8 * (b & 3));
+    }
+    const float s = scale_value(a.scales[mx_scale_at(w.row, c >> 5, blocks, kb, a.tiles)]);
+    char* dst = static_cast<char*>(a.out) + (w.row * a.ld + c) * EB;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {                // 32 bytes of the result
+      constexpr int E = 32 / EB;
+      float x[E / 8][8];
+#pragma unroll
+      for (int k = 0; k < E / 8; ++k) {
+        e2m1x8(q[h * (E / 8) + k], x[k]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[k][e] *= s;
+      }
+      if (a.vec && n == UNIT) {
+        uint32_t o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if constexpr (EB == 4) o[k] = __float_as_uint(x[0][k]);
+          else o[k] = T == T_BF16 ? float_to_bf16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]) : float_to_f16x2(x[k >> 2][2 * (k & 3)], x[k >> 2][2 * (k & 3) + 1]);
+        }
+        store32(dst + 32 * h, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (E * h + e < n) Elem<T>::put(dst, E * h + e, x[e >> 3][e & 7]);
+      }
     }
   }
 }
