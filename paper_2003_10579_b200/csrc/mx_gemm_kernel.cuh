@@ -2,8 +2,10 @@
 //
 // tcgen05.mma kind::mxf4 multiplies 4-bit operands with a scale per 32 elements of k; one instruction takes 128 rows of A, BN rows
 // of B and 64 elements of k.  A stage holds 256 elements of k: 128 bytes a row, one swizzle atom, loaded by TMA; the rows'
-// scales come as whole 512-byte tiles (128 rows x 128 elements of k, mx_kernel.cuh), two to a TMA box, and go from shared into tensor
-// memory with tcgen05.cp, into columns of their own for each stage of the ring, so that a stage's release also frees them.
+// scales come as whole 512-byte tiles (128 rows x 128 elements of k, mx_kernel.cuh), two to a TMA box (plain bulk copies of 512 or 1024
+// bytes were far slower), and go from shared into tensor memory with tcgen05.cp, into columns of their own for each stage of the
+// ring, so that a stage's release also frees them.  This kernel takes products with few tiles or few rows; it is bound by latencies: launch,
+// first loads, the chain of its stages (1 x 12288 x 4096: 10.4 us, 26.7 MB; 1024 x 1024 x 1024: 7.4 us).
 //
 //   warp 0     producer: TMA loads into the ring
 //   warp 1     allocates tensor memory; one lane issues the copies of the scales and the MMAs
@@ -353,16 +355,21 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 // rows of A and half of B's rows.  Both load their own parts and count them on the leader's barrier; the leader issues the MMAs for
 // both; its commits release the slots of both.  Each block keeps its 128 x 256 accumulators and the scales of all 256 rows of B.
 //
-// What bounds it is the time from a slot's release to its refill, about 1.4 us of L2 latency, over the slots that shared memory
-// holds; so the scales, whose way is longer, have rings of their own that run further ahead, and nothing else sits in the codes' ring.
+// A slot of codes comes back about 1.4 us after its release, so the scales, whose way is longer, have rings of their own that run
+// further ahead, and nothing else sits in the codes' ring.  Measured at 4096 x 8192 x 8192 (bf16 result): 113 us, 4.8 PFLOP/s; the issuing
+// warp then finds codes and scales ready (no waits on either), an MMA takes about 200 cycles where the same MMA issued again on the same
+// operands takes 100: what bounds the main loop is the MMAs' own operand traffic through shared memory beside the 35 KB of loads a
+// stage.  Between tiles about 3 us are exposed (last MMA, reading the accumulators, first MMA): with 256 accumulator columns
+// and the scales there is no room for a second set.
 //
 //   warp 0      codes: TMA loads (leader's barrier)
 //   warp 1      tensor memory; in the leader one lane issues the MMAs
-//   warps 2-5   scales from shared to tensor memory with plain stores.  (tcgen05.cp by the issuing lane puts
-//               their latency into the codes' ring: 1190 cycles a stage instead of 784 without copies.)
+//   warps 2-5   scales from shared to tensor memory with plain stores.  (tcgen05.cp by the issuing lane puts their latency into
+//               the codes' ring: 1190 cycles a stage instead of 784 without copies.  Their arrivals at the leader are relaxed: the stores are
+//               ordered by tcgen05.wait::st and the fence, and a release at cluster scope took about a microsecond each.)
 //   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers, frees the accumulators, and writes while the next
 //               tile's MMAs run: 32 bytes a lane, or through shared memory where D's rows are not 32-byte aligned
-//   warp 14     scales: TMA loads (own barrier), eight stages deep
+//   warp 14     scales: TMA loads (own barrier), 512 elements of k at a time
 // Persistent: the producers run ahead of the epilogue into the next tile.
 constexpr int MXP_THREADS = 480;
 constexpr int MXP_STAGES = 5;                                         // codes: 256 elements of k (six: the same time)
@@ -387,7 +394,7 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
       ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
 }
 // Issued by one elected lane of a converged warp: with the whole warp in step the operands stay in uniform registers, where the
-// instruction wants them (a loop of one lane alone moved them there one by one: 890 cycles a stage instead of 620).
+// instruction wants them (4096 x 8192 x 8192: 121 us issued by one lane alone, 116 us so).
 __device__ __forceinline__ void mxp_commit(uint32_t bar) {            // to the barrier at this address in both blocks
   asm volatile(
       "{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
