@@ -4,6 +4,7 @@ library's CUDA kernels.  Importing this module loads ``libstraggler_sim.so`` and
 has not been built - there is no CPU path behind these calls."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 
@@ -406,6 +407,8 @@ def sweep_host(data, runs, *, P, delay_kind, mu, shift=0.0, eta, m, seed, n_repl
 
 
 # ---- operators of a parameter server for models of language-model size ---------------------------------------------------
+# A call with stream=None works on the device's current stream.  With a stream given, results belong to it, and what other streams
+# have to do before the call, or with its results, the caller orders (wait_stream, events).
 class MxTensor:
     """A matrix [rows, cols] in MXFP4: E2M1 codes (two a byte, even element in the low half, rows padded to 128 elements) and
     a power-of-two scale byte per block of 32 elements of a row.  layout "linear": scale bytes [rows, ceil(cols / 32)]; a
@@ -429,7 +432,7 @@ class MxTensor:
 
     @classmethod
     def empty(cls, rows, cols, layout, device):
-        """Uninitialised, codes and scales in one buffer."""
+        """Uninitialised, codes and scales in one buffer that belongs to the device's current stream."""
         self = cls.__new__(cls)
         nc, ns = _mx_bytes(rows, cols, layout)
         self._buffer = buf = torch.empty(nc + ns, dtype=torch.uint8, device=device)
@@ -438,6 +441,11 @@ class MxTensor:
         self.codes_ptr = buf.data_ptr()
         self.scales_ptr = self.codes_ptr + nc
         return self
+
+    def record_stream(self, stream):
+        """As of a tensor: the memory is not given to others before what `stream` has been given so far is done."""
+        for t in (self._buffer,) if self._buffer is not None else (self._codes, self._scales):
+            t.record_stream(stream)
 
     @property
     def codes(self):
@@ -460,6 +468,18 @@ def _mx_bytes(rows, cols, layout):
 
 # the raw stream of a device without a Stream object around it, where torch offers that (2 us a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+def _given(stream, device, *used):
+    """A context in which new buffers belong to `stream` (None: the device's current one), which works on `used` too: memory that the
+    caller gives back right after a call is not handed on before `stream` is done with it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if stream.device != device:
+        raise ValueError("the stream is one of %s, the buffers are on %s" % (stream.device, device))
+    for t in used:
+        t.record_stream(stream)
+    return torch.cuda.stream(stream)
 
 
 def _on(device, stream, call, *args):
@@ -499,7 +519,10 @@ class AdamW:
         kinds = ("m", "v") if state_bits == 32 else ("m", "v", "m_scale", "v_scale")
         if state is None:
             dt = torch.float32 if state_bits == 32 else torch.uint8
+            fresh = torch.cuda.current_stream(self.device) if self.device.type == "cuda" else None
             state = {k: [torch.zeros(-(-p.numel() // 32) if k.endswith("scale") else p.numel(), dtype=dt, device=self.device) for p in params] for k in kinds}
+            if fresh is not None:
+                fresh.synchronize()          # the first step may run on any stream
         if len(decay) != len(params) or (shadow is not None and len(shadow) != len(params)) or any(k not in state or len(state[k]) != len(params) for k in kinds):
             raise ValueError("weight_decay, shadow and every list of state need one entry per parameter")
 
@@ -545,7 +568,8 @@ class AdamW:
         """Step number `step` (1, 2, ...) with learning rate lr and the average of the first K pushes (default: all), on
         `stream` (default: the device's current one).  step and lr may both be CUDA tensors of one element (int64, float32):
         they are read when the step runs, for steps captured in a graph."""
-        st = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+        with _given(stream, self.device, *(t for t in (step, lr) if torch.is_tensor(t) and t.is_cuda)):
+            st = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
         K = self.n_grads if K is None else K
         if torch.is_tensor(step) or torch.is_tensor(lr):
             for t, dt in ((step, torch.int64), (lr, torch.float32)):
@@ -556,6 +580,7 @@ class AdamW:
             _check(lib.sim_adamw_step(self._h, step, lr, grad_scale, K, st))
 
     def close(self):
+        """Frees the tables; a graph that holds steps of this object must not be replayed after it."""
         if self._h:
             lib.sim_adamw_destroy(self._h)
             self._h = C.c_void_p()
@@ -583,8 +608,9 @@ def mx_quantize(x, *, along="rows", rounding="nearest", seed=0, layout="tiles", 
     if along not in ("rows", "cols", "both") or rounding not in ("nearest", "stochastic") or layout not in ("linear", "tiles"):
         raise ValueError("along: rows, cols or both; rounding: nearest or stochastic; layout: linear or tiles")
     rows, cols, ld = _matrix(x, "x")
-    q = MxTensor.empty(rows, cols, layout, x.device) if along != "cols" else None
-    qt = MxTensor.empty(cols, rows, layout, x.device) if along != "rows" else None
+    with _given(stream, x.device, x):
+        q = MxTensor.empty(rows, cols, layout, x.device) if along != "cols" else None
+        qt = MxTensor.empty(cols, rows, layout, x.device) if along != "rows" else None
     _check(_on(x.device, stream, lib.sim_mx_quantize, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed,
                q and q.codes_ptr, q and q.scales_ptr, qt and qt.codes_ptr, qt and qt.scales_ptr))
     return (q, qt) if along == "both" else q if qt is None else qt
@@ -592,10 +618,11 @@ def mx_quantize(x, *, along="rows", rounding="nearest", seed=0, layout="tiles", 
 
 def mx_dequantize(q, dtype=torch.float32, *, out=None, stream=None):
     """The values of an MxTensor as a matrix [rows, cols] of dtype (float32, bfloat16, float16), or into `out`."""
-    if out is None:
-        if dtype not in DTYPES:
-            raise ValueError("dtype must be float32, bfloat16 or float16")
-        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
+    with _given(stream, q.device, q, *(() if out is None else (out,))):
+        if out is None:
+            if dtype not in DTYPES:
+                raise ValueError("dtype must be float32, bfloat16 or float16")
+            out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
     rows, cols, ld = _matrix(out, "out")
     if (rows, cols) != (q.rows, q.cols) or out.device != q.device:
         raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.device))
@@ -607,10 +634,11 @@ def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
     """a b^T [a.rows, b.rows] of two MxTensors with as many columns, layout "tiles", as bfloat16 or float32, or into `out`."""
     if a.cols != b.cols or a.layout != "tiles" or b.layout != "tiles" or a.device != b.device:
         raise ValueError("both operands need the same number of columns, the layout 'tiles' and one device")
-    if out is None:
-        if dtype not in (torch.float32, torch.bfloat16):
-            raise ValueError("dtype must be bfloat16 or float32")
-        out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
+    with _given(stream, a.device, a, b, *(() if out is None else (out,))):
+        if out is None:
+            if dtype not in (torch.float32, torch.bfloat16):
+                raise ValueError("dtype must be bfloat16 or float32")
+            out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
     rows, cols, ld = _matrix(out, "out")
     if (rows, cols) != (a.rows, b.rows) or out.device != a.device or out.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.device))

@@ -303,6 +303,46 @@ def test_a_pushed_gradient_reaches_the_parameters(B):
     assert torch.all((p - want).abs() <= 0.1 * 2.0 ** -18)
 
 
+def test_results_on_a_given_stream_are_its_own(B):
+    """A buffer freed while its stream still writes it must not become the result of a call on another stream, and an operand dropped
+    after its call must not be overwritten before that stream has read it."""
+    x = torch.randn(1024, 4096, device="cuda")
+    want = B.mx_quantize(x)
+    back, prod = B.mx_dequantize(want), B.mx_matmul(want, want)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def busy(shape, dtype):               # memory that the current stream fills some milliseconds later, handed back at once
+        t = torch.empty(shape, dtype=dtype, device="cuda")
+        torch.cuda._sleep(20_000_000)
+        t.fill_(7)
+
+    for t in (want._buffer, back, prod):
+        busy(1, t.dtype)                  # a kernel's first launch waits for the device
+    torch.cuda.synchronize()
+    busy(want._buffer.shape, torch.uint8)
+    q = B.mx_quantize(x, stream=side)
+    busy(back.shape, back.dtype)
+    r = B.mx_dequantize(want, stream=side)
+    busy(prod.shape, prod.dtype)
+    c = B.mx_matmul(want, want, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(q._buffer, want._buffer) and torch.equal(r, back) and torch.equal(c, prod)
+    y, q2 = x.clone(), B.mx_quantize(x)
+    torch.empty_like(x).zero_()
+    torch.empty_like(want._buffer).zero_()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    q = B.mx_quantize(y, stream=side)
+    r = B.mx_dequantize(q2, stream=side)
+    del y, q2
+    torch.empty_like(x).zero_()
+    torch.empty_like(want._buffer).zero_()
+    torch.cuda.synchronize()
+    assert torch.equal(q._buffer, want._buffer) and torch.equal(r, back)
+
+
 def test_refusals(B):
     x = torch.randn(4, 64, device="cuda")
     q = B.mx_quantize(x)
