@@ -190,6 +190,7 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
   if (e == cudaSuccess && nb_c) e = cudaMemcpy(d + nb_t, chunks.data(), nb_c, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(d + nb_t + nb_c, g.data(), nb_g, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(d + nb_t + nb_c + nb_g, gs.data(), nb_g, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);   // a copy from pageable memory may return before it has arrived; other streams do not wait for it
   if (e != cudaSuccess) {
     cudaFree(h->tables);
     delete h;
@@ -254,7 +255,10 @@ sim_status sim_adamw_step_device(const sim_adamw* h, const int64_t* t, const flo
 void sim_adamw_destroy(sim_adamw* h) {
   if (!h) return;
   DeviceGuard guard(h->device);
+  cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;   // a handle may be dropped while some stream captures: that must not end the capture
+  cudaThreadExchangeStreamCaptureMode(&mode);
   cudaFree(h->tables);          // waits for the device: no step can still be reading the tables
+  cudaThreadExchangeStreamCaptureMode(&mode);
   delete h;
 }
 

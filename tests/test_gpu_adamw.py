@@ -257,6 +257,34 @@ def test_captured_steps_and_another_stream(B):
     assert all(torch.equal(a, b) for a, b in zip(want, ps + [s for k in opt.state for s in opt.state[k]]))
 
 
+def test_a_handle_dropped_during_a_capture(B):
+    """Freeing one handle's tables leaves another's capture whole."""
+    p, g = torch.ones(1000, device="cuda"), torch.ones(1000, device="cuda")
+    opt, other = B.AdamW([p], [[g]], weight_decay=0.0), B.AdamW([torch.ones(10, device="cuda")], [[torch.ones(10, device="cuda")]])
+    step, lr = torch.ones(1, dtype=torch.int64, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        other.close()
+        opt.step(step, lr)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.allclose(p, torch.full_like(p, 0.5), rtol=2.0 ** -18)       # m / sqrt(v) = 1 up to eps
+
+
+def test_the_first_step_on_another_stream(B):
+    """A list is ready for any stream when it has been made, the zeros of its states too."""
+    side, n = torch.cuda.Stream(), 1 << 22
+    p, g = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    opt = B.AdamW([p], [[g]], weight_decay=0.0)
+    opt.step(1, 0.5, stream=side)
+    torch.cuda.synchronize()
+    assert torch.allclose(opt.state["m"][0], torch.full_like(p, 0.1), rtol=2.0 ** -22)
+    assert torch.allclose(p, torch.full_like(p, 0.5), rtol=2.0 ** -18)
+
+
 def test_non_finite_gradients_show(B):
     p, g = torch.ones(64, device="cuda"), torch.ones(64, device="cuda")
     g[3] = float("nan")

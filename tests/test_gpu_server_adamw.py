@@ -68,6 +68,25 @@ def test_growing_K_and_resume(B):
     assert_params_close(a[0], o.w, "growing K")
 
 
+@pytest.mark.parametrize("variant", ["ksync", "kasync"])
+def test_K_from_the_risk(B, variant):
+    """K that follows the full-data risk of the AdamW server's parameters."""
+    data = inputs.make_lsq(600, 32, 0.1, 94)
+    w0 = np.zeros(32, np.float32)
+    adamw, kw = (0.9, 0.999, 1e-8, 0.0), dict(P=6, K=1, variant=variant, delay_kind="exp", mu=1.0, m=8, seed=3)
+    sim = B.Simulation(to_device(data), eta=0.05, n_replicas=2, **kw)
+    sim.set_adamw(adamw[:2], adamw[2], adamw[3])
+    sim.set_adasync_loss(1, 2.0)
+    sim.set_params(torch.from_numpy(w0).cuda())
+    sim.run(60)
+    w, tr = sim.params(), sim.trace()
+    sim.close()
+    for r in range(2):
+        o = OracleReplica(model="lsq", X=data["X"], y=data["y"], w0=w0, eta=0.05, replica=r, K0=1, t_interval=2.0, k_rule="loss", adamw=adamw, **kw).run(60)
+        assert len(o.k_events) > 1 and o.trace["K"] == tr["K"][r].tolist()
+        assert_params_close(w[r], o.w, "K from the risk, %s" % variant)
+
+
 def test_adamw_server_equals_the_step_over_tensors(B):
     """The simulated server's update and the step over a list of tensors are one operator: with P = K = 1 and a data set of one
     row every minibatch is that row, so the gradients can be formed here and stepped with the other entry point."""
