@@ -420,14 +420,27 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
   return ok != 0;
 }
 
-// The warp's wait of microseconds: the lane is put to sleep by the hardware (up to a millisecond a time) instead of polling, which leaves
-// the issue slots to the others (4096 x 8192 x 8192: 128 us polling, 111 us).
+__device__ __forceinline__ unsigned long long time_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+// The warp's wait for a whole tile: the lane is put to sleep by the hardware (it wakes after microseconds, not after the millisecond
+// asked for) instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us polling, 111 us).  It gives
+// up after four seconds: the longest tile whose operands fit the memory takes 0.2 s.
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
   uint32_t ok = 0;
-  if ((threadIdx.x & 31) == 0)
-    for (int i = 0; i < (1 << 12) && !ok; ++i)
+  if ((threadIdx.x & 31) == 0) {
+    unsigned long long begin = 0;
+    for (int i = 0; i < (1 << 22) && !ok; ++i) {
       asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                    : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
+      if ((i & 63) == 63 && !ok) {
+        if (!begin) begin = time_ns();
+        else if (time_ns() - begin > 4000000000ull) break;
+      }
+    }
+  }
   ok = __any_sync(0xFFFFFFFFu, ok != 0);
   __syncwarp();
   return ok != 0;

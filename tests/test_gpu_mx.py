@@ -355,6 +355,18 @@ def test_refusals(B):
             bad()
 
 
+@pytest.mark.parametrize("M,N,K", [(1500, 1600, 1 << 23), (1, 128, 1 << 26)])
+def test_very_long_sums(B, M, N, K):
+    """Tiles that take tens of milliseconds: the bounded waits for them do not run out.  Ones only: every partial sum is exact."""
+    def ones(rows):
+        codes = torch.full((rows * K // 2,), 0x22, dtype=torch.uint8, device="cuda")
+        scales = torch.full((-(-rows // 128) * (K // 128) * 512,), 127, dtype=torch.uint8, device="cuda")
+        return B.MxTensor(codes, scales, rows, K, "tiles")
+    c = B.mx_matmul(ones(M), ones(N), torch.float32)
+    assert torch.all(c == float(K))
+    torch.cuda.empty_cache()
+
+
 def test_offsets_beyond_32_bits(B):
     """A flat vector and a matrix of more than 2^32 bytes and elements: their ends are those of a small call on the same values."""
     n = (1 << 31) + 77
