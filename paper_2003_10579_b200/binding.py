@@ -435,7 +435,7 @@ class MxTensor:
         """Uninitialised, codes and scales in one buffer that belongs to the device's current stream."""
         self = cls.__new__(cls)
         nc, ns = _mx_bytes(rows, cols, layout)
-        self._buffer = buf = torch.empty(nc + ns, dtype=torch.uint8, device=device)
+        self._buffer = buf = torch.empty_strided((nc + ns,), (1,), dtype=torch.uint8, device=device)
         self._codes = self._scales = None
         self.rows, self.cols, self.layout, self.device = rows, cols, layout, buf.device
         self.codes_ptr = buf.data_ptr()
@@ -470,16 +470,23 @@ def _mx_bytes(rows, cols, layout):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_NO_STREAM = contextlib.nullcontext()
+
+
 def _given(stream, device, *used):
-    """A context in which new buffers belong to `stream` (None: the device's current one), which works on `used` too: memory that the
-    caller gives back right after a call is not handed on before `stream` is done with it."""
-    if stream is None:
-        return contextlib.nullcontext()
+    """A context in which new buffers belong to `stream`, which works on `used` too: memory that the caller gives back right after a call is
+    not handed on before `stream` is done with it."""
     if stream.device != device:
         raise ValueError("the stream is one of %s, the buffers are on %s" % (stream.device, device))
     for t in used:
         t.record_stream(stream)
     return torch.cuda.stream(stream)
+
+
+def _empty(rows, cols, dtype, device, stream):
+    """A new matrix (with strides given torch takes 0.8 us less than torch.empty does)."""
+    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+        return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
 
 
 def _on(device, stream, call, *args):
@@ -568,8 +575,9 @@ class AdamW:
         """Step number `step` (1, 2, ...) with learning rate lr and the average of the first K pushes (default: all), on
         `stream` (default: the device's current one).  step and lr may both be CUDA tensors of one element (int64, float32):
         they are read when the step runs, for steps captured in a graph."""
-        with _given(stream, self.device, *(t for t in (step, lr) if torch.is_tensor(t) and t.is_cuda)):
-            st = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
+        if stream is not None:
+            _given(stream, self.device, *(t for t in (step, lr) if torch.is_tensor(t) and t.is_cuda))
+        st = _raw_stream(self.device.index) if stream is None else stream.cuda_stream
         K = self.n_grads if K is None else K
         if torch.is_tensor(step) or torch.is_tensor(lr):
             for t, dt in ((step, torch.int64), (lr, torch.float32)):
@@ -608,24 +616,29 @@ def mx_quantize(x, *, along="rows", rounding="nearest", seed=0, layout="tiles", 
     if along not in ("rows", "cols", "both") or rounding not in ("nearest", "stochastic") or layout not in ("linear", "tiles"):
         raise ValueError("along: rows, cols or both; rounding: nearest or stochastic; layout: linear or tiles")
     rows, cols, ld = _matrix(x, "x")
-    with _given(stream, x.device, x):
-        q = MxTensor.empty(rows, cols, layout, x.device) if along != "cols" else None
-        qt = MxTensor.empty(cols, rows, layout, x.device) if along != "rows" else None
-    _check(_on(x.device, stream, lib.sim_mx_quantize, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed,
+    device = x.device
+    with _NO_STREAM if stream is None else _given(stream, device, x):
+        q = MxTensor.empty(rows, cols, layout, device) if along != "cols" else None
+        qt = MxTensor.empty(cols, rows, layout, device) if along != "rows" else None
+    _check(_on(device, stream, lib.sim_mx_quantize, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, layout == "tiles", rounding == "stochastic", seed,
                q and q.codes_ptr, q and q.scales_ptr, qt and qt.codes_ptr, qt and qt.scales_ptr))
     return (q, qt) if along == "both" else q if qt is None else qt
 
 
 def mx_dequantize(q, dtype=torch.float32, *, out=None, stream=None):
     """The values of an MxTensor as a matrix [rows, cols] of dtype (float32, bfloat16, float16), or into `out`."""
-    with _given(stream, q.device, q, *(() if out is None else (out,))):
-        if out is None:
-            if dtype not in DTYPES:
-                raise ValueError("dtype must be float32, bfloat16 or float16")
-            out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.device)
-    rows, cols, ld = _matrix(out, "out")
-    if (rows, cols) != (q.rows, q.cols) or out.device != q.device:
-        raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.device))
+    if stream is not None:
+        _given(stream, q.device, q)
+    if out is None:
+        if dtype not in DTYPES:
+            raise ValueError("dtype must be float32, bfloat16 or float16")
+        out, rows, cols, ld = _empty(q.rows, q.cols, dtype, q.device, stream), q.rows, q.cols, q.cols
+    else:
+        rows, cols, ld = _matrix(out, "out")
+        if (rows, cols) != (q.rows, q.cols) or out.device != q.device:
+            raise ValueError("out must be [%d, %d] on %s" % (q.rows, q.cols, q.device))
+        if stream is not None:
+            _given(stream, q.device, out)
     _check(_on(q.device, stream, lib.sim_mx_dequantize, q.codes_ptr, q.scales_ptr, rows, cols, q.layout == "tiles", DTYPES[out.dtype], out.data_ptr(), ld))
     return out
 
@@ -634,13 +647,17 @@ def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
     """a b^T [a.rows, b.rows] of two MxTensors with as many columns, layout "tiles", as bfloat16 or float32, or into `out`."""
     if a.cols != b.cols or a.layout != "tiles" or b.layout != "tiles" or a.device != b.device:
         raise ValueError("both operands need the same number of columns, the layout 'tiles' and one device")
-    with _given(stream, a.device, a, b, *(() if out is None else (out,))):
-        if out is None:
-            if dtype not in (torch.float32, torch.bfloat16):
-                raise ValueError("dtype must be bfloat16 or float32")
-            out = torch.empty((a.rows, b.rows), dtype=dtype, device=a.device)
-    rows, cols, ld = _matrix(out, "out")
-    if (rows, cols) != (a.rows, b.rows) or out.device != a.device or out.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.device))
+    if stream is not None:
+        _given(stream, a.device, a, b)
+    if out is None:
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("dtype must be bfloat16 or float32")
+        out, ld = _empty(a.rows, b.rows, dtype, a.device, stream), b.rows
+    else:
+        rows, cols, ld = _matrix(out, "out")
+        if (rows, cols) != (a.rows, b.rows) or out.device != a.device or out.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("out must be [%d, %d] of bfloat16 or float32 on %s" % (a.rows, b.rows, a.device))
+        if stream is not None:
+            _given(stream, a.device, out)
     _check(_on(a.device, stream, lib.sim_mx_matmul, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, a.rows, b.rows, a.cols, DTYPES[out.dtype], out.data_ptr(), ld))
     return out
