@@ -367,18 +367,19 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 //   warps 2-5   scales from shared to tensor memory with plain stores.  (tcgen05.cp by the issuing lane puts their latency into
 //               the codes' ring: 1190 cycles a stage instead of 784 without copies.  Their arrivals at the leader are relaxed: the stores are
 //               ordered by tcgen05.wait::st and the fence, and a release at cluster scope took about a microsecond each.)
-//   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers, frees the accumulators, and writes while the next
-//               tile's MMAs run: 32 bytes a lane, or through shared memory where D's rows are not 32-byte aligned
+//   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers (half of an fp32 result into shared memory), frees the
+//               accumulators, and writes through shared memory while the next tile's MMAs run, two rows of 256 bytes at a time
+//               (8192 x 8192 x 1024: 46 us; 32 bytes of its own row a lane: 58 us)
 //   warp 14     scales: TMA loads (own barrier), 512 elements of k at a time
 // Persistent: the producers run ahead of the epilogue into the next tile.
 constexpr int MXP_THREADS = 480;
-constexpr int MXP_STAGES = 5;                                         // codes: 256 elements of k (six: the same time)
 constexpr int MXP_SF_STAGES = 4, MXP_SFT_STAGES = 4;                  // scales of 512 elements of k: in shared memory, in tensor memory
 constexpr int MXP_HALF = 128 * 128;                                   // 128 rows x 128 bytes: A's rows, and this block's half of B's
 constexpr int MXP_SF_BYTES = 3 * 2048;                                // of 128 rows of A and 256 of B: four tiles of each 128 rows
+constexpr int MXP_STAGES = 4;                                         // codes: 256 elements of k (five: 1 % less at k = 8192 at most)
 constexpr int MXP_OFF_SF = MXP_STAGES * 2 * MXP_HALF;
-constexpr int MXP_OFF_STORE = MXP_OFF_SF + MXP_SF_STAGES * MXP_SF_BYTES;    // 4 KB for each epilogue warp
-constexpr int MXP_OFF_BARS = MXP_OFF_STORE + 8 * 4096;
+constexpr int MXP_OFF_STORE = MXP_OFF_SF + MXP_SF_STAGES * MXP_SF_BYTES;    // 8 KB for each epilogue warp: 32 rows of 256 bytes
+constexpr int MXP_OFF_BARS = MXP_OFF_STORE + 8 * 8192;
 constexpr int MXP_BARS = 2 * (MXP_STAGES + MXP_SF_STAGES + MXP_SFT_STAGES) + 2;
 constexpr int MXP_SMEM = MXP_OFF_BARS + 8 * MXP_BARS + 16 + 1024;
 constexpr int MXP_SCALE_COLS = 48;                                    // four tiles: 16 columns of A's scales, 32 of B's
@@ -420,27 +421,15 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
   return ok != 0;
 }
 
-__device__ __forceinline__ unsigned long long time_ns() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
-  return t;
-}
-// The warp's wait for a whole tile: the lane is put to sleep by the hardware (it wakes after microseconds, not after the millisecond
-// asked for) instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us polling, 111 us).  It gives
-// up after four seconds: the longest tile whose operands fit the memory takes 0.2 s.
+// The warp's wait for a whole tile: the lane is put to sleep by the hardware (it wakes every few microseconds, at the latest after the twenty
+// asked for) instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us polling, 113 us).  The limit is
+// a few seconds; the longest tile whose operands fit the memory takes 0.2 s.
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
   uint32_t ok = 0;
-  if ((threadIdx.x & 31) == 0) {
-    unsigned long long begin = 0;
-    for (int i = 0; i < (1 << 22) && !ok; ++i) {
+  if ((threadIdx.x & 31) == 0)
+    for (int i = 0; i < (1 << 20) && !ok; ++i)
       asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                   : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
-      if ((i & 63) == 63 && !ok) {
-        if (!begin) begin = time_ns();
-        else if (time_ns() - begin > 4000000000ull) break;
-      }
-    }
-  }
+                   : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
   ok = __any_sync(0xFFFFFFFFu, ok != 0);
   __syncwarp();
   return ok != 0;
@@ -647,7 +636,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
   } else {
     const int q = warp & 3, half = (warp - 6) >> 2;
     const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16) + 128 * half, done = cluster_addr(acc_empty, 0);
-    unsigned char* st = base_p + MXP_OFF_STORE + (warp - 6) * 4096;
+    unsigned char* st = base_p + MXP_OFF_STORE + (warp - 6) * 8192;
     uint32_t phase = 0;
     for (int tile = (int)blockIdx.x >> 1; tile < n_tiles; tile += pairs, phase ^= 1u) {
       int a0, b0;
@@ -658,57 +647,56 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
       tc_fence_after();
       const int rows = (int)max(0ll, min(32ll, g.rows_a - a0));
       constexpr int EB = Elem<T>::bytes, GROUP = 256 / EB;                      // columns taken into registers at a time: 256 bytes of a row
-#pragma unroll
-      for (int c0 = 0; c0 < 128; c0 += GROUP) {
-        uint32_t w[64];
-        if constexpr (EB == 2) {
-#pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            uint32_t v[32];
-            mxg_ld32(trow + 32 * h, v);
-            mxg_ld_wait();
-            mxg_pack<T, 32>(v, w + 16 * h);
-          }
-        } else {
-          mxg_ld32(trow + c0, w);
-          mxg_ld32(trow + c0 + 32, w + 32);
-          mxg_ld_wait();
-        }
-        if (c0 + GROUP == 128) {                                                // the accumulators are read: the next tile may start
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(done);
-        }
+      const long long cols = g.rows_b - b0;                                     // columns that exist from here on
+      uint32_t w[64];
+      auto to_rows = [&]() {                                                    // the lane's 256 bytes as a row of shared memory
         if (failed) {
 #pragma unroll
           for (int j = 0; j < 64; ++j) w[j] = EB == 2 ? 0x7FC07FC0u : 0x7FC00000u;
         }
-        const long long cols = g.rows_b - b0 - c0;                              // columns that exist from here on
-        if (g.vec && cols >= GROUP) {
-          // a lane writes its row, 32 bytes at a time
-          char* out = static_cast<char*>(g.d) + ((long long)(a0 + lane) * g.ldd + b0 + c0) * EB;
-          if (lane < rows) {
+        __syncwarp();
 #pragma unroll
-            for (int p = 0; p < 8; ++p)
-              asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out + 32 * p), "r"(w[8 * p]), "r"(w[8 * p + 1]), "r"(w[8 * p + 2]),
-                           "r"(w[8 * p + 3]), "r"(w[8 * p + 4]), "r"(w[8 * p + 5]), "r"(w[8 * p + 6]), "r"(w[8 * p + 7]) : "memory");
-          }
+        for (int p = 0; p < 16; ++p)
+          *reinterpret_cast<uint4*>(st + lane * 256 + ((p ^ (lane & 7)) << 4)) = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
+      };
+      auto write = [&](int c0) {                                                // to D's columns from b0 + c0 on, sixteen lanes a row
+        __syncwarp();
+        if (g.vec && cols >= c0 + GROUP && rows == 32) {
+          char* out = static_cast<char*>(g.d) + ((long long)(a0 + (lane >> 4)) * g.ldd + b0 + c0) * EB + (lane & 15) * 16;
+          const unsigned char* row = st + (lane >> 4) * 256;
+#pragma unroll
+          for (int it = 0; it < 16; ++it, out += 2 * g.ldd * EB)
+            *reinterpret_cast<uint4*>(out) = *reinterpret_cast<const uint4*>(row + it * 512 + (((lane & 15) ^ ((2 * it + (lane >> 4)) & 7)) << 4));
         } else {
-          // sixteen rows at a time through the warp's 4 KB
 #pragma unroll 1
-          for (int h = 0; h < 2; ++h) {
-            __syncwarp();
-            if ((lane >> 4) == h) {
-              const int r = lane & 15;
-#pragma unroll
-              for (int p = 0; p < 16; ++p)
-                *reinterpret_cast<uint4*>(st + r * 256 + ((p ^ (r & 7)) << 4)) = make_uint4(w[4 * p], w[4 * p + 1], w[4 * p + 2], w[4 * p + 3]);
-            }
-            __syncwarp();
-            mxp_write_rows<EB>(st, lane, g.d, g.ldd, a0 + 16 * h, min(16, rows - 16 * h), b0 + c0, (int)max(0ll, min((long long)GROUP, cols)));
-          }
+          for (int h = 0; h < 2; ++h)
+            mxp_write_rows<EB>(st + 4096 * h, lane, g.d, g.ldd, a0 + 16 * h, min(16, rows - 16 * h), b0 + c0, (int)max(0ll, min((long long)GROUP, cols - c0)));
         }
+      };
+      if constexpr (EB == 2) {
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          uint32_t v[32];
+          mxg_ld32(trow + 32 * h, v);
+          mxg_ld_wait();
+          mxg_pack<T, 32>(v, w + 16 * h);
+        }
+      } else {
+        // the first half of the columns waits in shared memory, so that the accumulators are free before anything is written
+        mxg_ld32(trow, w);
+        mxg_ld32(trow + 32, w + 32);
+        mxg_ld_wait();
+        to_rows();
+        mxg_ld32(trow + 64, w);
+        mxg_ld32(trow + 96, w + 32);
+        mxg_ld_wait();
       }
+      tc_fence_before();                                                        // the accumulators are read: the next tile may start
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(done);
+      if (EB == 4) write(0);
+      to_rows();
+      write(128 - GROUP);
     }
   }
   tc_fence_before();

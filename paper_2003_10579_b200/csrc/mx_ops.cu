@@ -218,7 +218,6 @@ sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const 
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e;
   if (pair) {
-    g.vec = aligned(c, 32) && ldc * elem_bytes(type) % 32 == 0 ? 1 : 0;
     g.rows_a = M; g.rows_b = N;
     g.tiles_a = (int)((M + 255) / 256); g.tiles_b = (int)((N + 255) / 256);
     if (!make_map(&m.a, a_codes, M, K, 128) || !make_map(&m.b, b_codes, N, K, 128) || !make_scale_map(&m.sa, a_scales, M, kb, 4) || !make_scale_map(&m.sb, b_scales, N, kb, 4))
