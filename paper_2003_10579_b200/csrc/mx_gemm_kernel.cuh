@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 // further ahead, and nothing else sits in the codes' ring.  Measured at 4096 x 8192 x 8192 (bf16 result): 113 us, 4.8 PFLOP/s; the issuing
 // warp then finds codes and scales ready (no waits on either), an MMA takes about 200 cycles where the same MMA issued again on the same
 // operands takes 100: what bounds the main loop is the MMAs' own operand traffic through shared memory beside the 35 KB of loads a
-// stage.  Between tiles about 3 us are exposed (last MMA, reading the accumulators, first MMA): with 256 accumulator columns
+// stage.  Between tiles 1.5 to 3 us are exposed (last MMA, reading the accumulators, first MMA): with 256 accumulator columns
 // and the scales there is no room for a second set.
 //
 //   warp 0      codes: TMA loads (leader's barrier)
