@@ -197,8 +197,11 @@ sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const 
   const int kb = (int)((K + 127) / 128), sms = sm_count();
   const int64_t tiles_a = (ra + 127) / 128;
   int bn = rb <= 16 ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
-  // pairs of multiprocessors on 256 x 256 tiles once there is a tile for every second pair (256 x 4096 x 4096, 16 tiles: 15.8 us against 12.5)
-  const bool pair = ra > 128 && rb > 128 && (ra + 255) / 256 * ((rb + 255) / 256) >= sms / 4;
+  // Pairs of multiprocessors on 256 x 256 tiles: from a tile for every second pair on (256 x 4096 x 4096, 16 tiles: 14.6 us against 13.6),
+  // and, while single multiprocessors finish in one wave, for long sums only (1280 x 2048 x 1024, 40 tiles: 10.5 against 8.5 us; 1024 x 4096 x
+  // 4096, 64 tiles: 15.7 against 15.9; 1024 x 1280 x 8192: 20.8 against 21.4; 2048 x 4096 x 1024, 128 tiles: 12.6 against 14.6)
+  const int64_t tiles_256 = (ra + 255) / 256 * ((rb + 255) / 256);
+  const bool pair = ra > 128 && rb > 128 && tiles_256 >= sms / 4 && (tiles_256 > sms / 2 || kb >= 32);
   const int64_t tiles_b = (rb + bn - 1) / bn;
   if (tiles_a * tiles_b > (int64_t)1 << 30) return record_error(SIM_ERR_ARG, "sim_mx_matmul: the result has too many tiles");
   // Few tiles: k is split over a cluster.  Narrow tiles add little to the end of the kernel, so down to 512 elements of k a block and up to

@@ -188,6 +188,13 @@ def test_products_match(B, M, N, K, dtype):
     product_case(B, M, N, K, dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("M,N,K", [(2050, 2047, 4200), (2300, 2305, 515), (1281, 2049, 8000)])
+def test_products_of_a_few_large_tiles(B, M, N, K, dtype):
+    """One or two rounds of the large tiles, ragged on every side: chosen for long sums, or once the small tiles need a second wave."""
+    product_case(B, M, N, K, dtype)
+
+
 @pytest.mark.parametrize("M,N,K", [(4096, 8192, 2048), (8192, 8192, 512), (2816, 5376, 4100)])
 def test_many_tiles_a_multiprocessor(B, M, N, K):
     """Several rounds of tiles for every pair of multiprocessors, so that each role of the kernel runs into the next tile, with
