@@ -385,7 +385,8 @@ sim_status sim_adamw_step(const sim_adamw* h, int64_t t, float lr, float grad_sc
  * *t (>= 1) before each replay. */
 sim_status sim_adamw_step_device(const sim_adamw* h, const int64_t* t, const float* lr, float grad_scale, int32_t K, void* cuda_stream);
 
-/* Waits for the device and frees the tables. */
+/* Waits for the device and frees the tables (also while another stream captures).  A graph that holds steps of the handle must not be
+ * replayed after it. */
 void sim_adamw_destroy(sim_adamw* h);
 
 /*
