@@ -372,9 +372,10 @@ sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, 
  * Step t (1, 2, ...; below 2^32) of every tensor, with the first K of its push buffers, in order:
  *   g = (grad_scale / K) sum_{l<K} g_l,  m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2,
  *   p = p (1 - lr weight_decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps).
+ * m and v are fp32 numbers during the step: v under 2^-126 has fewer bits, under 2^-150 it is zero, over 2^128 infinite.
  * 8-bit states: the step uses m and v in fp32; what is kept is rounded stochastically, with 16-bit numbers from
  * Philox4x32-10 (key = seed; counter = (element / 8, tag 2, t, index in the list)), so the same calls give the same bits
- * whatever else runs.  A positive sqrt(v) is never kept as zero (v below 2^-126 counts as zero).  A gradient that is not finite makes its element's states
+ * whatever else runs.  A positive sqrt(v) is never kept as zero.  A gradient that is not finite makes its element's states
  * (8 bits: its block's) NaN.  Elements outside [0, n) are neither read nor written.  Enqueues one launch per combination of
  * parameter and gradient type on cuda_stream (a stream of the handle's device); the handle is only read, so steps of
  * different handles may overlap.

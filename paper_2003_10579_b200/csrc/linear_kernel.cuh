@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(NT) linear1_kernel(NumericArgs a) {
               const float s2 = ac.s2 * g[4 * c + e];
               mo[e] = fmaf(ac.b1, mo[e], ac.c1 * g[4 * c + e]);
               vo[e] = fmaf(ac.b2, vo[e], s2 * s2);
-              w_cur[4 * c + e] = adamw_param(ac, a.adam_keep, w_cur[4 * c + e], mo[e], sqrt_fast(vo[e]));
+              w_cur[4 * c + e] = adamw_param(ac, a.adam_keep, w_cur[4 * c + e], mo[e], root(vo[e]));
               g[4 * c + e] = 0.f;
             }
             *mp = make_float4(mo[0], mo[1], mo[2], mo[3]);

@@ -1,0 +1,65 @@
+"""The server's operators where their ranges end: moments next to the smallest fp32 numbers, unaligned lists of every push type, the documented
+rounding of 8-bit states bit for bit, results between guard elements, long waits and small data sets.  Tolerances are derived in each test."""
+import numpy as np
+import pytest
+import torch
+
+from parity import to_device
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2003_10579_b200 import binding
+    return binding
+
+
+def tiny(n, seed):
+    """Gradients of 2^-62 to 2^-57: their squares times 1 - b2 = 2^-10 lie on both sides of 2^-126."""
+    rng = np.random.default_rng(seed)
+    return (np.exp2(rng.uniform(-62, -57, n)) * rng.choice([-1.0, 1.0], n)).astype(np.float32)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("at", [0, 1])
+def test_second_moments_under_the_smallest_normal(B, bits, at):
+    """With eps = 1e-20 the divisor is |g| for gradients far above eps, however small their squares.  v is formed in fp32: under 2^-126 it is off by
+    up to 2^-150, half a step there (its own rounding; s2 g is a normal number), so its root by the fraction 2^-151 / v; the rest as
+    elsewhere 2^-20.  at = 1: unaligned."""
+    n, eps, lr = 4500, 1e-20, 0.5
+    g = tiny(n, 3)
+    flat = [torch.zeros(n + 8, device="cuda") for _ in range(2)]
+    p, grad = (t[at: at + n] for t in flat)
+    grad.copy_(torch.from_numpy(g))
+    opt = B.AdamW([p], [[grad]], eps=eps, weight_decay=0.0, state_bits=bits)
+    opt.step(1, lr)
+    g64 = g.astype(np.float64)
+    want, v = -lr * g64 / (np.abs(g64) + eps), 0.001 * g64 * g64
+    got = p.double().cpu().numpy()
+    assert np.all(np.abs(got - want) <= lr * (2.0 ** -20 + 2.0 ** -151 / v))
+    if bits == 8:
+        assert bool((opt.state["v"][0] != 0).all())
+        return
+    m0, v0 = (opt.state[k][0].double().cpu().numpy() for k in ("m", "v"))
+    assert np.all(np.abs(v0 - v) <= 2.0 ** -20 * v + 2.0 ** -150)
+    opt.step(2, lr)
+    m, v = 0.9 * m0 + 0.1 * g64, 0.999 * v0 + 0.001 * g64 * g64
+    want = got - lr * (m / (1 - 0.9 ** 2)) / (np.sqrt(v / (1 - 0.999 ** 2)) + eps)
+    # v' = fma(b2, v, rn(s s)), s = s2 g, has two roundings (with v = 0 the sum was exact): up to 2 x 2^-150, so 2^-150 / v of the root
+    assert np.all(np.abs(p.double().cpu().numpy() - want) <= 2.0 ** -20 * (np.abs(got) + lr) + lr * 2.0 ** -150 / v)
+
+
+def test_second_moments_under_the_smallest_normal_of_the_simulated_server(B):
+    """The same in the simulated server's update: one row x, y = 1, w = 0, so the first gradient is -x exactly."""
+    d, eps, eta = 256, 1e-20, 0.5
+    x = tiny(d, 4)
+    data = {"model": "lsq", "X": x[None], "y": np.ones(1, np.float32), "n_classes": 1, "hidden": 0}
+    sim = B.Simulation(to_device(data), P=1, K=1, variant="ksync", delay_kind="exp", mu=1.0, eta=eta, m=1, seed=0, n_replicas=2)
+    sim.set_adamw((0.9, 0.999), eps, 0.0)
+    sim.set_params(torch.zeros(d, device="cuda"))
+    sim.run(1)
+    g = -x.astype(np.float64)
+    for w in sim.params():
+        assert np.all(np.abs(w - -eta * g / (np.abs(g) + eps)) <= eta * (2.0 ** -20 + 2.0 ** -151 / (0.001 * g * g)))
+    sim.close()
