@@ -124,8 +124,8 @@ sim_status sim_set_adasync_loss(sim_handle* h, int32_t K0, double t_interval);
  * AdamW instead of Eq. 2 / Eq. 3 as the server's update (same formulas as sim_adamw_step below, fp32 moments): the mean of the K
  * gradients - possibly taken at stale parameters - updates the moments, and w_{j+1} = w_j (1 - eta weight_decay) - eta
  * (m / (1 - beta1^(j+1))) / (sqrt(v / (1 - beta2^(j+1))) + eps).  Everything else (arrivals, clock, minibatches, trace) is
- * unchanged.  LSQ and LOGISTIC; only before sim_reserve / sim_run.  SIM_ERR_ARG for other models, betas outside [0, 1), eps not finite
- * or below 2^-126, weight_decay < 0, a handle with eta < 0.
+ * unchanged.  LSQ and LOGISTIC; only before sim_reserve / sim_run.  SIM_ERR_ARG for other models, betas outside [0, 1), eps outside
+ * [2^-126, 2^125], weight_decay < 0, a handle with eta < 0.
  */
 sim_status sim_set_adamw(sim_handle* h, double beta1, double beta2, double eps, float weight_decay);
 
@@ -362,7 +362,7 @@ typedef struct sim_adamw sim_adamw;   /* opaque; holds tables only, no state: bu
 /*
  * Binds a list of tensors with n_grads push buffers each on the current device.  state_bits is 32 or 8.  Allocates and fills
  * the tables (waits for the copy); no later call allocates or waits.  Errors: SIM_ERR_ARG for an empty list, n_grads outside
- * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps not finite or below 2^-126, a tensor with missing or misaligned
+ * [1, SIM_MAX_P], other state_bits, betas outside [0, 1), eps outside [2^-126, 2^125], a tensor with missing or misaligned
  * pointers or unknown types, overlapping buffers; SIM_ERR_ALLOC / SIM_ERR_CUDA otherwise.  *out is NULL on failure.
  */
 sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, int32_t n_grads, int32_t state_bits, double beta1,

@@ -34,7 +34,10 @@ __device__ __forceinline__ float root(float x) {
   const bool low = x < ROOT_NORMAL;
   return root_normal(low ? x * 281474976710656.f : x) * (low ? 5.9604644775390625e-8f : 1.f);
 }
-// relative error at most 2^-22; the divisor is at least eps, which the host requires to be a normal number
+// The instruction takes divisors under 2^-126 for zero and gives zero for those over 2^126.  eps is in the divisor, and sqrt(v / (1 - b2^t)) is
+// under 2^92 (v an fp32 number, 1 - b2 at least 2^-53), so with eps in this range neither happens.
+inline bool adamw_eps_ok(float eps) { return eps >= 1.17549435e-38f && eps <= 4.25352959e37f; }       // 2^-126, 2^125
+// relative error at most 2^-22
 __device__ __forceinline__ float reciprocal_fast(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));

@@ -1,6 +1,5 @@
 // C entry points of the AdamW step over a list of tensors (adamw_kernel.cuh): argument checks, tables, launches.
 #include <algorithm>
-#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <new>
@@ -130,7 +129,7 @@ sim_status create(const sim_adamw_tensor* ts, int n_tensors, int n_grads, int bi
   if (n_grads < 1 || n_grads > SIM_MAX_P) return record_error(SIM_ERR_ARG, "sim_adamw_create: n_grads must be in [1, SIM_MAX_P]");
   if (bits != 32 && bits != 8) return record_error(SIM_ERR_ARG, "sim_adamw_create: state_bits must be 32 or 8");
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return record_error(SIM_ERR_ARG, "sim_adamw_create: betas must be in [0, 1)");
-  if (!((float)eps >= FLT_MIN) || std::isinf((float)eps)) return record_error(SIM_ERR_ARG, "sim_adamw_create: eps must be finite and at least 2^-126");
+  if (!adamw_eps_ok((float)eps)) return record_error(SIM_ERR_ARG, "sim_adamw_create: eps must be in [2^-126, 2^125]");
   long long total_chunks = 0;
   for (int i = 0; i < n_tensors; ++i) {
     const sim_status st = check_tensor(ts[i], i, n_grads, bits);

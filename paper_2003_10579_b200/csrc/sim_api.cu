@@ -2,7 +2,6 @@
 // See include/straggler_sim.h for the contract of every entry point.
 #include "../../include/straggler_sim.h"
 
-#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstring>
@@ -851,7 +850,7 @@ sim_status sim_set_adamw(sim_handle* h, double beta1, double beta2, double eps, 
   if (h->n_updates > 0 || h->cap > 0) return fail(h, SIM_ERR_STATE, "sim_set_adamw is only allowed before sim_reserve / sim_run");
   if (h->prob.model != SIM_LSQ && h->prob.model != SIM_LOGISTIC) return fail(h, SIM_ERR_ARG, "AdamW as the server's update needs a least-squares or logistic model");
   if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return fail(h, SIM_ERR_ARG, "betas must be in [0, 1)");
-  if (!((float)eps >= FLT_MIN) || std::isinf((float)eps)) return fail(h, SIM_ERR_ARG, "eps must be finite and at least 2^-126");
+  if (!adamw_eps_ok((float)eps)) return fail(h, SIM_ERR_ARG, "eps must be in [2^-126, 2^125]");
   if (!(weight_decay >= 0.f) || std::isinf(weight_decay)) return fail(h, SIM_ERR_ARG, "weight_decay must be finite and >= 0");
   if (!(h->eta >= 0.f)) return fail(h, SIM_ERR_ARG, "AdamW needs a step size eta >= 0");
   const size_t np = (size_t)h->R * h->n_params;

@@ -63,3 +63,13 @@ def test_second_moments_under_the_smallest_normal_of_the_simulated_server(B):
     for w in sim.params():
         assert np.all(np.abs(w - -eta * g / (np.abs(g) + eps)) <= eta * (2.0 ** -20 + 2.0 ** -151 / (0.001 * g * g)))
     sim.close()
+
+
+def test_the_simulated_server_refuses_eps_whose_reciprocal_is_no_normal_number(B):
+    data = {"model": "lsq", "X": np.ones((4, 8), np.float32), "y": np.ones(4, np.float32), "n_classes": 1, "hidden": 0}
+    sim = B.Simulation(to_device(data), P=1, K=1, variant="ksync", delay_kind="exp", mu=1.0, eta=0.1, m=1, seed=0, n_replicas=1)
+    for eps in (2.0 ** -127, 2.0 ** 126, 1e300):
+        with pytest.raises(B.SimError) as e:
+            sim.set_adamw(eps=eps)
+        assert e.value.status == 1
+    sim.close()
