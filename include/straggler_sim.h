@@ -232,8 +232,8 @@ sim_status sim_error_curve(const sim_handle* h, const double* grid, int32_t n_gr
  * Diagnostic (no counterpart in the paper): exercises the path by which a device-side wait that runs out is
  * reported.  Every wait in the library's kernels is bounded; when one gives up, the block votes, sets the handle's
  * error word and drains, and the next synchronising call returns SIM_ERR_TIMEOUT and leaves the handle unusable.
- * This call enqueues a one-block kernel that waits about a thousand polls on a barrier nobody arrives at, so that
- * exactly this happens: sim_trace_size / sim_get_* then return SIM_ERR_TIMEOUT and sim_run SIM_ERR_STATE.  The
+ * This call enqueues a one-block kernel that waits about a thousand polls, and then 50 ms by the device's clock, on a
+ * barrier nobody arrives at, so that exactly this happens: sim_trace_size / sim_get_* then return SIM_ERR_TIMEOUT and sim_run SIM_ERR_STATE.  The
  * kernel ends by itself; the device and other handles are unaffected.  Returns SIM_OK after enqueueing.
  */
 sim_status sim_selftest_wait_timeout(sim_handle* h);

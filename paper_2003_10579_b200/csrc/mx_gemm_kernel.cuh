@@ -421,18 +421,14 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
   return ok != 0;
 }
 
-// The warp's wait for a whole tile: the lane is put to sleep by the hardware (it wakes every few microseconds, at the latest after the twenty
-// asked for) instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us polling, 113 us).  The limit is
-// a few seconds; the longest tile whose operands fit the memory takes 0.2 s.
+// The warp's wait for a whole tile: one lane sleeps instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us
+// polling, 113 us).  The limit is four seconds; the longest tile whose operands fit the memory takes 0.2 s.
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
-  uint32_t ok = 0;
-  if ((threadIdx.x & 31) == 0)
-    for (int i = 0; i < (1 << 20) && !ok; ++i)
-      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                   : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
-  ok = __any_sync(0xFFFFFFFFu, ok != 0);
+  bool ok = false;
+  if ((threadIdx.x & 31) == 0) ok = mbar_wait_asleep(bar, parity, 4000000000ull);
+  ok = __any_sync(0xFFFFFFFFu, ok);
   __syncwarp();
-  return ok != 0;
+  return ok;
 }
 
 // slot and parity of a ring, stepped

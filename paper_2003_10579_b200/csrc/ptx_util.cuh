@@ -39,6 +39,28 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_
   }
   return false;
 }
+// Bounded wait in which the hardware puts the thread to sleep for up to twenty microseconds at a time.  It may wake the thread earlier, so
+// that a number of wake-ups says nothing about time: the limit goes by the clock (read after every 256 tries, so that ordinary
+// waits do not read it), and the tries end it only if the clock stood still.
+__device__ __forceinline__ unsigned long long time_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ bool mbar_wait_asleep(uint32_t bar, uint32_t parity, unsigned long long limit_ns) {
+  unsigned long long begin = 0;
+  for (int round = 0; round < 1 << 18; ++round) {
+    uint32_t ok = 0;
+    for (int i = 0; i < 256 && !ok; ++i)
+      asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                   : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+    if (ok) return true;
+    const unsigned long long now = time_ns();
+    if (round == 0) begin = now;
+    if (now - begin > limit_ns) return false;
+  }
+  return false;
+}
 // global -> shared bulk copy of `bytes` (multiple of 16, both addresses 16-byte aligned)
 __device__ __forceinline__ void bulk_g2s(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile(

@@ -406,15 +406,16 @@ sim_status eval_into(sim_handle* h, float* loss) {
   return SIM_OK;
 }
 
-// Self-test of the timeout path: a wait on a barrier that nobody arrives at, with a limit of `limit` polls.  It runs out,
-// the block votes on it and reports through the handle's error word - the steps a numeric kernel takes when one of
+// Self-test of the timeout path: waits on a barrier that nobody arrives at, one with a limit of `limit` polls, one of `limit_ns`.  Both run out,
+// the block votes on them and reports through the handle's error word - the steps a numeric kernel takes when one of
 // its bounded waits gives up.  The kernel returns by itself; nothing is left waiting.
-__global__ void wait_timeout_selftest_kernel(int* err, uint32_t limit) {
+__global__ void wait_timeout_selftest_kernel(int* err, uint32_t limit, unsigned long long limit_ns) {
   __shared__ uint64_t bar;
   if (threadIdx.x == 0) { mbar_init(smem_addr(&bar), 1); mbar_fence_init(); }
   __syncthreads();
-  const bool ok = mbar_wait(smem_addr(&bar), 0u, limit);
-  if (__syncthreads_or(!ok) && threadIdx.x == 0) atomicExch(err, ERR_WAIT_TIMEOUT);
+  bool ok = mbar_wait(smem_addr(&bar), 0u, limit);
+  if (threadIdx.x == 0 && mbar_wait_asleep(smem_addr(&bar), 0u, limit_ns)) ok = true;
+  if (__syncthreads_and(!ok) && threadIdx.x == 0) atomicExch(err, ERR_WAIT_TIMEOUT);
 }
 
 // risk trace [evals][R] (as recorded) -> [R][evals] for the caller, with the clock of each evaluation: entry 0 is
@@ -967,7 +968,7 @@ sim_status sim_risk_envelope(sim_handle* const* handles, int32_t n_handles, cons
 
 sim_status sim_selftest_wait_timeout(sim_handle* h) {
   if (!h) return fail(nullptr, SIM_ERR_ARG, "handle is NULL");
-  wait_timeout_selftest_kernel<<<1, 64, 0, h->stream>>>(h->err, 1u << 10);
+  wait_timeout_selftest_kernel<<<1, 64, 0, h->stream>>>(h->err, 1u << 10, 50000000ull);
   CUDA_TRY(h, cudaGetLastError());
   return SIM_OK;
 }

@@ -1,5 +1,7 @@
 """The server's operators where their ranges end: moments next to the smallest fp32 numbers, unaligned lists of every push type, the documented
 rounding of 8-bit states bit for bit, results between guard elements, long waits and small data sets.  Tolerances are derived in each test."""
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -73,3 +75,20 @@ def test_the_simulated_server_refuses_eps_whose_reciprocal_is_no_normal_number(B
             sim.set_adamw(eps=eps)
         assert e.value.status == 1
     sim.close()
+
+
+def test_a_wait_with_a_limit_in_time_keeps_to_it(B):
+    """The self-test's second wait sleeps on a barrier that nobody arrives at and gives up after 50 ms by the clock, however often the hardware
+    wakes it; the wait for a tile of a large product is this one with four seconds."""
+    data = {"model": "lsq", "X": np.ones((4, 8), np.float32), "y": np.ones(4, np.float32), "n_classes": 1, "hidden": 0}
+    sim = B.Simulation(to_device(data), P=1, K=1, variant="ksync", delay_kind="exp", mu=1.0, eta=0.1, m=1, seed=0, n_replicas=1)
+    torch.cuda.synchronize()
+    begin = time.perf_counter()
+    sim.selftest_wait_timeout()
+    torch.cuda.synchronize()
+    took = time.perf_counter() - begin
+    with pytest.raises(B.SimError) as e:
+        sim.trace_size()
+    assert e.value.status == 4
+    sim.close()
+    assert 0.05 <= took < 0.5
