@@ -94,7 +94,7 @@ struct sim_handle {
   // risk with data and parameters in MXFP4: the data's codes and scales (made on the first call), the parameters', logits, sums
   uint8_t* mx_x = nullptr; uint8_t* mx_x_new = nullptr; uint8_t* mx_xs = nullptr; uint8_t* mx_w = nullptr; uint8_t* mx_ws = nullptr;
   float* mx_params = nullptr; float* mx_z = nullptr; double* mx_partial = nullptr;
-  long long mx_chunk = 0;
+  long long mx_chunk = 0, mx_ldz = 0;   // rows of data a product, logits between rows of mx_z
   TraceBuffers tr;
   bool poisoned = false;
   bool in_arena = false;      // buffers come from the creating thread's DeviceArena and are not freed one by one
@@ -799,17 +799,19 @@ static sim_status eval_mxfp4(sim_handle* h, float* loss) {
   if (!h->mx_x) {                       // the data set does not change while the handle lives: its 4-bit form is made once
     long long chunk = ((256ll << 20) / 4 / rows_w) / MXE_SEG * MXE_SEG;      // rows of logits in 256 MB, whole segments
     chunk = chunk < MXE_SEG ? MXE_SEG : chunk > 65536 ? 65536 : chunk;
+    const long long row = n < chunk ? (n + 3) / 4 * 4 : chunk;               // a row of logits, whole 16-byte pieces: no longer than the data set
     auto room = [&](auto** p, size_t count) { return *p ? cudaSuccess : dev_alloc(p, count, h->stream, false); };   // what an earlier, failed call made stays
     CUDA_TRY(h, room(&h->mx_w, (size_t)sim_mx_codes_bytes(rows_w, d)));
     CUDA_TRY(h, room(&h->mx_ws, (size_t)sim_mx_scales_bytes(rows_w, d, 1)));
     if (h->uses_pool) CUDA_TRY(h, room(&h->mx_params, (size_t)h->R * h->n_params));
-    CUDA_TRY(h, room(&h->mx_z, (size_t)rows_w * chunk));
+    CUDA_TRY(h, room(&h->mx_z, (size_t)rows_w * row));
     CUDA_TRY(h, room(&h->mx_partial, (size_t)h->R * seg_total));
     CUDA_TRY(h, room(&h->mx_xs, (size_t)sim_mx_scales_bytes(n, d, 1)));
     CUDA_TRY(h, room(&h->mx_x_new, (size_t)sim_mx_codes_bytes(n, d)));
     if ((st = sim_mx_quantize(h->prob.X, SIM_F32, n, d, d, 1, 0, 0, h->mx_x_new, h->mx_xs, nullptr, nullptr, h->stream)) != SIM_OK) return mx_failed(st);
     h->mx_x = h->mx_x_new;
     h->mx_chunk = chunk;
+    h->mx_ldz = row;
   }
   const float* w = h->w_state;
   if (h->uses_pool) {
@@ -822,12 +824,12 @@ static sim_status eval_mxfp4(sim_handle* h, float* loss) {
   const void* y = mdl == SIM_LSQ ? static_cast<const void*>(h->prob.y) : static_cast<const void*>(h->prob.label);
   for (long long row0 = 0; row0 < n; row0 += h->mx_chunk) {
     const long long rows = n - row0 < h->mx_chunk ? n - row0 : h->mx_chunk;
-    st = sim_mx_matmul(h->mx_w, h->mx_ws, h->mx_x + row0 * pitch, h->mx_xs + row0 / 128 * tile_row, rows_w, rows, d, SIM_F32, h->mx_z, h->mx_chunk, h->stream);
+    st = sim_mx_matmul(h->mx_w, h->mx_ws, h->mx_x + row0 * pitch, h->mx_xs + row0 / 128 * tile_row, rows_w, rows, d, SIM_F32, h->mx_z, h->mx_ldz, h->stream);
     if (st != SIM_OK) return mx_failed(st);
     const unsigned segs = (unsigned)((rows + MXE_SEG - 1) / MXE_SEG);
     for (int r0 = 0; r0 < h->R; r0 += 65535) {        // the grid's second dimension
       const int part = h->R - r0 < 65535 ? h->R - r0 : 65535;
-      mx_loss_kernel<<<dim3(segs, (unsigned)part), 256, 0, h->stream>>>(h->mx_z + (long long)r0 * C * h->mx_chunk, h->mx_chunk, y, (int)mdl, (int)C, row0, (int)rows,
+      mx_loss_kernel<<<dim3(segs, (unsigned)part), 256, 0, h->stream>>>(h->mx_z + (long long)r0 * C * h->mx_ldz, h->mx_ldz, y, (int)mdl, (int)C, row0, (int)rows,
                                                                         h->mx_partial + (long long)r0 * seg_total, (int)seg_total, (int)(row0 / MXE_SEG));
       CUDA_TRY(h, cudaGetLastError());
     }

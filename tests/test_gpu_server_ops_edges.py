@@ -92,3 +92,28 @@ def test_a_wait_with_a_limit_in_time_keeps_to_it(B):
     assert e.value.status == 4
     sim.close()
     assert 0.05 <= took < 0.5
+
+
+def test_the_risk_in_mxfp4_of_a_small_data_set_takes_little_memory(B):
+    """The logits of 1024 replicas over 2001 rows are 8 MB; with everything else the first call's buffers stay under 32 MB (cudaMalloc rounds
+    up to 2 MB).  The value is that of the same replicas in smaller groups."""
+    rng = np.random.default_rng(6)
+    data = {"model": "lsq", "X": rng.standard_normal((2001, 16)).astype(np.float32), "y": rng.standard_normal(2001).astype(np.float32), "n_classes": 1, "hidden": 0}
+    dev, kw = to_device(data), dict(P=2, K=1, variant="ksync", delay_kind="exp", mu=1.0, eta=0.1, m=4, seed=1)
+    warm = B.Simulation(dev, n_replicas=1, **kw)               # kernels are loaded, torch has its memory
+    warm.run(1)
+    warm.eval_loss(mxfp4=True)
+    sim = B.Simulation(dev, n_replicas=1024, **kw)
+    sim.run(7)
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    got = sim.eval_loss(mxfp4=True)
+    assert free - torch.cuda.mem_get_info()[0] < 32 << 20
+    for base in (0, 1019):
+        part = B.Simulation(dev, n_replicas=5, replica_base=base, **kw)
+        part.run(7)
+        # other tiles, so other orders of the 16 sums of the logits: each within 16 x 2^-23 of its magnitude, doubled by the square
+        assert np.allclose(part.eval_loss(mxfp4=True), got[base: base + 5], rtol=2.0 ** -16, atol=0)
+        part.close()
+    sim.close()
+    warm.close()
