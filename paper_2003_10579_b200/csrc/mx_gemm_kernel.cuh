@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
     }
     __syncwarp();
   } else if (warp == 1) {
-    const uint32_t sf_base = tmem + BN, b_col = (uint32_t)((b0 & 127) >> 5);
+    const uint32_t sf_base = tmem + BN;                        // b0 is a multiple of 128 (BN < 128: zero, the host gives one tile): B's scales start with their tile
     const uint64_t adesc0 = tc_desc_kmajor(base), bdesc0 = tc_desc_kmajor(base + MXG_A_BYTES);
     int s = 0;
     uint32_t phase = 0;
@@ -231,8 +231,8 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
         mxg_copy_scales(sfb + 4 * k, sc + 1024 + 512 * k);
       }
       for (int k = 0; k < nk; ++k) {
-        mxg_mma(tmem, ad + 4 * k, bd + 4 * k, mxg_idesc(BN, 0), sfa + 4 * k, sfb + 4 * k + b_col, (it > 0 || k > 0) ? 1u : 0u);
-        mxg_mma(tmem, ad + 4 * k + 2, bd + 4 * k + 2, mxg_idesc(BN, 2), sfa + 4 * k, sfb + 4 * k + b_col, 1u);
+        mxg_mma(tmem, ad + 4 * k, bd + 4 * k, mxg_idesc(BN, 0), sfa + 4 * k, sfb + 4 * k, (it > 0 || k > 0) ? 1u : 0u);
+        mxg_mma(tmem, ad + 4 * k + 2, bd + 4 * k + 2, mxg_idesc(BN, 2), sfa + 4 * k, sfb + 4 * k, 1u);
       }
       mxg_commit(empty(s));
       if (it == stages - 1) mxg_commit(acc_bar);
@@ -245,7 +245,9 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
     const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16);
     float* part = reinterpret_cast<float*>(base_p);            // the ring's bytes: every MMA has read them
     constexpr int CH = BN < 32 ? 16 : 32;
-    for (int ch = 0; ch < BN / CH; ++ch) {
+    // columns in 32s; 16-bit rows that leave through shared memory take two of them for a line
+    constexpr int STEP = !SPLIT && !SWAP && CH == 32 && Elem<T>::bytes == 2 && BN >= 64 ? 2 : 1;
+    for (int ch = 0; ch < BN / CH; ch += STEP) {
       uint32_t v[32];
       if (CH == 32) {
         tc_ld32(trow + ch * 32, v);
@@ -278,7 +280,6 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
         constexpr int EB = Elem<T>::bytes, CC = 128 / EB;
         if constexpr (CH == 32 && BN * EB >= 128) {
           if constexpr (EB == 2) {
-            if (ch & 1) continue;
             uint32_t w[64];
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = v[j];
