@@ -121,108 +121,105 @@ __global__ void __launch_bounds__(256, 4) mx_quantize_tile_kernel(const __grid_c
   const int tid = threadIdx.x;
   const long long row_tiles = (a.rows + 127) / 128, col_tiles = (a.cols + 127) / 128;
   const long long blocks = (a.cols + 31) / 32, blocks_t = (a.rows + 31) / 32;
-  {
-    const long long t = blockIdx.x;
-    const long long rt = t / col_tiles, c_t = t % col_tiles, r0 = rt * 128, c0 = c_t * 128;
-    const int r_first = tid >> 4, g = tid & 15;
-    const long long c = c0 + 8 * g;
-    const bool wide = a.vec && c + 8 <= a.cols;
-    const char* src = static_cast<const char*>(a.x) + (r0 + r_first) * a.ld * EB;
+  const long long t = blockIdx.x;
+  const long long rt = t / col_tiles, c_t = t % col_tiles, r0 = rt * 128, c0 = c_t * 128;
+  const int r_first = tid >> 4, g = tid & 15;
+  const long long c = c0 + 8 * g;
+  const bool wide = a.vec && c + 8 <= a.cols;
+  const char* src = static_cast<const char*>(a.x) + (r0 + r_first) * a.ld * EB;
 #pragma unroll
-    for (int batch = 0; batch < 2; ++batch) {
-      Raw8<T> x[4];
+  for (int batch = 0; batch < 2; ++batch) {
+    Raw8<T> x[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = (4 * batch + i) * 16 + r_first;
-        const char* from = src + (long long)(4 * batch + i) * 16 * a.ld * EB;
-        if (r0 + r < a.rows && wide) x[i].load(from, c);
-        else x[i].load_some(from, c, r0 + r < a.rows ? (int)max(0ll, min(8ll, a.cols - c)) : 0);
-      }
+    for (int i = 0; i < 4; ++i) {
+      const int r = (4 * batch + i) * 16 + r_first;
+      const char* from = src + (long long)(4 * batch + i) * 16 * a.ld * EB;
+      if (r0 + r < a.rows && wide) x[i].load(from, c);
+      else x[i].load_some(from, c, r0 + r < a.rows ? (int)max(0ll, min(8ll, a.cols - c)) : 0);
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = (4 * batch + i) * 16 + r_first;
-        uint4* to = reinterpret_cast<uint4*>(tile + (r * 128 + 8 * g) * EB);
-        to[0] = make_uint4(x[i].w[0], x[i].w[1], x[i].w[2], x[i].w[3]);
-        if constexpr (EB == 4) to[1] = make_uint4(x[i].w[4], x[i].w[5], x[i].w[6], x[i].w[7]);
-        if (a.codes) {
-          uint32_t amax = x[i].amax();
-          amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
-          amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
-          const uint32_t code = scale_code_e2m1(amax);
-          float v[8];
+    for (int i = 0; i < 4; ++i) {
+      const int r = (4 * batch + i) * 16 + r_first;
+      uint4* to = reinterpret_cast<uint4*>(tile + (r * 128 + 8 * g) * EB);
+      to[0] = make_uint4(x[i].w[0], x[i].w[1], x[i].w[2], x[i].w[3]);
+      if constexpr (EB == 4) to[1] = make_uint4(x[i].w[4], x[i].w[5], x[i].w[6], x[i].w[7]);
+      if (a.codes) {
+        uint32_t amax = x[i].amax();
+        amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+        amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+        const uint32_t code = scale_code_e2m1(amax);
+        float v[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = x[i].value(e);
-          const uint32_t w = encode_e2m1<SR>(v, scale_inverse(code), SR ? mx_random(a.keys, MX_TAG_ROWS, (c0 >> 3) + g, r0 + r) : U4{0, 0, 0, 0});
-          if (r0 + r < a.rows) *reinterpret_cast<uint32_t*>(a.codes + (r0 + r) * (col_tiles * 64) + c0 / 2 + g * 4) = w;
-          if ((g & 3) == 0) {
-            if (a.tiles) sc_s[(r & 31) * 16 + (r >> 5) * 4 + (g >> 2)] = (unsigned char)code;
-            else if (r0 + r < a.rows && (c0 >> 5) + (g >> 2) < blocks) a.scales[(r0 + r) * blocks + (c0 >> 5) + (g >> 2)] = (uint8_t)code;
-          }
+        for (int e = 0; e < 8; ++e) v[e] = x[i].value(e);
+        const uint32_t w = encode_e2m1<SR>(v, scale_inverse(code), SR ? mx_random(a.keys, MX_TAG_ROWS, (c0 >> 3) + g, r0 + r) : U4{0, 0, 0, 0});
+        if (r0 + r < a.rows) *reinterpret_cast<uint32_t*>(a.codes + (r0 + r) * (col_tiles * 64) + c0 / 2 + g * 4) = w;
+        if ((g & 3) == 0) {
+          if (a.tiles) sc_s[(r & 31) * 16 + (r >> 5) * 4 + (g >> 2)] = (unsigned char)code;
+          else if (r0 + r < a.rows && (c0 >> 5) + (g >> 2) < blocks) a.scales[(r0 + r) * blocks + (c0 >> 5) + (g >> 2)] = (uint8_t)code;
         }
       }
     }
-    __syncthreads();
-    if (a.codes && a.tiles && tid < 128)
-      reinterpret_cast<uint32_t*>(a.scales + (rt * col_tiles + c_t) * 512)[tid] = reinterpret_cast<const uint32_t*>(sc_s)[tid];
-#pragma unroll 1
-    for (int task = tid; task < 4 * 128 / CT; task += 256) {
-      const int cp = task % (128 / CT), rb = task / (128 / CT);
-      const unsigned char* col_s = tile + (rb * 32 * 128 + cp * CT) * EB;
-      // largest magnitudes of the column (of both columns side by side)
-      uint32_t top = 0;
-      float topf = 0.f;
-#pragma unroll
-      for (int i = 0; i < 32; i += 2) {
-        const uint32_t p = *reinterpret_cast<const uint32_t*>(col_s + i * 128 * EB), q = *reinterpret_cast<const uint32_t*>(col_s + (i + 1) * 128 * EB);
-        if (EB == 2) top = max_u16x2(top, max_u16x2(p & 0x7FFF7FFFu, q & 0x7FFF7FFFu));
-        else topf = max3_abs(topf, __uint_as_float(p), __uint_as_float(q));
-      }
-      uint32_t code[CT];
-      float inv[CT];
-#pragma unroll
-      for (int h = 0; h < CT; ++h) {
-        uint32_t amax;
-        if constexpr (EB == 2) amax = Raw8<T>::widen(h ? top >> 16 : top & 0xFFFFu);
-        else amax = __float_as_uint(topf) & ABS_MASK;
-        code[h] = scale_code_e2m1(amax);
-        inv[h] = scale_inverse(code[h]);
-      }
-      uint32_t w[CT][4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t raw[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(col_s + (8 * q + i) * 128 * EB);
-#pragma unroll
-        for (int h = 0; h < CT; ++h) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (T == T_F32) v[i] = __uint_as_float(raw[i]);
-            else if (T == T_BF16) v[i] = __uint_as_float(h ? raw[i] & 0xFFFF0000u : raw[i] << 16);
-            else v[i] = f16_to_float(h ? raw[i] >> 16 : raw[i] & 0xFFFFu);
-          }
-          w[h][q] = encode_e2m1<SR>(v, inv[h], SR ? mx_random(a.keys, MX_TAG_COLS, (r0 >> 3) + rb * 4 + q, c0 + cp * CT + h) : U4{0, 0, 0, 0});
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < CT; ++h) {
-        const int col = cp * CT + h;
-        *reinterpret_cast<uint4*>(ct_s + col * 80 + rb * 16) = make_uint4(w[h][0], w[h][1], w[h][2], w[h][3]);
-        if (a.tiles) sct_s[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)code[h];
-        else if (c0 + col < a.cols && (r0 >> 5) + rb < blocks_t) a.scales_t[(c0 + col) * blocks_t + (r0 >> 5) + rb] = (uint8_t)code[h];
-      }
-    }
-    __syncthreads();
-    for (int i = tid; i < 512; i += 256) {
-      const int col = i >> 2, piece = i & 3;
-      if (c0 + col < a.cols)
-        *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * (row_tiles * 64) + r0 / 2 + piece * 16) = *reinterpret_cast<const uint4*>(ct_s + col * 80 + piece * 16);
-    }
-    if (a.tiles && tid < 128)
-      reinterpret_cast<uint32_t*>(a.scales_t + (c_t * row_tiles + rt) * 512)[tid] = reinterpret_cast<const uint32_t*>(sct_s)[tid];
-    __syncthreads();
   }
+  __syncthreads();
+  if (a.codes && a.tiles && tid < 128)
+    reinterpret_cast<uint32_t*>(a.scales + (rt * col_tiles + c_t) * 512)[tid] = reinterpret_cast<const uint32_t*>(sc_s)[tid];
+#pragma unroll 1
+  for (int task = tid; task < 4 * 128 / CT; task += 256) {
+    const int cp = task % (128 / CT), rb = task / (128 / CT);
+    const unsigned char* col_s = tile + (rb * 32 * 128 + cp * CT) * EB;
+    // largest magnitudes of the column (of both columns side by side)
+    uint32_t top = 0;
+    float topf = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const uint32_t p = *reinterpret_cast<const uint32_t*>(col_s + i * 128 * EB), q = *reinterpret_cast<const uint32_t*>(col_s + (i + 1) * 128 * EB);
+      if (EB == 2) top = max_u16x2(top, max_u16x2(p & 0x7FFF7FFFu, q & 0x7FFF7FFFu));
+      else topf = max3_abs(topf, __uint_as_float(p), __uint_as_float(q));
+    }
+    uint32_t code[CT];
+    float inv[CT];
+#pragma unroll
+    for (int h = 0; h < CT; ++h) {
+      uint32_t amax;
+      if constexpr (EB == 2) amax = Raw8<T>::widen(h ? top >> 16 : top & 0xFFFFu);
+      else amax = __float_as_uint(topf) & ABS_MASK;
+      code[h] = scale_code_e2m1(amax);
+      inv[h] = scale_inverse(code[h]);
+    }
+    uint32_t w[CT][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      uint32_t raw[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) raw[i] = *reinterpret_cast<const uint32_t*>(col_s + (8 * q + i) * 128 * EB);
+#pragma unroll
+      for (int h = 0; h < CT; ++h) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (T == T_F32) v[i] = __uint_as_float(raw[i]);
+          else if (T == T_BF16) v[i] = __uint_as_float(h ? raw[i] & 0xFFFF0000u : raw[i] << 16);
+          else v[i] = f16_to_float(h ? raw[i] >> 16 : raw[i] & 0xFFFFu);
+        }
+        w[h][q] = encode_e2m1<SR>(v, inv[h], SR ? mx_random(a.keys, MX_TAG_COLS, (r0 >> 3) + rb * 4 + q, c0 + cp * CT + h) : U4{0, 0, 0, 0});
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < CT; ++h) {
+      const int col = cp * CT + h;
+      *reinterpret_cast<uint4*>(ct_s + col * 80 + rb * 16) = make_uint4(w[h][0], w[h][1], w[h][2], w[h][3]);
+      if (a.tiles) sct_s[(col & 31) * 16 + (col >> 5) * 4 + rb] = (unsigned char)code[h];
+      else if (c0 + col < a.cols && (r0 >> 5) + rb < blocks_t) a.scales_t[(c0 + col) * blocks_t + (r0 >> 5) + rb] = (uint8_t)code[h];
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < 512; i += 256) {
+    const int col = i >> 2, piece = i & 3;
+    if (c0 + col < a.cols)
+      *reinterpret_cast<uint4*>(a.codes_t + (c0 + col) * (row_tiles * 64) + r0 / 2 + piece * 16) = *reinterpret_cast<const uint4*>(ct_s + col * 80 + piece * 16);
+  }
+  if (a.tiles && tid < 128)
+    reinterpret_cast<uint32_t*>(a.scales_t + (c_t * row_tiles + rt) * 512)[tid] = reinterpret_cast<const uint32_t*>(sct_s)[tid];
 }
 template <int T>
 constexpr int mx_tile_smem() { return 128 * 128 * Elem<T>::bytes + 128 * 80 + 1024; }
