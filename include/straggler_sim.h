@@ -376,7 +376,7 @@ sim_status sim_adamw_create(const sim_adamw_tensor* tensors, int32_t n_tensors, 
  * 8-bit states: the step uses m and v in fp32; what is kept is rounded stochastically, with 16-bit numbers from
  * Philox4x32-10 (key = seed; counter = (element / 8, tag 2, t, index in the list)), so the same calls give the same bits
  * whatever else runs.  A positive sqrt(v) is never kept as zero.  A gradient that is not finite makes its element's states
- * (8 bits: its block's) NaN.  Elements outside [0, n) are neither read nor written.  Enqueues one launch per combination of
+ * (8 bits: its block's, also where v is infinite) NaN.  Elements outside [0, n) are neither read nor written.  Enqueues one launch per combination of
  * parameter and gradient type on cuda_stream (a stream of the handle's device); the handle is only read, so steps of
  * different handles may overlap.
  */
@@ -396,6 +396,7 @@ void sim_adamw_destroy(sim_adamw* h);
  *   tiles = 0   [rows][ceil(cols / 32)]; with rows = 1 the form of a pushed gradient (SIM_MXFP4 of sim_adamw_tensor)
  *   tiles = 1   the order sim_mx_matmul reads, 16-byte aligned: 512 bytes per 128 rows x 4 blocks, the tiles of one row group one
  *               behind the other; row r of a tile at byte 16 (r % 32) + 4 (r / 32), its four blocks side by side
+ * The products read whole tiles: in scales from elsewhere, the bytes of blocks behind a row's last may be anything but 0xFF.
  * The two calls give the sizes of the buffers (0 for sizes outside [1, 2^35] or more than 2^48 elements).
  */
 int64_t sim_mx_codes_bytes(int64_t rows, int64_t cols);

@@ -413,7 +413,8 @@ class MxTensor:
     """A matrix [rows, cols] in MXFP4: E2M1 codes (two a byte, even element in the low half, rows padded to 128 elements) and
     a power-of-two scale byte per block of 32 elements of a row.  layout "linear": scale bytes [rows, ceil(cols / 32)]; a
     single row is also the form of a pushed gradient.  layout "tiles": the order the products read, 512 bytes per 128 rows x
-    4 blocks (row r of a tile at byte 16 (r % 32) + 4 (r / 32)).  codes and scales are flat uint8 tensors."""
+    4 blocks (row r of a tile at byte 16 (r % 32) + 4 (r / 32)); the bytes of blocks behind a row's last may be anything but 0xFF.
+    codes and scales are flat uint8 tensors."""
 
     __slots__ = ("rows", "cols", "layout", "device", "codes_ptr", "scales_ptr", "_codes", "_scales", "_buffer")
 

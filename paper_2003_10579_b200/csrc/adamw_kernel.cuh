@@ -1,4 +1,4 @@
-// AdamW over a list of tensors, one launch: the step of a parameter server that averages K pushed gradients.
+// AdamW over a list of tensors, a launch per combination of types: the step of a parameter server that averages K pushed gradients.
 //
 //   g  = (grad_scale / K) sum_{l<K} g_l            (in arrival order, fp32)
 //   m' = b1 m + (1 - b1) g,   v' = b2 v + (1 - b2) g^2
@@ -15,7 +15,8 @@
 //
 // Bound by HBM (at fp32 p, bf16 g: 26 bytes an element with 32-bit states, 14 with 8-bit ones): 257 M elements with a bf16 copy 1.05 ms, 6.8
 // TB/s.  With 8-bit states the arithmetic is close behind (about 57 instructions an element, most of them the two roundings and
-// Philox): 205 M elements 0.49 ms, 5.9 TB/s; with four MXFP4 pushes to decode it leads (65 M elements 0.23 ms).  A thread owns eight
+// Philox): 205 M elements 0.49 to 0.54 ms by the clock, 5.4 to 5.9 TB/s.  With four MXFP4 pushes to decode, 56.6 M elements 0.23 ms, neither HBM (60 %)
+// nor the issue slots (58 %, 80 instructions an element) are full: a chunk's loads start when the last chunk is stored.  A thread owns eight
 // consecutive elements, so all streams are 16-byte accesses; four neighbouring lanes own a block of 32 and find its largest
 // magnitude with two shuffles.  Chunks of 2048 elements of any tensor come from a table made when the list
 // was bound.
@@ -316,9 +317,10 @@ __device__ __forceinline__ void adamw_chunk_narrow(const AdamwArgs& a, const Ada
   }
 }
 
-// MULTI: more than one push.  With 32-bit states a block per chunk (the hardware deals them: 257 M elements 1.10 ms, a grid that stays 1.30
-// ms); with 8-bit states, where the arithmetic counts, a grid that fills the machine once and stays (205 M elements 0.49 ms, a block
-// per chunk 0.54 ms).
+// MULTI: more than one push.  With 32-bit states a block per chunk (the hardware deals them: 257 M elements with a bf16 copy 1.04 ms, a grid
+// that stays 1.28 ms); with 8-bit states, where the arithmetic counts, a grid that fills the machine once and stays (205 M elements 0.49 ms, a
+// block per chunk 0.56 ms).  Step and rate read on the device: every block works the coefficients out (257 M elements 1.05 ms, 12.9 M
+// 50 against 47 us).
 template <int PT, int GT, int BITS, bool MULTI>
 __global__ void __launch_bounds__(ADAMW_THREADS, 4) adamw_kernel(const __grid_constant__ AdamwArgs a) {
   __shared__ AdamwCoef coef_s;

@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
 //               ordered by tcgen05.wait::st and the fence, and a release at cluster scope took about a microsecond each.)
 //   warps 6-13  epilogue: a warp takes 32 rows x 128 columns into registers (half of an fp32 result into shared memory), frees the
 //               accumulators, and writes through shared memory while the next tile's MMAs run, two rows of 256 bytes at a time
-//               (8192 x 8192 x 1024: 46 us; 32 bytes of its own row a lane: 58 us)
+//               (8192 x 8192 x 1024: 44 to 49 us by the clock; 32 bytes of its own row a lane: 58 us)
 //   warp 14     scales: TMA loads (own barrier), 512 elements of k at a time
 // Persistent: the producers run ahead of the epilogue into the next tile.
 constexpr int MXP_THREADS = 480;

@@ -6,7 +6,7 @@
 //   tiles   the order the block-scaled tensor-core products read: tiles of 128 rows x 4 blocks, 512 bytes, tiles of one row group
 //           one behind the other; row r of a tile at byte 16 (r % 32) + 4 (r / 32), its four blocks side by side.
 // The floor of each is HBM: 4 or 2 bytes an element in, 17/32 out per orientation.  Measured: 8192 x 5120 bf16 along rows 18.6 us (5.7 TB/s),
-// along both axes 37 us (3.5 TB/s: about 18 instructions an element lead), read back 19.6 us (5.4 TB/s); 30 M fp32 along one row 26.7
+// along both axes 37 us (3.5 TB/s; 69 % of the issue slots: a block's three phases wait for one another; stochastically 78 us), read back 19.6 us (5.4 TB/s); 30 M fp32 along one row 26.7
 // us, stochastically 31 us (4.4 TB/s), read back 26.6 us.
 #pragma once
 #include "lowbits.cuh"
