@@ -429,6 +429,100 @@ sim_status sim_mx_dequantize(const uint8_t* codes, const uint8_t* scales, int64_
 sim_status sim_mx_matmul(const uint8_t* a_codes, const uint8_t* a_scales, const uint8_t* b_codes, const uint8_t* b_scales, int64_t M, int64_t N,
                          int64_t K, sim_dtype type, void* c, int64_t ldc, void* cuda_stream);
 
+/* ---- operators of a worker for models of language-model size -------------------------------------------------------------
+ *
+ * What a worker computes between fetching parameters and pushing a gradient when the model is large: its layers (products with bias,
+ * activation and residual, and the products of their backward pass), what it keeps of them until then (activations in 8 bits),
+ * and its loss (log probabilities of the given tokens).  As above: the caller's DEVICE buffers, enqueued on the given stream, nothing
+ * allocated, nothing waited for; SIM_ERR_ARG is found before anything is launched.  Matrices are row-major with rows `ld` elements apart
+ * and need only the alignment of their type (rows on 16-byte boundaries are faster).  A matrix without elements is no error: nothing
+ * is launched for it.
+ */
+
+/* relu(z) = max(z, 0), with slope 0 at 0;  gelu(z) = z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)));  silu(z) = z / (1 + e^-z).
+ * NaN stays NaN. */
+typedef enum { SIM_ACT_NONE = 0, SIM_ACT_RELU = 1, SIM_ACT_GELU = 2, SIM_ACT_SILU = 3 } sim_act;
+
+/*
+ * A kept matrix [rows][cols]: E4M3 codes in rows of 32 ceil(cols / 32) bytes (16-byte aligned; the tail of a row is zero) and scale bytes
+ * [rows][ceil(cols / 32)], one per block of 32 elements of a row: 2^(byte - 127), the smallest power of two, at least 2^-127, for
+ * which no magnitude of the block exceeds 448 times it.  Elements are rounded to nearest even; a block with an infinity or a NaN
+ * gets the byte 0xFF and reads as NaN.  The two calls give the sizes of the buffers (0 for sizes outside [1, 2^31]).
+ */
+int64_t sim_ckpt_codes_bytes(int64_t rows, int64_t cols);
+int64_t sim_ckpt_scales_bytes(int64_t rows, int64_t cols);
+
+/* x [rows][cols] (SIM_F32, SIM_BF16 or SIM_F16) into codes and scales. */
+sim_status sim_ckpt_write(const void* x, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, uint8_t* codes, uint8_t* scales, void* cuda_stream);
+
+/* out = act(the kept values), rounded once to SIM_F32, SIM_BF16 or SIM_F16 (infinity where one is beyond the type's range). */
+sim_status sim_ckpt_read(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t cols, sim_act act, sim_dtype type, void* out, int64_t ld, void* cuda_stream);
+
+/*
+ * dz = dy act'(z) for z kept in 8 bits, and db = the sums of dz over its rows (fp32 sums of what has not been rounded, in a fixed order,
+ * rounded once to db_type).  db may be NULL; with codes, scales and dz NULL, db is the sums of dy.  dz has dy's type and may
+ * be dy itself with the same rows.  db needs a workspace of sim_act_backward_workspace bytes (4-byte aligned).
+ */
+int64_t sim_act_backward_workspace(int64_t rows, int64_t cols);
+sim_status sim_act_backward(const void* dy, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, const uint8_t* codes, const uint8_t* scales, sim_act act, void* dz, int64_t lddz,
+                            void* db, sim_dtype db_type, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * c [M][N] = act(a b^T + bias) + residual, or with act_grad  c = (a b^T) act'(z) + residual.
+ *   a, b      a is [M][K], or with a_t [K][M]; b is [N][K], or with b_t [K][N]; both SIM_BF16 or both SIM_F16, fp32 accumulation on the tensor
+ *             cores; K = 0 gives sums of nothing (a and b are not read)
+ *   bias      [N] or NULL, SIM_F32 or of the operands' type; not with act_grad
+ *   z         a kept matrix [M][N]: without act_grad codes and scales may be NULL, else act's argument a b^T + bias is left there (from its fp32
+ *             value); with act_grad it is read
+ *   residual  [M][N] of c's type, or NULL; may be c itself with the same rows
+ *   c         SIM_F32, or the operands' type: one rounding at the end
+ * Nothing else may overlap c, z or the workspace.  M, N, K in [0, 2^30].  Operands whose rows do not start on 16-byte boundaries are copied
+ * into the workspace first (sim_matmul_workspace bytes, 0 for none; 256-byte aligned).  The same call gives the same bits every time.  A
+ * device-side wait that runs out leaves its part of c NaN.
+ * A layer with x [tokens][in] and w [out][in]: y from a = x, b = w.  From dy [tokens][out]: the gradient by x from a = dy, b = w, b_t (with
+ * act_grad also through the activation that gave x, whose argument was kept; the residual then is the gradient that reached x another
+ * way); the gradient by w from a = dy, a_t, b = x, b_t.
+ */
+typedef struct {
+  int64_t M, N, K;
+  sim_dtype type;
+  const void* a;
+  int64_t lda;
+  int32_t a_t;
+  const void* b;
+  int64_t ldb;
+  int32_t b_t;
+  const void* bias;
+  sim_dtype bias_type;
+  sim_act act;
+  int32_t act_grad;
+  uint8_t* z_codes;
+  uint8_t* z_scales;
+  const void* residual;
+  int64_t ldr;
+  void* c;
+  sim_dtype c_type;
+  int64_t ldc;
+} sim_product;
+int64_t sim_matmul_workspace(const sim_product* p);
+sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Log probabilities, entropies, likeliest alternatives and gradients of logits [rows][vocab] (SIM_F32, SIM_BF16 or SIM_F16), l = logits / temperature:
+ *   lse[r] = log sum_v exp l[r][v],  logp[r] = l[r][tokens[r]] - lse[r],  entropy[r] = -sum_v p log p,  p = exp(l - lse)
+ *   top_ids, top_logp [rows][top]: the `top` largest logits in falling order, the lower index first among equals (NaN above all numbers)
+ *   d_logits[r][v] = (d_logp[r] ([v = token] - p[v]) - d_entropy[r] p[v] (log p[v] + entropy[r])) / temperature: the gradient of a loss whose
+ *                    derivatives by logp and entropy are d_logp and d_entropy (either may be NULL: zero)
+ * Any result may be NULL; a call for d_logits alone is the backward pass.  tokens: 4- or 8-byte integers; a negative one is no token (logp 0,
+ * no gradient by it), one of at least vocab makes logp and the row's gradient NaN.  A logit of -inf has probability 0; a row
+ * of nothing else has lse and every log probability -inf, entropy 0 and gradient 0.  A row with a NaN or +inf is NaN.  A logit over 2^126 temperature
+ * counts as infinite.  d_logits may be logits itself with the same rows.  vocab in [1, 2^30], rows up to 2^27, top up to 32, temperature in [0.001, 1000].
+ * Sums are fp32, in a fixed order: the same bits every time.
+ */
+sim_status sim_log_probs(const void* logits, sim_dtype type, int64_t rows, int64_t vocab, int64_t ld, const void* tokens, int32_t token_bytes, float temperature, int32_t top,
+                         float* logp, float* entropy, float* lse, int32_t* top_ids, float* top_logp, const float* d_logp, const float* d_entropy, void* d_logits, int64_t ldd,
+                         void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,7 @@ library's CUDA kernels.  Importing this module loads ``libstraggler_sim.so`` and
 has not been built - there is no CPU path behind these calls."""
 from __future__ import annotations
 
+import collections
 import contextlib
 import ctypes as C
 import os
@@ -25,9 +26,12 @@ EXPORTS = ["sim_create", "sim_set_params", "sim_set_adasync", "sim_set_adasync_l
            "sim_get_risk_trace", "sim_risk_curve", "sim_risk_envelope", "sim_selftest_wait_timeout", "sim_n_params", "sim_last_error",
            "sim_destroy", "sim_draw_delays", "sim_draw_indices", "sim_simulate_host", "sim_sweep_host", "sim_schedule_noalloc",
            "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy",
-           "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul", "sim_set_adamw", "sim_eval_loss_mxfp4"]
+           "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul", "sim_set_adamw", "sim_eval_loss_mxfp4",
+           "sim_ckpt_codes_bytes", "sim_ckpt_scales_bytes", "sim_ckpt_write", "sim_ckpt_read", "sim_act_backward_workspace", "sim_act_backward",
+           "sim_matmul_workspace", "sim_matmul", "sim_log_probs"]
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # SIM_F32, SIM_BF16, SIM_F16
 MXFP4 = 3
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 class SimProblem(C.Structure):
@@ -44,6 +48,13 @@ class SimAdamwTensor(C.Structure):
     _fields_ = [("n", C.c_int64), ("p_type", C.c_int), ("g_type", C.c_int), ("p", C.c_void_p), ("g", C.POINTER(C.c_void_p)),
                 ("g_scale", C.POINTER(C.c_void_p)), ("m", C.c_void_p), ("v", C.c_void_p), ("m_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("shadow", C.c_void_p), ("weight_decay", C.c_float)]
+
+
+class SimProduct(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("type", C.c_int), ("a", C.c_void_p), ("lda", C.c_int64), ("a_t", C.c_int32),
+                ("b", C.c_void_p), ("ldb", C.c_int64), ("b_t", C.c_int32), ("bias", C.c_void_p), ("bias_type", C.c_int), ("act", C.c_int),
+                ("act_grad", C.c_int32), ("z_codes", C.c_void_p), ("z_scales", C.c_void_p), ("residual", C.c_void_p), ("ldr", C.c_int64),
+                ("c", C.c_void_p), ("c_type", C.c_int), ("ldc", C.c_int64)]
 
 
 class SimError(RuntimeError):
@@ -104,10 +115,21 @@ def _load():
     L.sim_mx_quantize.argtypes = [vp, C.c_int, i64, i64, i64, i32, i32, u64, vp, vp, vp, vp, vp]
     L.sim_mx_dequantize.argtypes = [vp, vp, i64, i64, i32, C.c_int, vp, i64, vp]
     L.sim_mx_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, C.c_int, vp, i64, vp]
+    L.sim_ckpt_codes_bytes.argtypes = [i64, i64]
+    L.sim_ckpt_scales_bytes.argtypes = [i64, i64]
+    L.sim_ckpt_write.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, vp]
+    L.sim_ckpt_read.argtypes = [vp, vp, i64, i64, C.c_int, C.c_int, vp, i64, vp]
+    L.sim_act_backward_workspace.argtypes = [i64, i64]
+    L.sim_act_backward.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, C.c_int, vp, i64, vp, C.c_int, vp, i64, vp]
+    L.sim_matmul_workspace.argtypes = [C.POINTER(SimProduct)]
+    L.sim_matmul.argtypes = [C.POINTER(SimProduct), vp, i64, vp]
+    L.sim_log_probs.argtypes = [vp, C.c_int, i64, i64, i64, vp, i32, C.c_float, i32] + [vp] * 8 + [i64, vp]
+    sizes = ("sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_ckpt_codes_bytes", "sim_ckpt_scales_bytes", "sim_act_backward_workspace", "sim_matmul_workspace")
     for name in EXPORTS:
-        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy", "sim_mx_codes_bytes", "sim_mx_scales_bytes"):
+        if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy") + sizes:
             getattr(L, name).restype = C.c_int
-    L.sim_mx_codes_bytes.restype = L.sim_mx_scales_bytes.restype = i64
+    for name in sizes:
+        getattr(L, name).restype = i64
     return L
 
 
@@ -662,3 +684,331 @@ def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
             _given(stream, a.device, out)
     _check(_on(a.device, stream, lib.sim_mx_matmul, a.codes_ptr, a.scales_ptr, b.codes_ptr, b.scales_ptr, a.rows, b.rows, a.cols, DTYPES[out.dtype], out.data_ptr(), ld))
     return out
+
+
+# ---- operators of a worker for models of language-model size --------------------------------------------------------------
+class Checkpoint:
+    """A matrix [rows, cols] kept in 8 bits: E4M3 codes in rows of 32 ceil(cols / 32) bytes and a power-of-two scale byte per block of 32
+    elements of a row, [rows, ceil(cols / 32)].  codes (16-byte aligned) and scales are flat uint8 tensors."""
+
+    __slots__ = ("rows", "cols", "device", "codes_ptr", "scales_ptr", "_codes", "_scales", "_buffer")
+
+    def __init__(self, codes, scales, rows, cols):
+        need_c, need_s = _ckpt_bytes(rows, cols)
+        for name, t, need in (("codes", codes, need_c), ("scales", scales, need_s)):
+            if t.dtype != torch.uint8 or not t.is_cuda or not t.is_contiguous() or t.numel() < need or t.device != codes.device:
+                raise ValueError("%s must be a contiguous CUDA uint8 tensor of at least %d bytes, on one device" % (name, need))
+        self._codes, self._scales, self._buffer = codes, scales, None
+        self.rows, self.cols, self.device = rows, cols, codes.device
+        self.codes_ptr, self.scales_ptr = codes.data_ptr(), scales.data_ptr()
+
+    @classmethod
+    def empty(cls, rows, cols, device):
+        """Uninitialised, codes and scales in one buffer that belongs to the device's current stream."""
+        self = cls.__new__(cls)
+        nc, ns = _ckpt_bytes(rows, cols)
+        self._buffer = buf = torch.empty_strided((nc + ns,), (1,), dtype=torch.uint8, device=device)
+        self._codes = self._scales = None
+        self.rows, self.cols, self.device = rows, cols, buf.device
+        self.codes_ptr = buf.data_ptr()
+        self.scales_ptr = self.codes_ptr + nc
+        return self
+
+    def record_stream(self, stream):
+        """As of a tensor: the memory is not given to others before what `stream` has been given so far is done."""
+        for t in (self._buffer,) if self._buffer is not None else (self._codes, self._scales):
+            t.record_stream(stream)
+
+    @property
+    def codes(self):
+        return self._buffer[:self.scales_ptr - self.codes_ptr] if self._codes is None else self._codes[:self.rows * (-(-self.cols // 32) * 32)]
+
+    @property
+    def scales(self):
+        return self._buffer[self.scales_ptr - self.codes_ptr:] if self._scales is None else self._scales[:self.rows * -(-self.cols // 32)]
+
+
+def _ckpt_bytes(rows, cols):
+    """Bytes of codes and of scales, as sim_ckpt_codes_bytes and sim_ckpt_scales_bytes give them."""
+    blocks = -(-cols // 32)
+    return rows * 32 * blocks, rows * blocks
+
+
+def _act_code(name):
+    if name not in ACTS:
+        raise ValueError("an activation is one of %s" % ", ".join(ACTS))
+    return ACTS[name]
+
+
+def _plain(x, what, dtypes=tuple(DTYPES)):
+    """A CUDA matrix (or vector: one row), possibly without elements, neighbours along the last dimension -> (rows, cols, elements between rows)."""
+    if not torch.is_tensor(x) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
+        raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, " or ".join(str(d)[6:] for d in dtypes)))
+    rows, cols = (1, x.shape[0]) if x.dim() == 1 else x.shape
+    if x.numel() and ((cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(0) < cols)):
+        raise ValueError("%s must have neighbouring elements along its last dimension and rows that do not overlap" % what)
+    return rows, cols, x.stride(0) if rows > 1 and x.numel() else cols
+
+
+def _same(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError("%s must be on %s" % (name, device))
+
+
+def _result(out, rows, cols, dtypes, device, stream, what="out"):
+    """(out or a new matrix of the first of dtypes, its row distance)"""
+    if out is None:
+        return _empty(rows, cols, dtypes[0], device, stream), cols
+    r, c, ld = _plain(out, what, dtypes)
+    if (r, c) != (rows, cols) or out.device != device:
+        raise ValueError("%s must be [%d, %d] on %s" % (what, rows, cols, device))
+    if stream is not None:
+        _given(stream, device, out)
+    return out, ld
+
+
+def checkpoint(x, *, stream=None):
+    """The 8-bit form of a matrix (or vector: one row) of float32, bfloat16 or float16."""
+    rows, cols, ld = _plain(x, "x")
+    with _NO_STREAM if stream is None else _given(stream, x.device, x):
+        q = Checkpoint.empty(rows, cols, x.device)
+    _check(_on(x.device, stream, lib.sim_ckpt_write, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, q.codes_ptr, q.scales_ptr))
+    return q
+
+
+def checkpoint_read(q, dtype=torch.bfloat16, *, act="none", out=None, stream=None):
+    """act of the values of a Checkpoint as a matrix [rows, cols] of dtype (float32, bfloat16, float16), or into `out`."""
+    code = _act_code(act)
+    if out is None and dtype not in DTYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    if stream is not None:
+        _given(stream, q.device, q)
+    out, ld = _result(out, q.rows, q.cols, (dtype,) if out is None else tuple(DTYPES), q.device, stream)
+    _check(_on(q.device, stream, lib.sim_ckpt_read, q.codes_ptr, q.scales_ptr, q.rows, q.cols, code, DTYPES[out.dtype], out.data_ptr(), ld))
+    return out
+
+
+def _scratch(nbytes, device, stream):
+    """Room that a call uses until it is done (None for none)."""
+    if nbytes == 0:
+        return None
+    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+        return torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
+
+
+def _sums(dy, rows, cols, ld, z, code, dz, lddz, db, device, stream):
+    room = lib.sim_act_backward_workspace(rows, cols) if db is not None else 0
+    ws = _scratch(room, device, stream)
+    _check(_on(device, stream, lib.sim_act_backward, dy.data_ptr(), DTYPES[dy.dtype], rows, cols, ld, z and z.codes_ptr, z and z.scales_ptr, code,
+               None if dz is None else dz.data_ptr(), lddz, None if db is None else db.data_ptr(), 0 if db is None else DTYPES[db.dtype],
+               None if ws is None else ws.data_ptr(), room))
+
+
+def _vector(out, n, dtypes, device, stream, what):
+    if out is None:
+        return _empty(1, n, dtypes[0], device, stream)[0]
+    if not out.is_cuda or out.device != device or out.dtype not in dtypes or out.dim() != 1 or out.numel() != n or not out.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d on %s" % (what, n, device))
+    if stream is not None:
+        _given(stream, device, out)
+    return out
+
+
+def act_backward(dy, z, act, *, bias=True, dtype=torch.float32, out=None, stream=None):
+    """(dz, db): dz = dy act'(z) in dy's type for a Checkpoint z of an activation's argument, db its sums over the rows (of dz before it is
+    rounded) as a vector of dtype, or None without `bias`.  out: (dz, db) to write into, either may be None; dz may be dy."""
+    code = _act_code(act)
+    rows, cols, ld = _plain(dy, "dy")
+    device = dy.device
+    if not isinstance(z, Checkpoint) or (z.rows, z.cols) != (rows, cols) or z.device != device:
+        raise ValueError("z must be a Checkpoint [%d, %d] on %s" % (rows, cols, device))
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be float32, bfloat16 or float16")
+    if stream is not None:
+        _given(stream, device, dy, z)
+    dz, db = out or (None, None)
+    dz, lddz = _result(dz, rows, cols, (dy.dtype,), device, stream, "dz")
+    db = _vector(db, cols, (dtype,) if db is None else tuple(DTYPES), device, stream, "db") if bias else None
+    _sums(dy, rows, cols, ld, z, code, dz, lddz, db, device, stream)
+    return dz, db
+
+
+_HALF = (torch.bfloat16, torch.float16)
+
+
+def _side(x, what, dtype=None):
+    """An operand of a product, its rows along either dimension -> (rows, cols, elements between its rows in memory, whether those lie along the
+    first dimension's neighbours)."""
+    if not torch.is_tensor(x) or not x.is_cuda or x.dim() not in (1, 2) or x.dtype not in ((dtype,) if dtype else _HALF):
+        raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, str(dtype)[6:] if dtype else "bfloat16 or float16"))
+    rows, cols = (1, x.shape[0]) if x.dim() == 1 else x.shape
+    if x.numel() == 0 or ((cols == 1 or x.stride(-1) == 1) and (rows == 1 or x.stride(0) >= cols)):
+        return rows, cols, x.stride(0) if rows > 1 and x.numel() else cols, False
+    if x.dim() == 2 and (rows == 1 or x.stride(0) == 1) and x.stride(1) >= rows:
+        return rows, cols, x.stride(1), True
+    raise ValueError("%s must have neighbouring elements along one dimension, and the others must not overlap" % what)
+
+
+def _product(device, stream, M, N, K, dtype, a, lda, a_t, b, ldb, b_t, c, ldc, *, bias=None, act=0, act_grad=False, z=None, residual=None, ldr=0):
+    p = SimProduct(M, N, K, DTYPES[dtype], a, lda, a_t, b, ldb, b_t, None, 0, act, act_grad, None, None, None, 0, c.data_ptr(), DTYPES[c.dtype], ldc)
+    if bias is not None:
+        p.bias, p.bias_type = bias.data_ptr(), DTYPES[bias.dtype]
+    if z is not None:
+        p.z_codes, p.z_scales = z.codes_ptr, z.scales_ptr
+    if residual is not None:
+        p.residual, p.ldr = residual.data_ptr(), ldr
+    # rows on 16-byte boundaries need no room; the library is asked for the rest
+    room = 0 if (a | b | (lda | ldb) * 2) & 15 == 0 else lib.sim_matmul_workspace(C.byref(p))
+    ws = _scratch(room, device, stream)
+    _check(_on(device, stream, lib.sim_matmul, C.byref(p), None if ws is None else ws.data_ptr(), room))
+
+
+def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None, out=None, stream=None):
+    """act(x w^T + bias) + residual as [tokens, out] for x [tokens, in] (or one token: [in]) and w [out, in], both bfloat16 or both float16, with
+    either of their dimensions in memory's order.  bias [out]: float32 or the operands' type.  The result (dtype, or `out`) has the
+    operands' type or float32, and so has the residual.  keep: (result, Checkpoint of x w^T + bias), for the backward pass."""
+    code = _act_code(act)
+    M, K, lda, a_t = _side(x, "x")
+    N, Kw, ldb, b_t = _side(w, "w", x.dtype)
+    device = x.device
+    if K != Kw:
+        raise ValueError("x and w must have as many columns")
+    kinds = (x.dtype, torch.float32)
+    if (out.dtype if out is not None else dtype or x.dtype) not in kinds:
+        raise ValueError("the result is float32 or of the operands' type")
+    _same(device, w=w, bias=bias, residual=residual)
+    if bias is not None and (bias.dtype not in kinds or bias.dim() != 1 or bias.numel() != N or (N > 1 and bias.stride(0) != 1)):
+        raise ValueError("bias must be a contiguous vector of %d of float32 or the operands' type" % N)
+    if stream is not None:
+        _given(stream, device, *(t for t in (x, w, bias, residual) if t is not None))
+    out, ldc = _result(out, M, N, (dtype or x.dtype,) if out is None else kinds, device, stream)
+    ldr = 0
+    if residual is not None:
+        r, c, ldr = _plain(residual, "residual", (out.dtype,))
+        if (r, c) != (M, N):
+            raise ValueError("residual must be [%d, %d]" % (M, N))
+    z = None
+    if keep:
+        with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+            z = Checkpoint.empty(M, N, device)
+    _product(device, stream, M, N, K, x.dtype, x.data_ptr(), lda, a_t, w.data_ptr(), ldb, b_t, out, ldc, bias=bias, act=code, z=z, residual=residual, ldr=ldr)
+    return (out, z) if keep else out
+
+
+def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=torch.float32, out=None, stream=None):
+    """(dx, dw, db) of linear(x, w, bias) from dy [tokens, out], w [out, in] and x: the tensor [tokens, in] itself, or a Checkpoint.  With a
+    Checkpoint v the layer's input was x_act(v) and is taken as x_act of the kept values, rounded to dy's type; dx is then the gradient by v,
+    (dy w) x_act'(v).  residual [tokens, in]: added to dx (the gradient that reached the input another way).  dx has dy's type, dw [out, in]
+    and db [out] have dtype (float32 or dy's).  need: which of them ("x", "w", "b"); the others are None.  out: (dx, dw, db) to write
+    into, each may be None."""
+    code = _act_code(x_act)
+    M, N, lda, a_t = _side(dy, "dy")
+    Nw, K, ldb, b_t = _side(w, "w", dy.dtype)
+    device = dy.device
+    kept = isinstance(x, Checkpoint)
+    if kept:
+        Mx, Kx = x.rows, x.cols
+    else:
+        Mx, Kx, ldx, x_t = _side(x, "x", dy.dtype)
+        if code:
+            raise ValueError("x_act belongs to a Checkpoint: a tensor x is the layer's input itself")
+    if Nw != N or Mx != M or Kx != K or x.device != device:
+        raise ValueError("dy [%d, %d], w [%d, %d] and x [%d, %d] do not belong together, or are on several devices" % (M, N, Nw, K, Mx, Kx))
+    _same(device, w=w, residual=residual)
+    kinds = (dy.dtype, torch.float32)
+    if dtype not in kinds or not need or any(n not in "xwb" for n in need):
+        raise ValueError("dtype is float32 or dy's, need is made of x, w and b")
+    if stream is not None:
+        _given(stream, device, *(t for t in (dy, x, w, residual) if t is not None))
+    dx, dw, db = out or (None, None, None)
+    if "x" in need:
+        dx, ldc = _result(dx, M, K, (dy.dtype,), device, stream, "dx")
+        ldr = 0
+        if residual is not None:
+            r, c, ldr = _plain(residual, "residual", (dy.dtype,))
+            if (r, c) != (M, K):
+                raise ValueError("residual must be [%d, %d]" % (M, K))
+        grad = kept and code != 0
+        _product(device, stream, M, K, N, dy.dtype, dy.data_ptr(), lda, a_t, w.data_ptr(), ldb, not b_t, dx, ldc, act=code if grad else 0, act_grad=grad,
+                 z=x if grad else None, residual=residual, ldr=ldr)
+    if "w" in need:
+        dw, ldc = _result(dw, N, K, (dtype,) if dw is None else kinds, device, stream, "dw")
+        if kept:
+            # rows of whole 16-byte pieces, as the product wants them
+            with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+                h = torch.empty_strided((M, K), (-(-K // 8) * 8, 1), dtype=dy.dtype, device=device)
+            ldx, x_t = h.stride(0), False
+            _check(_on(device, stream, lib.sim_ckpt_read, x.codes_ptr, x.scales_ptr, M, K, code, DTYPES[dy.dtype], h.data_ptr(), ldx))
+        else:
+            h = x
+        _product(device, stream, N, K, M, dy.dtype, dy.data_ptr(), lda, not a_t, h.data_ptr(), ldx, not x_t, dw, ldc)
+    if "b" in need:
+        db = _vector(db, N, (dtype,) if db is None else tuple(DTYPES), device, stream, "db")
+        if a_t:
+            raise ValueError("db needs dy with neighbouring elements along its last dimension")
+        _sums(dy, M, N, lda, None, 0, None, 0, db, device, stream)
+    return dx if "x" in need else None, dw if "w" in need else None, db if "b" in need else None
+
+
+LogProbs = collections.namedtuple("LogProbs", "logp entropy lse top_ids top_logp dlogits")
+
+
+def log_probs(logits, tokens=None, *, top=0, temperature=1.0, d_logp=None, d_entropy=None, out=None, stream=None):
+    """Of logits [rows, vocab] (float32, bfloat16, float16; one row: [vocab]) divided by temperature: a LogProbs with float32 vectors logp (of tokens
+    [rows], int64 or int32; 0 where a token is negative; None without tokens), entropy and lse, and for top > 0 the `top` likeliest
+    alternatives of each row: top_ids int32 and top_logp float32 [rows, top], the lower index first among equals.  With d_logp or
+    d_entropy (float32 [rows]: the derivatives of a loss by logp and entropy) also dlogits, the loss' gradient by the logits in their type,
+    in `out` where given (which may be logits itself)."""
+    rows, vocab, ld, device, tb = _logits(logits, tokens, d_logp, d_entropy)
+    grad = d_logp is not None or d_entropy is not None
+    if out is not None and not grad:
+        raise ValueError("out takes the gradient, which needs d_logp or d_entropy")
+    if stream is not None:
+        _given(stream, device, *(t for t in (logits, tokens, d_logp, d_entropy) if t is not None))
+    if vocab == 0 or not 0 <= top <= min(32, vocab):
+        raise ValueError("vocab must be at least 1 and top in [0, min(32, vocab)]")
+    d, ldd = _result(out, rows, vocab, (logits.dtype,), device, stream) if grad else (None, 0)
+    # one buffer for all vectors: entropy, lse, logp, then the alternatives
+    n = (3 if tokens is not None else 2) + 2 * top
+    buf = _empty(n, rows, torch.float32, device, stream)
+    base, size = buf.data_ptr(), 4 * rows
+    lp = base + 2 * size if tokens is not None else None
+    ti = base + (n - 2 * top) * size if top else None
+    tl = base + (n - top) * size if top else None
+    _check(_on(device, stream, lib.sim_log_probs, logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, ld, None if tokens is None else tokens.data_ptr(), tb,
+               temperature, top, lp, base, base + size, ti, tl, None if d_logp is None else d_logp.data_ptr(), None if d_entropy is None else d_entropy.data_ptr(),
+               None if d is None else d.data_ptr(), ldd))
+    if logits.dim() == 1 and out is None and d is not None:
+        d = d[0]
+    ids = logs = None
+    if top:
+        ids, logs = buf[n - 2 * top: n - top].view(torch.int32).view(rows, top), buf[n - top:].view(rows, top)
+    return LogProbs(buf[2] if tokens is not None else None, buf[0], buf[1], ids, logs, d)
+
+
+def log_probs_backward(logits, tokens, d_logp=None, d_entropy=None, *, temperature=1.0, out=None, stream=None):
+    """The gradient by the logits of a loss whose derivatives by logp and entropy are only known after the forward pass (log_probs)."""
+    if d_logp is None and d_entropy is None:
+        raise ValueError("d_logp or d_entropy is required")
+    rows, vocab, ld, device, tb = _logits(logits, tokens, d_logp, d_entropy)
+    if stream is not None:
+        _given(stream, device, *(t for t in (logits, tokens, d_logp, d_entropy) if t is not None))
+    d, ldd = _result(out, rows, vocab, (logits.dtype,), device, stream)
+    _check(_on(device, stream, lib.sim_log_probs, logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, ld, None if tokens is None else tokens.data_ptr(), tb,
+               temperature, 0, None, None, None, None, None, None if d_logp is None else d_logp.data_ptr(), None if d_entropy is None else d_entropy.data_ptr(), d.data_ptr(), ldd))
+    return d[0] if logits.dim() == 1 and out is None else d
+
+
+def _logits(logits, tokens, d_logp, d_entropy):
+    rows, vocab, ld = _plain(logits, "logits")
+    device = logits.device
+    if tokens is not None and (not torch.is_tensor(tokens) or tokens.device != device or tokens.dtype not in (torch.int64, torch.int32) or tokens.numel() != rows or
+                               not tokens.is_contiguous()):
+        raise ValueError("tokens must be a contiguous int64 or int32 tensor of %d elements on %s" % (rows, device))
+    for name, t in (("d_logp", d_logp), ("d_entropy", d_entropy)):
+        if t is not None and (not torch.is_tensor(t) or t.device != device or t.dtype != torch.float32 or t.numel() != rows or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous float32 tensor of %d elements on %s" % (name, rows, device))
+    if d_logp is not None and tokens is None:
+        raise ValueError("d_logp needs tokens")
+    return rows, vocab, ld, device, 0 if tokens is None else tokens.element_size()

@@ -1,0 +1,464 @@
+// Log probabilities of given tokens, entropies, the likeliest alternatives, and the gradient by the logits, at vocabulary size.
+//
+// With l = x / T and c = log2(e) / T everything is taken in powers of two: d = c x - m for a whole number m near the largest c x,
+//   s = sum 2^d,  q = sum 2^d d,   lse = (m + log2 s) ln 2,  log p = (d - log2 s) ln 2,  H = (log2 s - q / s) ln 2,
+// one pass over the row with running m, s, q a thread.  m being whole, moving it scales s and q exactly, and a thread moves it only
+// when a logit is over 2^8 times (in 2^d) beyond it, so the rescaling's exponential is rare.  s and q are fp32: a thread adds at most
+// vocab / threads terms, then the threads meet in a tree.  m is kept in quarters, m4 = m / 4: a row of nothing but the lowest fp32
+// number would overflow as c x.
+//
+// The gradient by x_v is (g (1[v = token] - p_v) - h p_v (log p_v + H)) / T: a second look at the row, which L2 still holds.
+//
+// The `top` largest logits: the first pass leaves each thread's largest one; the top-th of those is a bound that at least `top`
+// logits reach, and every logit that reaches it lies in a thread's share that does.  Those few shares are looked through
+// again, a warp a share, and what reaches the bound is ranked by counting, the lower index first among equals.  Where more reach it than the
+// list takes (rows of equal logits), the largest is taken `top` times, each time only the share that gave it searched again.
+//
+// Floor: HBM, the row read once (and the gradient written once).
+#pragma once
+#include "lowbits.cuh"
+#include "ptx_util.cuh"
+
+namespace ssim {
+
+constexpr int LP_MAX_TOP = 32;
+constexpr int LP_LIST = 1024;               // logits that may reach the bound
+constexpr float LP_LN2 = 0.6931471805599453f;
+constexpr float LP_NONE = -200.f;           // 2^-200 is zero
+
+struct LogpArgs {
+  const void* x;
+  long long rows, vocab, ld;
+  const void* tokens;                       // or null
+  int token64;
+  float c, c4, inv_t;                       // log2(e) / T, a quarter of it, 1 / T
+  int top;
+  float *logp, *entropy, *lse, *top_logp;   // any may be null
+  int* top_ids;
+  const float *d_logp, *d_entropy;          // may be null: zero
+  void* out;                                // gradient, or null
+  long long ldo;
+};
+
+__device__ __forceinline__ float exp2_fast(float d) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
+__device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
+__device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
+
+// Whole numbers in the order of the logits, NaN above all, both zeros alike; 0 is none and so is 2^32 - 1.  Back: the logit.
+__device__ __forceinline__ uint32_t logit_key(float x) {
+  const uint32_t b = __float_as_uint(x + 0.f);
+  return x != x ? 0xFFFFFFFEu : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float logit_of_key(uint32_t k) {
+  return k > 0xFF800000u ? quiet_nan() : __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k);
+}
+// bits of a key that are the same for all values of one sign of a type
+template <int T> struct KeyShift { static constexpr int value = T == T_BF16 ? 16 : T == T_F16 ? 13 : 0; };
+
+// Running reference and sums of some logits
+struct LogSum {
+  float m4 = neg_inf(), s = 0.f, q = 0.f;
+  __device__ __forceinline__ bool far() const { return fabsf(m4) > 1048576.f && m4 != neg_inf(); }    // c x may overflow
+  __device__ __forceinline__ void move(float to4) {          // to a reference to4 >= m4
+    const float by = 4.f * (to4 - m4);
+    if (by < 250.f) {
+      const float f = exp2_fast(-by);
+      q = (q - by * s) * f;
+      s *= f;
+    } else if (by >= 250.f) {
+      s = s == s ? 0.f : s;                                  // a NaN stays
+      q = s;
+    }
+    m4 = to4;
+  }
+  __device__ __forceinline__ void reach(float most, float c4) {
+    const float top4 = __fmul_rn(most, c4);
+    if (top4 > m4 + 2.f) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4);
+  }
+  __device__ __forceinline__ float off() const { return m4 == neg_inf() ? 0.f : -4.f * m4; }
+  __device__ __forceinline__ float dist(float x, float c, float c4) const {
+    if (m4 == neg_inf()) return x;
+    return far() ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, -4.f * m4);
+  }
+  __device__ __forceinline__ void add(float d) {             // d >= LP_NONE or NaN
+    const float e = exp2_fast(d);
+    s += e;
+    q = fmaf(e, d, q);
+  }
+  template <int N>
+  __device__ __forceinline__ float take(const float (&x)[N], float c, float c4) {
+    float most = x[0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) most = max_nan(most, x[e]);
+    reach(most, c4);
+    if (!far()) {
+      const float o = off();
+#pragma unroll
+      for (int e = 0; e < N; ++e) add(max_nan(fmaf(x[e], c, o), LP_NONE));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) add(max_nan(4.f * (__fmul_rn(x[e], c4) - m4), LP_NONE));   // equal logits differ by nothing
+    }
+    return most;
+  }
+  __device__ __forceinline__ void join(float om4, float os, float oq) {
+    LogSum o;
+    o.m4 = om4; o.s = os; o.q = oq;
+    const float to = fmaxf(m4, om4);
+    if (m4 != to) move(to);
+    if (o.m4 != to) o.move(to);
+    s += o.s; q += o.q;
+  }
+  template <int G>
+  __device__ __forceinline__ void join_lanes() {             // over groups of G lanes, the same in each
+#pragma unroll
+    for (int k = G / 2; k > 0; k >>= 1) {
+      const float om = __shfl_xor_sync(0xFFFFFFFFu, m4, k), os = __shfl_xor_sync(0xFFFFFFFFu, s, k), oq = __shfl_xor_sync(0xFFFFFFFFu, q, k);
+      join(om, os, oq);
+    }
+  }
+};
+
+// What a row's sums say
+struct LogRow {
+  LogSum t;
+  float l2;                                 // log2 s
+  bool none;                                // nothing but -inf
+  __device__ __forceinline__ explicit LogRow(const LogSum& sum) : t(sum), l2(log2f(sum.s)), none(sum.s == 0.f) {}
+  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far() ? (l2 == l2 ? t.m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, t.m4, l2) * LP_LN2; }
+  __device__ __forceinline__ float logp(float x, float c, float c4) const {
+    if (none) return neg_inf();
+    if (!(fabsf(x) < 1e30f)) return (__fmul_rn(x, c4) - t.m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
+    const float lp = (t.dist(x, c, c4) - l2) * LP_LN2;
+    return lp > 0.f ? 0.f : lp;                              // by rounding only
+  }
+  __device__ __forceinline__ float entropy() const {
+    const float h = (l2 - t.q / t.s) * LP_LN2;
+    return none || h < 0.f ? 0.f : h;
+  }
+};
+
+// The gradient by a logit: p (a lp + b), lp = log2 p; at the token plus g / T
+struct LogGrad {
+  float c, c4, o, m4, l2, a, b, g;
+  bool far, none;
+  __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow& r, float g_, float h) {
+    c = k.c; c4 = k.c4; m4 = r.t.m4; l2 = r.l2; far = r.t.far(); none = r.none;
+    o = -fmaf(4.f, m4, l2);
+    a = -h * LP_LN2 * k.inv_t;
+    b = -(g_ + h * r.entropy()) * k.inv_t;
+    g = none ? 0.f : g_ * k.inv_t;
+  }
+  __device__ __forceinline__ float at(float x) const {
+    if (none) return 0.f;
+    const float lp = max_nan(far ? 4.f * (__fmul_rn(x, c4) - m4) - l2 : fmaf(x, c, o), LP_NONE);
+    return exp2_fast(lp) * fmaf(a, lp, b);
+  }
+};
+
+__device__ __forceinline__ long long token_of(const LogpArgs& a, long long row) {
+  if (!a.tokens) return -1;
+  return a.token64 ? static_cast<const long long*>(a.tokens)[row] : (long long)static_cast<const int*>(a.tokens)[row];
+}
+__device__ __forceinline__ float token_weight(const LogpArgs& a, long long row, long long token) {   // derivative of the loss by logp
+  if (token < 0 || !a.d_logp) return 0.f;
+  return token < a.vocab ? a.d_logp[row] : quiet_nan();
+}
+template <int T>
+__device__ __forceinline__ void write_row(const LogpArgs& a, const LogRow& r, long long row, long long token) {
+  if (a.lse) a.lse[row] = r.lse();
+  if (a.entropy) a.entropy[row] = r.entropy();
+  if (a.logp) a.logp[row] = token < 0 ? 0.f : token >= a.vocab ? quiet_nan() : r.logp(Elem<T>::get(a.x, row * a.ld + token), a.c, a.c4);
+}
+
+// ---- short rows: G lanes a row, E logits a lane, in registers ---------------------------------------------------------------
+template <int T, int G, int E>
+__global__ void __launch_bounds__(128) logp_short_kernel(const __grid_constant__ LogpArgs a) {
+  const long long row = (long long)blockIdx.x * (128 / G) + threadIdx.x / G;
+  const int lane = threadIdx.x % G, vocab = (int)a.vocab;
+  const bool live = row < a.rows;
+  const long long base = live ? row * a.ld : 0;
+  float x[E];
+  LogSum t;
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = live && i * G + lane < vocab ? Elem<T>::get(a.x, base + i * G + lane) : neg_inf();
+  t.take(x, a.c, a.c4);
+  if (G > 1) t.join_lanes<G>();
+  const LogRow r(t);
+  const long long token = live ? token_of(a, row) : -1;
+  if (live && lane == 0) write_row<T>(a, r, row, token);
+  if (a.top) {
+    uint32_t key[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) key[i] = i * G + lane < vocab ? logit_key(x[i]) : 0u;
+    for (int k = 0; k < a.top; ++k) {
+      uint32_t best = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) best = max(best, key[i]);
+      uint32_t all = best;
+#pragma unroll
+      for (int o = G / 2; o > 0; o >>= 1) all = max(all, __shfl_xor_sync(0xFFFFFFFFu, all, o));
+      int id = 0x7FFFFFFF;
+#pragma unroll
+      for (int i = E - 1; i >= 0; --i)
+        if (key[i] == all && all != 0u) id = i * G + lane;
+#pragma unroll
+      for (int o = G / 2; o > 0; o >>= 1) id = min(id, __shfl_xor_sync(0xFFFFFFFFu, id, o));
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (i * G + lane == id) key[i] = 0u;
+      if (live && lane == 0) {
+        if (a.top_ids) a.top_ids[row * a.top + k] = id;
+        if (a.top_logp) a.top_logp[row * a.top + k] = r.logp(logit_of_key(all), a.c, a.c4);
+      }
+    }
+  }
+  __syncwarp();              // the token's logit has been read: the gradient may go over the logits
+  if (a.out && live) {
+    const LogGrad d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const int v = i * G + lane;
+      if (v < vocab) Elem<T>::put(a.out, row * a.ldo + v, d.at(x[i]) + (v == token ? d.g : 0.f));
+    }
+  }
+}
+
+// ---- long rows: a block a row, or a cluster of blocks with a slice each -----------------------------------------------------------
+// A slice: elements before the first 16-byte boundary, groups of eight from there, elements behind the last group
+template <int T>
+struct Slice {
+  static constexpr int EB = Elem<T>::bytes;
+  const char* at;
+  int n, head, groups, tail;                // a slice has less than 2^31 elements
+  __device__ __forceinline__ Slice(const void* x, long long first, int n_) : at(static_cast<const char*>(x) + first * EB), n(n_) {
+    head = min(n, (int)((-(intptr_t)at) & 15) / EB);
+    groups = (n - head) >> 3;
+    tail = n - head - 8 * groups;
+  }
+  __device__ __forceinline__ int index(int group) const { return head + 8 * group; }
+  __device__ __forceinline__ int tail_index() const { return head + 8 * groups; }
+  __device__ __forceinline__ float one(int i) const { return Elem<T>::get(at, i); }
+  __device__ __forceinline__ void load(int group, Raw8<T>& r) const { r.load(at, index(group)); }
+};
+template <int T>
+__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = r.value(e);
+}
+
+// Calls f(index in the slice, logit) for the elements of thread t's share
+template <int T, int NT, typename F>
+__device__ __forceinline__ void each_of_share(const Slice<T>& sl, int t, F f) {
+  if (t < sl.head) f(t, sl.one(t));
+  for (int g = t; g < sl.groups; g += NT) {
+    Raw8<T> r;
+    sl.load(g, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f(sl.index(g) + e, r.value(e));
+  }
+  if (t < sl.tail) f(sl.tail_index() + t, sl.one(sl.tail_index() + t));
+}
+
+template <int NT>
+struct LogpShared {
+  float m4[NT / 32], s[NT / 32], q[NT / 32];
+  float row[4];                                      // the block's own sums, for the others of the cluster
+  unsigned long long list[LP_LIST], best[LP_MAX_TOP], pick[NT / 32];
+  int share[NT], shares, listed;
+};
+
+__device__ __forceinline__ unsigned long long rank_word(uint32_t key, uint32_t index) { return (unsigned long long)key << 32 | (0xFFFFFFFFu - index); }
+
+// words [n] in shared memory, all different where not zero -> the first `top` in falling order (zeros where there are fewer)
+template <int NT>
+__device__ __forceinline__ void rank_words(const unsigned long long* words, int n, int top, unsigned long long* best) {
+  if ((int)threadIdx.x < top) best[threadIdx.x] = 0ull;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += NT) {
+    const unsigned long long w = words[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += words[j] > w ? 1 : 0;
+    if (w && above < top) best[above] = w;
+  }
+  __syncthreads();
+}
+
+template <int T, int NT>
+__device__ __noinline__ void top_of_slice(LogpShared<NT>& sh, const Slice<T>& sl, uint32_t first, int top, uint32_t kmax) {
+  constexpr int SHIFT = KeyShift<T>::value;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid == 0) sh.shares = sh.listed = 0;
+  uint32_t bound = 0;
+  for (int bit = 31 - SHIFT; bit >= 0; --bit) {
+    const uint32_t trial = bound | 1u << bit;
+    if (__syncthreads_count((kmax >> SHIFT) >= trial) >= top) bound = trial;
+  }
+  if (kmax != 0u && (kmax >> SHIFT) >= bound) sh.share[atomicAdd(&sh.shares, 1)] = tid;
+  __syncthreads();
+  auto list = [&](int i, float x) {
+    const uint32_t key = logit_key(x);
+    if ((key >> SHIFT) >= bound) {
+      const int at = atomicAdd(&sh.listed, 1);
+      if (at < LP_LIST) sh.list[at] = rank_word(key, first + (uint32_t)i);
+    }
+  };
+  for (int k = warp; k < sh.shares; k += NT / 32) {
+    const int t = sh.share[k];
+    if (lane == 0 && t < sl.head) list(t, sl.one(t));
+    if (lane == 1 && t < sl.tail) list(sl.tail_index() + t, sl.one(sl.tail_index() + t));
+    for (int g = t + lane * NT; g < sl.groups; g += 32 * NT) {
+      Raw8<T> r;
+      sl.load(g, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) list(sl.index(g) + e, r.value(e));
+    }
+  }
+  __syncthreads();
+  if (sh.listed <= LP_LIST) {
+    rank_words<NT>(sh.list, sh.listed, top, sh.best);
+    return;
+  }
+  // the largest, `top` times
+  unsigned long long mine = 0, under = ~0ull;
+  auto look = [&](int i, float x) {
+    const unsigned long long w = rank_word(logit_key(x), first + (uint32_t)i);
+    if (w < under && w > mine) mine = w;
+  };
+  each_of_share<T, NT>(sl, tid, look);
+  for (int k = 0; k < top; ++k) {
+    unsigned long long w = mine;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, w, o);
+      w = other > w ? other : w;
+    }
+    if (lane == 0) sh.pick[warp] = w;
+    __syncthreads();
+    w = sh.pick[0];
+    for (int j = 1; j < NT / 32; ++j) w = sh.pick[j] > w ? sh.pick[j] : w;
+    if (tid == 0) sh.best[k] = w;
+    if (w && mine == w) {
+      under = w;
+      mine = 0;
+      each_of_share<T, NT>(sl, tid, look);
+    }
+    __syncthreads();
+  }
+}
+
+template <int T, int NT>
+__global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ LogpArgs a, int slices, int slice_len) {
+  __shared__ LogpShared<NT> sh;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long row = blockIdx.x / (unsigned)slices;
+  const int part = (int)(blockIdx.x % (unsigned)slices);               // = the rank in the cluster
+  const long long first = (long long)part * slice_len;
+  const Slice<T> sl(a.x, row * a.ld + first, (int)max(0ll, min((long long)slice_len, a.vocab - first)));
+
+  LogSum t;
+  uint32_t kmax = 0;
+  auto some = [&](const float (&x)[8]) {
+    const float most = t.take(x, a.c, a.c4);
+    if (a.top) kmax = max(kmax, logit_key(most));
+  };
+  auto single = [&](float v) {
+    const float x[1] = {v};
+    t.take(x, a.c, a.c4);
+    if (a.top) kmax = max(kmax, logit_key(v));
+  };
+  if (tid < sl.head) single(sl.one(tid));
+  if (tid < sl.tail) single(sl.one(sl.tail_index() + tid));
+  constexpr int AHEAD = Elem<T>::bytes == 4 ? 2 : 4;                    // groups whose loads are in flight together
+  int g = tid;
+  for (; g + (AHEAD - 1) * NT < sl.groups; g += AHEAD * NT) {
+    Raw8<T> r[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) sl.load(g + k * NT, r[k]);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      float x[8];
+      unpack8<T>(r[k], x);
+      some(x);
+    }
+  }
+  for (; g < sl.groups; g += NT) {
+    Raw8<T> r;
+    sl.load(g, r);
+    float x[8];
+    unpack8<T>(r, x);
+    some(x);
+  }
+  t.join_lanes<32>();
+  if (lane == 0) { sh.m4[warp] = t.m4; sh.s[warp] = t.s; sh.q[warp] = t.q; }
+  __syncthreads();
+  t = LogSum();
+  for (int w = 0; w < NT / 32; ++w) t.join(sh.m4[w], sh.s[w], sh.q[w]);
+  if (a.top) top_of_slice<T, NT>(sh, sl, (uint32_t)first, a.top, kmax);
+  if (slices > 1) {
+    if (tid == 0) { sh.row[0] = t.m4; sh.row[1] = t.s; sh.row[2] = t.q; }
+    __syncthreads();
+    cluster_sync_all();
+    t = LogSum();
+    for (int k = 0; k < slices; ++k) {
+      const uint32_t from = cluster_addr(smem_addr(sh.row), (uint32_t)k);
+      t.join(ld_cluster1(from), ld_cluster1(from + 4), ld_cluster1(from + 8));
+    }
+    if (a.top && part == 0) {
+      for (int i = tid; i < slices * a.top; i += NT)
+        sh.list[i] = ld_cluster64(cluster_addr(smem_addr(sh.best + i % a.top), (uint32_t)(i / a.top)));
+      __syncthreads();
+    }
+    cluster_sync_all();                                                  // the others' sums and lists have been read
+    if (a.top && part == 0) rank_words<NT>(sh.list, slices * a.top, a.top, sh.best);
+  }
+  const LogRow r(t);
+  const long long token = token_of(a, row);
+  if (part == 0) {
+    if (tid == 0) write_row<T>(a, r, row, token);
+    if (tid < a.top) {
+      const unsigned long long w = sh.best[tid];
+      if (a.top_ids) a.top_ids[row * a.top + tid] = (int)(0xFFFFFFFFu - (uint32_t)w);
+      if (a.top_logp) a.top_logp[row * a.top + tid] = r.logp(logit_of_key((uint32_t)(w >> 32)), a.c, a.c4);
+    }
+  }
+  if (a.out) {
+    // The token's logit was read by thread 0 of the first slice, possibly of another block: where the gradient goes over the
+    // logits, nobody writes before that.
+    if (slices > 1) cluster_sync_all();
+    else __syncthreads();
+    const LogGrad d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
+    const long long tok = token - first;
+    char* out = static_cast<char*>(a.out) + (row * a.ldo + first) * Elem<T>::bytes;
+    const bool wide = ((reinterpret_cast<uintptr_t>(out) + sl.head * Elem<T>::bytes) & 15) == 0;
+    auto put = [&](int i, float x) { Elem<T>::put(out, i, d.at(x) + (i == tok ? d.g : 0.f)); };
+    if (tid < sl.head) put(tid, sl.one(tid));
+    if (tid < sl.tail) put(sl.tail_index() + tid, sl.one(sl.tail_index() + tid));
+    for (g = tid; g < sl.groups; g += AHEAD * NT) {
+      Raw8<T> raw[AHEAD];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k)
+        if (g + k * NT < sl.groups) sl.load(g + k * NT, raw[k]);
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        if (g + k * NT >= sl.groups) break;
+        const int at = sl.index(g + k * NT);
+        float x[8];
+        unpack8<T>(raw[k], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = d.at(x[e]);
+        if (tok >= at && tok < at + 8) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] += at + e == tok ? d.g : 0.f;
+        }
+        if (wide) Elem<T>::put8(out, at, x);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e) Elem<T>::put(out, at + e, x[e]);
+      }
+    }
+  }
+}
+
+}  // namespace ssim

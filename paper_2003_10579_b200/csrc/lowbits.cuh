@@ -201,6 +201,10 @@ template <> struct Elem<T_F16> {
 #pragma unroll
     for (int k = 0; k < 4; ++k) { v[2 * k] = f16_to_float(w[k] & 0xFFFFu); v[2 * k + 1] = f16_to_float(w[k] >> 16); }
   }
+  static __device__ __forceinline__ void put8(void* p, long long i, const float (&v)[8]) {
+    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) =
+        make_uint4(float_to_f16x2(v[0], v[1]), float_to_f16x2(v[2], v[3]), float_to_f16x2(v[4], v[5]), float_to_f16x2(v[6], v[7]));
+  }
 };
 
 // ---- eight consecutive elements as they are stored: their largest magnitude without unpacking 16-bit types ----------------

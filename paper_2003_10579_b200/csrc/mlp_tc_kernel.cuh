@@ -532,15 +532,6 @@ mlp_forward_tc_kernel(const __grid_constant__ CUtensorMap tmW, MlpArgs g) {
   if (failed && lane == 0) atomicExch(a.err, ERR_WAIT_TIMEOUT);
 }
 
-// Shared-memory matrix descriptor, 128-byte swizzle, MN-major operand (the M or N index is the
-// contiguous one): 64-element (128-byte) runs along MN, 8 such k-rows form a 1024-byte atom;
-// the next 8 k-rows are `sbo` bytes on (stride byte offset), the next 64 MN elements `lbo` bytes on
-// (leading byte offset).
-__device__ __forceinline__ uint64_t tc_desc_mnmajor(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(sbo >> 4) << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)2 << 61);
-}
-
 // ---- dW1 = bf16(X)^T bf16(delta1), fused with the update of W1: persistent kernel -----------------
 // Tiles of 128 rows of W1 x Hn columns (Hn <= 256) are dealt round-robin to one CTA per SM.  The
 // accumulator is double-buffered in tensor memory, so the epilogue of one tile overlaps the loads and

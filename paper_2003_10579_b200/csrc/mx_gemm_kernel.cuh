@@ -56,42 +56,14 @@ __device__ __forceinline__ void mxg_mma(uint32_t d, uint64_t adesc, uint64_t bde
       "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void mxg_commit(uint32_t bar) {
-  asm volatile(
-      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
-}
 // 512 bytes of shared memory, 32 rows of 16, to four tensor-memory columns of every quarter of the lanes
 __device__ __forceinline__ void mxg_copy_scales(uint32_t taddr, uint32_t saddr) {
   const uint64_t desc = (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);   // 8-row groups 128 B apart, no swizzle
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}" ::"r"(taddr), "l"(desc) : "memory");
 }
-__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
-// The warp's wait: one lane polls.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) {
-  bool ok = false;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait(bar, parity);
-  ok = __any_sync(0xFFFFFFFFu, ok);
-  __syncwarp();            // what the polling lane has seen is ordered before the others' accesses
-  return ok;
-}
 // A and B E2M1, scales E8M0, M = 128, N = n; id: which half of a column's four scale bytes (0 or 2)
 __device__ __forceinline__ uint32_t mxg_idesc(int n, uint32_t id) {
   return (id << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | (1u << 27) | (id << 29);
-}
-__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank) {
-  uint32_t p;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(addr), "r"(rank));
-  return p;
-}
-__device__ __forceinline__ float4 ld_cluster4(uint32_t cluster_ptr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_ptr) : "memory");
-  return v;
 }
 
 template <int T>
@@ -147,18 +119,6 @@ __device__ __forceinline__ void mxg_write_rows(const unsigned char* st, int lane
     }
   }
 }
-// 32 columns of the accumulators, without waiting for them
-__device__ __forceinline__ void mxg_ld32(uint32_t taddr, uint32_t* v) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-        "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]),
-        "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]),
-        "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-      : "r"(taddr));
-}
-__device__ __forceinline__ void mxg_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 template <int BN, int T, bool SWAP, bool SPLIT>
 __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -234,8 +194,8 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
         mxg_mma(tmem, ad + 4 * k, bd + 4 * k, mxg_idesc(BN, 0), sfa + 4 * k, sfb + 4 * k, (it > 0 || k > 0) ? 1u : 0u);
         mxg_mma(tmem, ad + 4 * k + 2, bd + 4 * k + 2, mxg_idesc(BN, 2), sfa + 4 * k, sfb + 4 * k, 1u);
       }
-      mxg_commit(empty(s));
-      if (it == stages - 1) mxg_commit(acc_bar);
+      tc_commit_elected(empty(s));
+      if (it == stages - 1) tc_commit_elected(acc_bar);
       if (++s == S::STAGES) { s = 0; phase ^= 1u; }
     }
   } else {
@@ -283,8 +243,8 @@ __global__ void __launch_bounds__(MXG_THREADS) mx_gemm_kernel(const __grid_const
             uint32_t w[64];
 #pragma unroll
             for (int j = 0; j < 32; ++j) w[j] = v[j];
-            mxg_ld32(trow + (ch + 1) * 32, w + 32);
-            mxg_ld_wait();
+            tc_ld32_async(trow + (ch + 1) * 32, w + 32);
+            tc_ld_wait();
             if (failed) {
 #pragma unroll
               for (int j = 32; j < 64; ++j) w[j] = 0x7FC00000u;
@@ -387,21 +347,8 @@ constexpr int MXP_SCALE_COLS = 48;                                    // four ti
 constexpr int MXP_TMEM_COLS = 512;
 static_assert(256 + MXP_SFT_STAGES * MXP_SCALE_COLS <= MXP_TMEM_COLS && MXP_SMEM <= 227 * 1024, "accumulators, scales and rings must fit");
 
-__device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-      ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
-}
 // Issued by one elected lane of a converged warp: with the whole warp in step the operands stay in uniform registers, where the
 // instruction wants them (4096 x 8192 x 8192: 121 us issued by one lane alone, 116 us so).
-__device__ __forceinline__ void mxp_commit(uint32_t bar) {            // to the barrier at this address in both blocks
-  asm volatile(
-      "{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
-      "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
 __device__ __forceinline__ void mxp_mma(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate) {
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\telect.sync _|q, 0xFFFFFFFF;\n\t"
@@ -416,29 +363,8 @@ __device__ __forceinline__ void mxp_st8(uint32_t taddr, const uint4 a, const uin
                ::"r"(taddr), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
 }
 
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // a look, without waiting
-  uint32_t ok;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
 
-// The warp's wait for a whole tile: one lane sleeps instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us
-// polling, 113 us).  The limit is four seconds; the longest tile whose operands fit the memory takes 0.2 s.
-__device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
-  bool ok = false;
-  if ((threadIdx.x & 31) == 0) ok = mbar_wait_asleep(bar, parity, 4000000000ull);
-  ok = __any_sync(0xFFFFFFFFu, ok);
-  __syncwarp();
-  return ok;
-}
 
-// slot and parity of a ring, stepped
-struct MxpRing {
-  int s = 0;
-  uint32_t phase;
-  __device__ __forceinline__ explicit MxpRing(uint32_t first) : phase(first) {}
-  template <int N> __device__ __forceinline__ void step() { if (++s == N) { s = 0; phase ^= 1u; } }
-};
 
 // Up to sixteen rows of 256 bytes from shared memory (16-byte pieces XOR-swizzled with the row) to rows of D at any alignment of the
 // element type: a lane writes an aligned 16-byte piece of its row, put together from five words of shared memory, and at most one of the
@@ -528,7 +454,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
   if (warp == 0) {
     if (lane == 0) {
-      MxpRing r(1);
+      Ring r(1);
       for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
         int a0, b0;
         tile_at(tile, a0, b0);
@@ -546,7 +472,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncwarp();
   } else if (warp == 14) {
     if (lane == 0) {
-      MxpRing r(1);
+      Ring r(1);
       for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
         int a0, b0;
         tile_at(tile, a0, b0);
@@ -569,7 +495,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
       // The MMA pipe queues about two instructions, 270 cycles of work.  What the thread does between the last MMA of a stage and the
       // first of the next has to be shorter, so the next stage's barriers are looked at while this one's MMAs are queued.
       const uint64_t adesc0 = tc_desc_kmajor(base), bdesc0 = tc_desc_kmajor(base + MXP_HALF);
-      MxpRing r(0), rs(0);
+      Ring r(0), rs(0);
       uint32_t acc_phase = 1;
       bool codes = false, scales = false;                                       // known to be there
       for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs, acc_phase ^= 1u) {
@@ -594,9 +520,9 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             mxp_mma(tmem, ad + 4, bd + 4, mxp_idesc(0), sfa + 4, sfb + 8, 1u);
             mxp_mma(tmem, ad + 6, bd + 6, mxp_idesc(2), sfa + 4, sfb + 8, 1u);
           }
-          mxp_commit(empty(s_now));
-          if (last) mxp_commit(sft_empty(rs_now));
-          if (it == stages - 1) mxp_commit(acc_full);
+          tc_commit_pair(empty(s_now));
+          if (last) tc_commit_pair(sft_empty(rs_now));
+          if (it == stages - 1) tc_commit_pair(acc_full);
         }
       }
     }
@@ -605,7 +531,7 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     // a lane holds rows l, 32 + l, 64 + l, 96 + l of each 512-byte tile: four columns of its tensor-memory lane; the four warps
     // write the same to their quarters of the lanes
     const uint32_t trow = sf_cols + ((uint32_t)(32 * (warp & 3)) << 16);
-    MxpRing r(0), rs(1);
+    Ring r(0), rs(1);
     for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
       for (int it = 0; it < sf_stages; ++it, r.step<MXP_SF_STAGES>(), rs.step<MXP_SFT_STAGES>()) {
         if (!mbar_wait_warp(sf_full(r.s), r.phase) || !mbar_wait_warp(sft_empty(rs.s), rs.phase)) { failed = true; break; }
@@ -674,19 +600,19 @@ mx_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 #pragma unroll
         for (int h = 0; h < 4; ++h) {
           uint32_t v[32];
-          mxg_ld32(trow + 32 * h, v);
-          mxg_ld_wait();
+          tc_ld32_async(trow + 32 * h, v);
+          tc_ld_wait();
           mxg_pack<T, 32>(v, w + 16 * h);
         }
       } else {
         // the first half of the columns waits in shared memory, so that the accumulators are free before anything is written
-        mxg_ld32(trow, w);
-        mxg_ld32(trow + 32, w + 32);
-        mxg_ld_wait();
+        tc_ld32_async(trow, w);
+        tc_ld32_async(trow + 32, w + 32);
+        tc_ld_wait();
         to_rows();
-        mxg_ld32(trow + 64, w);
-        mxg_ld32(trow + 96, w + 32);
-        mxg_ld_wait();
+        tc_ld32_async(trow + 64, w);
+        tc_ld32_async(trow + 96, w + 32);
+        tc_ld_wait();
       }
       tc_fence_before();                                                        // the accumulators are read: the next tile may start
       __syncwarp();
