@@ -460,8 +460,9 @@ sim_status sim_ckpt_read(const uint8_t* codes, const uint8_t* scales, int64_t ro
 
 /*
  * dz = dy act'(z) for z kept in 8 bits, and db = the sums of dz over its rows (fp32 sums of what has not been rounded, in a fixed order,
- * rounded once to db_type).  db may be NULL; with codes, scales and dz NULL, db is the sums of dy.  dz has dy's type and may
- * be dy itself with the same rows.  db needs a workspace of sim_act_backward_workspace bytes (4-byte aligned).
+ * rounded once to db_type).  db may be NULL; with codes and scales NULL, db is the sums of dy, and dz NULL or a copy of dy (rows of another
+ * length, say).  dz has dy's type and may be dy itself with the same rows.  db needs a workspace of sim_act_backward_workspace bytes (0 for few
+ * rows; 4-byte aligned).
  */
 int64_t sim_act_backward_workspace(int64_t rows, int64_t cols);
 sim_status sim_act_backward(const void* dy, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, const uint8_t* codes, const uint8_t* scales, sim_act act, void* dz, int64_t lddz,

@@ -8,6 +8,7 @@ import collections
 import contextlib
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -121,8 +122,8 @@ def _load():
     L.sim_ckpt_read.argtypes = [vp, vp, i64, i64, C.c_int, C.c_int, vp, i64, vp]
     L.sim_act_backward_workspace.argtypes = [i64, i64]
     L.sim_act_backward.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, C.c_int, vp, i64, vp, C.c_int, vp, i64, vp]
-    L.sim_matmul_workspace.argtypes = [C.POINTER(SimProduct)]
-    L.sim_matmul.argtypes = [C.POINTER(SimProduct), vp, i64, vp]
+    L.sim_matmul_workspace.argtypes = [vp]           # a sim_product
+    L.sim_matmul.argtypes = [vp, vp, i64, vp]
     L.sim_log_probs.argtypes = [vp, C.c_int, i64, i64, i64, vp, i32, C.c_float, i32] + [vp] * 8 + [i64, vp]
     sizes = ("sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_ckpt_codes_bytes", "sim_ckpt_scales_bytes", "sim_act_backward_workspace", "sim_matmul_workspace")
     for name in EXPORTS:
@@ -740,14 +741,23 @@ def _act_code(name):
     return ACTS[name]
 
 
-def _plain(x, what, dtypes=tuple(DTYPES)):
+_ALL, _HALF = tuple(DTYPES), (torch.bfloat16, torch.float16)
+
+
+def _plain(x, what, dtypes=_ALL):
     """A CUDA matrix (or vector: one row), possibly without elements, neighbours along the last dimension -> (rows, cols, elements between rows)."""
     if not torch.is_tensor(x) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
         raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, " or ".join(str(d)[6:] for d in dtypes)))
-    rows, cols = (1, x.shape[0]) if x.dim() == 1 else x.shape
-    if x.numel() and ((cols > 1 and x.stride(-1) != 1) or (rows > 1 and x.stride(0) < cols)):
+    if x.dim() == 2:
+        rows, cols = x.shape
+        ld, step = x.stride()
+    else:
+        (cols,), (step,), rows, ld = x.shape, x.stride(), 1, 0
+    if rows <= 1 or cols == 0:
+        ld = cols
+    if (step != 1 and cols > 1 and rows) or ld < cols:
         raise ValueError("%s must have neighbouring elements along its last dimension and rows that do not overlap" % what)
-    return rows, cols, x.stride(0) if rows > 1 and x.numel() else cols
+    return rows, cols, ld
 
 
 def _same(device, **tensors):
@@ -797,8 +807,15 @@ def _scratch(nbytes, device, stream):
         return torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
 
 
+def _padded(rows, cols, dtype, device, stream):
+    """(a matrix whose rows start on 16-byte boundaries, the elements between them)"""
+    ld = -(-cols // 8) * 8
+    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+        return torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device), ld
+
+
 def _sums(dy, rows, cols, ld, z, code, dz, lddz, db, device, stream):
-    room = lib.sim_act_backward_workspace(rows, cols) if db is not None else 0
+    room = lib.sim_act_backward_workspace(rows, cols) if db is not None and rows > 256 else 0      # few rows need none
     ws = _scratch(room, device, stream)
     _check(_on(device, stream, lib.sim_act_backward, dy.data_ptr(), DTYPES[dy.dtype], rows, cols, ld, z and z.codes_ptr, z and z.scales_ptr, code,
                None if dz is None else dz.data_ptr(), lddz, None if db is None else db.data_ptr(), 0 if db is None else DTYPES[db.dtype],
@@ -834,34 +851,39 @@ def act_backward(dy, z, act, *, bias=True, dtype=torch.float32, out=None, stream
     return dz, db
 
 
-_HALF = (torch.bfloat16, torch.float16)
-
-
-def _side(x, what, dtype=None):
+def _side(x, what, dtypes=_HALF):
     """An operand of a product, its rows along either dimension -> (rows, cols, elements between its rows in memory, whether those lie along the
     first dimension's neighbours)."""
-    if not torch.is_tensor(x) or not x.is_cuda or x.dim() not in (1, 2) or x.dtype not in ((dtype,) if dtype else _HALF):
-        raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, str(dtype)[6:] if dtype else "bfloat16 or float16"))
-    rows, cols = (1, x.shape[0]) if x.dim() == 1 else x.shape
-    if x.numel() == 0 or ((cols == 1 or x.stride(-1) == 1) and (rows == 1 or x.stride(0) >= cols)):
-        return rows, cols, x.stride(0) if rows > 1 and x.numel() else cols, False
-    if x.dim() == 2 and (rows == 1 or x.stride(0) == 1) and x.stride(1) >= rows:
-        return rows, cols, x.stride(1), True
+    if not torch.is_tensor(x) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
+        raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, " or ".join(str(d)[6:] for d in dtypes)))
+    if x.dim() == 2:
+        rows, cols = x.shape
+        ld, step = x.stride()
+    else:
+        (cols,), (step,), rows, ld = x.shape, x.stride(), 1, 0
+    if rows == 0 or cols == 0:
+        return rows, cols, cols, False
+    if step == 1 or cols == 1:
+        if rows == 1:
+            return rows, cols, cols, False
+        if ld >= cols:
+            return rows, cols, ld, False
+    if (ld == 1 or rows == 1) and step >= rows:
+        return rows, cols, step, True
     raise ValueError("%s must have neighbouring elements along one dimension, and the others must not overlap" % what)
 
 
-def _product(device, stream, M, N, K, dtype, a, lda, a_t, b, ldb, b_t, c, ldc, *, bias=None, act=0, act_grad=False, z=None, residual=None, ldr=0):
-    p = SimProduct(M, N, K, DTYPES[dtype], a, lda, a_t, b, ldb, b_t, None, 0, act, act_grad, None, None, None, 0, c.data_ptr(), DTYPES[c.dtype], ldc)
-    if bias is not None:
-        p.bias, p.bias_type = bias.data_ptr(), DTYPES[bias.dtype]
-    if z is not None:
-        p.z_codes, p.z_scales = z.codes_ptr, z.scales_ptr
-    if residual is not None:
-        p.residual, p.ldr = residual.data_ptr(), ldr
+_PRODUCT = struct.Struct("@qqqiPqiPqiPiiiPPPqPiq")          # a sim_product; made in half the time of SimProduct
+assert _PRODUCT.size == C.sizeof(SimProduct)
+
+
+def _product(device, stream, M, N, K, dtype, a, lda, a_t, b, ldb, b_t, c, ldc, bias=None, act=0, act_grad=False, z=None, residual=None, ldr=0):
+    p = _PRODUCT.pack(M, N, K, DTYPES[dtype], a, lda, a_t, b, ldb, b_t, *((0, 0) if bias is None else (bias.data_ptr(), DTYPES[bias.dtype])), act, act_grad,
+                      *((0, 0) if z is None else (z.codes_ptr, z.scales_ptr)), 0 if residual is None else residual.data_ptr(), ldr, c.data_ptr(), DTYPES[c.dtype], ldc)
     # rows on 16-byte boundaries need no room; the library is asked for the rest
-    room = 0 if (a | b | (lda | ldb) * 2) & 15 == 0 else lib.sim_matmul_workspace(C.byref(p))
-    ws = _scratch(room, device, stream)
-    _check(_on(device, stream, lib.sim_matmul, C.byref(p), None if ws is None else ws.data_ptr(), room))
+    room = 0 if (a | b | (lda | ldb) * 2) & 15 == 0 else lib.sim_matmul_workspace(p)
+    ws = _scratch(room, device, stream).data_ptr() if room else None
+    _check(_on(device, stream, lib.sim_matmul, p, ws, room))
 
 
 def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None, out=None, stream=None):
@@ -870,19 +892,23 @@ def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None
     operands' type or float32, and so has the residual.  keep: (result, Checkpoint of x w^T + bias), for the backward pass."""
     code = _act_code(act)
     M, K, lda, a_t = _side(x, "x")
-    N, Kw, ldb, b_t = _side(w, "w", x.dtype)
+    kind = x.dtype
+    N, Kw, ldb, b_t = _side(w, "w", (kind,))
     device = x.device
     if K != Kw:
         raise ValueError("x and w must have as many columns")
-    kinds = (x.dtype, torch.float32)
-    if (out.dtype if out is not None else dtype or x.dtype) not in kinds:
+    kinds = (kind, torch.float32)
+    if (out.dtype if out is not None else dtype or kind) not in kinds:
         raise ValueError("the result is float32 or of the operands' type")
     _same(device, w=w, bias=bias, residual=residual)
     if bias is not None and (bias.dtype not in kinds or bias.dim() != 1 or bias.numel() != N or (N > 1 and bias.stride(0) != 1)):
         raise ValueError("bias must be a contiguous vector of %d of float32 or the operands' type" % N)
     if stream is not None:
         _given(stream, device, *(t for t in (x, w, bias, residual) if t is not None))
-    out, ldc = _result(out, M, N, (dtype or x.dtype,) if out is None else kinds, device, stream)
+    if out is None:
+        out, ldc = _empty(M, N, dtype or kind, device, stream), N
+    else:
+        out, ldc = _result(out, M, N, kinds, device, stream)
     ldr = 0
     if residual is not None:
         r, c, ldr = _plain(residual, "residual", (out.dtype,))
@@ -892,7 +918,7 @@ def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None
     if keep:
         with _NO_STREAM if stream is None else torch.cuda.stream(stream):
             z = Checkpoint.empty(M, N, device)
-    _product(device, stream, M, N, K, x.dtype, x.data_ptr(), lda, a_t, w.data_ptr(), ldb, b_t, out, ldc, bias=bias, act=code, z=z, residual=residual, ldr=ldr)
+    _product(device, stream, M, N, K, kind, x.data_ptr(), lda, a_t, w.data_ptr(), ldb, b_t, out, ldc, bias, code, False, z, residual, ldr)
     return (out, z) if keep else out
 
 
@@ -904,13 +930,13 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     into, each may be None."""
     code = _act_code(x_act)
     M, N, lda, a_t = _side(dy, "dy")
-    Nw, K, ldb, b_t = _side(w, "w", dy.dtype)
+    Nw, K, ldb, b_t = _side(w, "w", (dy.dtype,))
     device = dy.device
     kept = isinstance(x, Checkpoint)
     if kept:
         Mx, Kx = x.rows, x.cols
     else:
-        Mx, Kx, ldx, x_t = _side(x, "x", dy.dtype)
+        Mx, Kx, ldx, x_t = _side(x, "x", (dy.dtype,))
         if code:
             raise ValueError("x_act belongs to a Checkpoint: a tensor x is the layer's input itself")
     if Nw != N or Mx != M or Kx != K or x.device != device:
@@ -922,6 +948,16 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     if stream is not None:
         _given(stream, device, *(t for t in (dy, x, w, residual) if t is not None))
     dx, dw, db = out or (None, None, None)
+    if "b" in need:
+        if a_t:
+            raise ValueError("db needs dy with neighbouring elements along its last dimension")
+        db = _vector(db, N, (dtype,) if db is None else tuple(DTYPES), device, stream, "db")
+        copy = None
+        if (dy.data_ptr() | lda * 2) & 15 and len(need) > 1:       # the products want rows on 16-byte boundaries: copied on the way
+            copy, ldd = _padded(M, N, dy.dtype, device, stream)
+        _sums(dy, M, N, lda, None, 0, copy, 0 if copy is None else ldd, db, device, stream)
+        if copy is not None:
+            dy, lda = copy, ldd
     if "x" in need:
         dx, ldc = _result(dx, M, K, (dy.dtype,), device, stream, "dx")
         ldr = 0
@@ -935,19 +971,12 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     if "w" in need:
         dw, ldc = _result(dw, N, K, (dtype,) if dw is None else kinds, device, stream, "dw")
         if kept:
-            # rows of whole 16-byte pieces, as the product wants them
-            with _NO_STREAM if stream is None else torch.cuda.stream(stream):
-                h = torch.empty_strided((M, K), (-(-K // 8) * 8, 1), dtype=dy.dtype, device=device)
-            ldx, x_t = h.stride(0), False
+            h, ldx = _padded(M, K, dy.dtype, device, stream)
+            x_t = False
             _check(_on(device, stream, lib.sim_ckpt_read, x.codes_ptr, x.scales_ptr, M, K, code, DTYPES[dy.dtype], h.data_ptr(), ldx))
         else:
             h = x
         _product(device, stream, N, K, M, dy.dtype, dy.data_ptr(), lda, not a_t, h.data_ptr(), ldx, not x_t, dw, ldc)
-    if "b" in need:
-        db = _vector(db, N, (dtype,) if db is None else tuple(DTYPES), device, stream, "db")
-        if a_t:
-            raise ValueError("db needs dy with neighbouring elements along its last dimension")
-        _sums(dy, M, N, lda, None, 0, None, 0, db, device, stream)
     return dx if "x" in need else None, dw if "w" in need else None, db if "b" in need else None
 
 
@@ -969,22 +998,18 @@ def log_probs(logits, tokens=None, *, top=0, temperature=1.0, d_logp=None, d_ent
     if vocab == 0 or not 0 <= top <= min(32, vocab):
         raise ValueError("vocab must be at least 1 and top in [0, min(32, vocab)]")
     d, ldd = _result(out, rows, vocab, (logits.dtype,), device, stream) if grad else (None, 0)
-    # one buffer for all vectors: entropy, lse, logp, then the alternatives
-    n = (3 if tokens is not None else 2) + 2 * top
-    buf = _empty(n, rows, torch.float32, device, stream)
-    base, size = buf.data_ptr(), 4 * rows
-    lp = base + 2 * size if tokens is not None else None
-    ti = base + (n - 2 * top) * size if top else None
-    tl = base + (n - top) * size if top else None
+    # one buffer for the vectors: logp, entropy, lse
+    buf = _empty(3, rows, torch.float32, device, stream)
+    at, size = buf.data_ptr(), 4 * rows
+    ids = _empty(rows, top, torch.int32, device, stream) if top else None
+    logs = _empty(rows, top, torch.float32, device, stream) if top else None
     _check(_on(device, stream, lib.sim_log_probs, logits.data_ptr(), DTYPES[logits.dtype], rows, vocab, ld, None if tokens is None else tokens.data_ptr(), tb,
-               temperature, top, lp, base, base + size, ti, tl, None if d_logp is None else d_logp.data_ptr(), None if d_entropy is None else d_entropy.data_ptr(),
-               None if d is None else d.data_ptr(), ldd))
-    if logits.dim() == 1 and out is None and d is not None:
+               temperature, top, None if tokens is None else at, at + size, at + 2 * size, ids.data_ptr() if top else None, logs.data_ptr() if top else None,
+               None if d_logp is None else d_logp.data_ptr(), None if d_entropy is None else d_entropy.data_ptr(), None if d is None else d.data_ptr(), ldd))
+    if d is not None and logits.dim() == 1 and out is None:
         d = d[0]
-    ids = logs = None
-    if top:
-        ids, logs = buf[n - 2 * top: n - top].view(torch.int32).view(rows, top), buf[n - top:].view(rows, top)
-    return LogProbs(buf[2] if tokens is not None else None, buf[0], buf[1], ids, logs, d)
+    logp, entropy, lse = buf.unbind()
+    return LogProbs(None if tokens is None else logp, entropy, lse, ids, logs, d)
 
 
 def log_probs_backward(logits, tokens, d_logp=None, d_entropy=None, *, temperature=1.0, out=None, stream=None):

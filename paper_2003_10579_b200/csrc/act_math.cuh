@@ -12,15 +12,19 @@ namespace ssim {
 enum : int { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };
 
 constexpr float GELU_C = 1.5957691216057308f, GELU_A = 0.044715f;      // 2 sqrt(2 / pi)
+constexpr float LOG2E = 1.4426950408889634f;
 
-// The approximate exponential and reciprocal are off by about 2^-21 of the value at most, far below a 16-bit type's half step.
-__device__ __forceinline__ float logistic(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
+__device__ __forceinline__ float exp2_fast(float d) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
+__device__ __forceinline__ float rcp_fast(float d) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
+
+// 1 / (1 + 2^-d).  The approximate power and reciprocal are off by about 2^-21 of the value at most, far below a 16-bit type's half step.
+__device__ __forceinline__ float logistic2(float d) { return rcp_fast(1.f + exp2_fast(-d)); }
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
   if (ACT == ACT_RELU) return z > 0.f ? z : z != z ? z : 0.f;
-  if (ACT == ACT_GELU) return z * logistic(GELU_C * z * fmaf(GELU_A * z, z, 1.f));
-  if (ACT == ACT_SILU) return z * logistic(z);
+  if (ACT == ACT_GELU) return z * logistic2(z * fmaf(LOG2E * GELU_C * GELU_A * z, z, LOG2E * GELU_C));
+  if (ACT == ACT_SILU) return z * logistic2(LOG2E * z);
   return z;
 }
 // The derivative; relu's at zero is zero.
@@ -29,13 +33,13 @@ __device__ __forceinline__ float act_slope(float z) {
   if (ACT == ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
   if (ACT == ACT_GELU) {
     const float t = fminf(fmaxf(z, -10.f), 10.f);                      // beyond, it is 0 or 1, and the cube would only raise the error of 1 - q
-    const float q = logistic(GELU_C * t * fmaf(GELU_A * t, t, 1.f));
-    const float d = fmaf(t * q * (1.f - q), GELU_C * fmaf(3.f * GELU_A * t, t, 1.f), q);
+    const float q = logistic2(t * fmaf(LOG2E * GELU_C * GELU_A * t, t, LOG2E * GELU_C));
+    const float d = fmaf(t * q * (1.f - q), fmaf(3.f * GELU_C * GELU_A * t, t, GELU_C), q);
     return z != z ? z : d;
   }
   if (ACT == ACT_SILU) {
     const float t = fminf(fmaxf(z, -80.f), 80.f);
-    const float q = logistic(t), d = fmaf(t * q, 1.f - q, q);
+    const float q = logistic2(LOG2E * t), d = fmaf(t * q, 1.f - q, q);
     return z != z ? z : d;
   }
   return 1.f;

@@ -10,6 +10,7 @@
 #pragma once
 #include "act_math.cuh"
 #include "lowbits.cuh"
+#include "ptx_util.cuh"
 
 namespace ssim {
 
@@ -24,8 +25,15 @@ struct CkptArgs {
   long long ldo;
   int vec;                    // rows of x and out on 16-byte boundaries
   float* partial;             // act_backward: column sums [splits][cols], or null
-  int split_rows;
+  void* db;                   // act_backward: column sums [cols] of db_type, where the splits are the blocks of a cluster, or null
+  int db_type, split_rows;
 };
+
+__device__ __forceinline__ void put_as(int type, void* p, long long i, float v) {
+  if (type == T_F32) Elem<T_F32>::put(p, i, v);
+  else if (type == T_BF16) Elem<T_BF16>::put(p, i, v);
+  else Elem<T_F16>::put(p, i, v);
+}
 
 // Row and piece of the pieces first, first + step, ... of a matrix with `pieces` to a row, without a division each time
 struct PieceWalk {
@@ -83,7 +91,7 @@ __global__ void __launch_bounds__(256) ckpt_write_kernel(const __grid_constant__
   }
 }
 
-// sixteen codes of a block and its scale -> values
+// four codes of a block and its scale -> values
 __device__ __forceinline__ void ckpt_values4(uint32_t w, float scale, float* v) {
   const float2 lo = from_e4m3x2(w & 0xFFFFu), hi = from_e4m3x2(w >> 16);
   v[0] = lo.x * scale; v[1] = lo.y * scale; v[2] = hi.x * scale; v[3] = hi.y * scale;
@@ -95,23 +103,25 @@ __global__ void __launch_bounds__(256) ckpt_read_kernel(const __grid_constant__ 
   const uint32_t blocks = (uint32_t)((a.cols + 31) / 32);
   const long long pitch = 32ll * blocks;
   if (a.vec) {
-    for (PieceWalk at((long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256, 2 * blocks); at.row < a.rows; at.next()) {   // halves of blocks
-      const long long c = 16ll * at.at;
-      if (c >= a.cols) continue;
-      const uint4 w = *reinterpret_cast<const uint4*>(a.codes + at.row * pitch + c);
-      const float scale = scale_value(a.scales[at.row * blocks + (at.at >> 1)]);
-      float v[2][8];
-      ckpt_values4(w.x, scale, v[0]); ckpt_values4(w.y, scale, v[0] + 4); ckpt_values4(w.z, scale, v[1]); ckpt_values4(w.w, scale, v[1] + 4);
+    for (PieceWalk at((long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256, blocks); at.row < a.rows; at.next()) {
+      const long long c = 32ll * at.at;
+      const uint4* from = reinterpret_cast<const uint4*>(a.codes + at.row * pitch + c);
+      const uint4 w0 = from[0], w1 = from[1];
+      const float scale = scale_value(a.scales[at.row * blocks + at.at]);
+      const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
       char* row = static_cast<char*>(a.out) + at.row * a.ldo * EB;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 4; ++h) {
+        float v[8];
+        ckpt_values4(w[2 * h], scale, v);
+        ckpt_values4(w[2 * h + 1], scale, v + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[h][e] = act_value<ACT>(v[h][e]);
-        if (c + 8 * h + 8 <= a.cols) Elem<T>::put8(row, c + 8 * h, v[h]);
+        for (int e = 0; e < 8; ++e) v[e] = act_value<ACT>(v[e]);
+        if (c + 8 * h + 8 <= a.cols) Elem<T>::put8(row, c + 8 * h, v);
         else
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (c + 8 * h + e < a.cols) Elem<T>::put(row, c + 8 * h + e, v[h][e]);
+            if (c + 8 * h + e < a.cols) Elem<T>::put(row, c + 8 * h + e, v[e]);
       }
     }
   } else {
@@ -125,91 +135,105 @@ __global__ void __launch_bounds__(256) ckpt_read_kernel(const __grid_constant__ 
 }
 
 // dz = dy act'(z) and the sums of dz (before it is rounded) over the rows.  A block takes 256 columns and split_rows rows, a warp every
-// eighth of these, a lane eight columns, four rows at a time so that loads of four rows are in flight.  The eight warps' sums meet in
-// shared memory in the order of the warps, the blocks' in a second kernel in the order of the splits: the same bits every time.
-// KEPT = false: no z, only the sums of dy.
-template <int T, int ACT, bool KEPT>
-__global__ void __launch_bounds__(256) act_backward_kernel(const __grid_constant__ CkptArgs a) {
-  constexpr int EB = Elem<T>::bytes;
+// eighth of these, a lane eight columns.  What a lane reads stays packed until its row's turn, so that the loads of two rows are
+// in flight and three blocks fit a multiprocessor.  The eight warps' sums meet in shared memory in the order of the warps; the blocks' in
+// the order of the splits, where there are at most eight in the distributed shared memory of a cluster, else in a second kernel: the same
+// bits every time.  KEPT = false: no z, only the sums of dy, and dz (if there is one) is a copy of dy.
+template <int T, int ACT, bool KEPT, bool VEC>
+__global__ void __launch_bounds__(256, 3) act_backward_kernel(const __grid_constant__ CkptArgs a) {
+  constexpr int EB = Elem<T>::bytes, AHEAD = VEC || !KEPT ? 2 : 1, STEP = VEC ? 1 : 32;      // STEP: between a lane's eight columns
   __shared__ float sums[8][256];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint32_t blocks = (uint32_t)((a.cols + 31) / 32);
   const long long pitch = 32ll * blocks, c0 = 256ll * blockIdx.x;
   const long long r0 = (long long)blockIdx.y * a.split_rows, r1 = min(a.rows, r0 + a.split_rows);
-  const int step = a.vec ? 1 : 32;                                       // a lane's eight columns: neighbours, or 32 apart
-  const long long c = c0 + (a.vec ? 8 * lane : lane);
-  const bool whole = a.vec && c + 8 <= a.cols;
+  const long long c = c0 + (VEC ? 8 * lane : lane);
+  const int n = (int)max(0ll, min(8ll, VEC ? a.cols - c : (a.cols - c + 31) / 32));                 // of the eight that exist
   float acc[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 
-  for (long long r = r0 + warp; r < r1; r += 32) {
-    float g[4][8], z[4][8];
+#pragma unroll 1
+  for (long long r = r0 + warp; r < r1; r += 8 * AHEAD) {
+    Raw8<T> g[AHEAD];
+    uint2 code[AHEAD];
+    uint32_t scale[AHEAD][VEC ? 1 : 8];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < AHEAD; ++k) {
       const long long row = r + 8 * k;
+      const int m = row < r1 ? n : 0;
       const char* src = static_cast<const char*>(a.x) + row * a.ld * EB;
-      if (row < r1 && whole) Elem<T>::get8(src, c, g[k]);
-      else
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[k][e] = row < r1 && c + e * step < a.cols ? Elem<T>::get(src, c + e * step) : 0.f;
+      if (VEC && m == 8) g[k].load(src, c);
+      else if (VEC) g[k].load_some(src, c, m);
+      else g[k].load_apart(src, c, 32, m);
       if constexpr (KEPT) {
-        const uint8_t* code = a.codes + row * pitch;
-        const uint8_t* scale = a.scales + row * blocks;
-        if (a.vec) {
-          if (row < r1 && c < pitch) {
-            const uint2 w = *reinterpret_cast<const uint2*>(code + c);
-            const float s = scale_value(scale[c >> 5]);
-            ckpt_values4(w.x, s, z[k]); ckpt_values4(w.y, s, z[k] + 4);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) z[k][e] = 0.f;
-          }
+        code[k] = make_uint2(0u, 0u);
+        const uint8_t* from = a.codes + row * pitch + c;
+        const uint8_t* sc = a.scales + row * blocks + (c >> 5);
+        if (VEC) {
+          scale[k][0] = 0u;
+          if (m > 0) { code[k] = *reinterpret_cast<const uint2*>(from); scale[k][0] = *sc; }        // c is in the row, and a row of codes has whole blocks
         } else {
+          uint32_t w[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            const long long at = c + 32 * e;
-            z[k][e] = row < r1 && at < pitch ? from_e4m3x2(code[at]).x * scale_value(scale[at >> 5]) : 0.f;
+            w[e] = e < m ? from[32 * e] : 0u;
+            scale[k][e] = e < m ? sc[e] : 0u;
           }
+          code[k] = make_uint2(w[0] | w[1] << 8 | w[2] << 16 | w[3] << 24, w[4] | w[5] << 8 | w[6] << 16 | w[7] << 24);
         }
       }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < AHEAD; ++k) {
       const long long row = r + 8 * k;
+      const int m = row < r1 ? n : 0;
+      float d[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) d[e] = g[k].value(e);
       if constexpr (KEPT) {
+        float z[8];
+        ckpt_values4(code[k].x, 1.f, z);
+        ckpt_values4(code[k].y, 1.f, z + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) g[k][e] *= act_slope<ACT>(z[k][e]);
-        if (row < r1) {
-          char* to = static_cast<char*>(a.out) + row * a.ldo * EB;
-          if (whole) Elem<T>::put8(to, c, g[k]);
-          else
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (c + e * step < a.cols) Elem<T>::put(to, c + e * step, g[k][e]);
-        }
+        for (int e = 0; e < 8; ++e) d[e] *= act_slope<ACT>(z[e] * scale_value(scale[k][VEC ? 0 : e]));
       }
-      if (row < r1)
+      if (KEPT || a.out) {
+        char* to = static_cast<char*>(a.out) + row * a.ldo * EB;
+        if (VEC && m == 8) Elem<T>::put8(to, c, d);
+        else
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += g[k][e];
+          for (int e = 0; e < 8; ++e)
+            if (e < m) Elem<T>::put(to, c + e * STEP, d[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += e < m ? d[e] : 0.f;
     }
   }
-  if (!a.partial) return;
+  if (!a.partial && !a.db) return;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sums[warp][(a.vec ? 8 * lane : lane) + e * step] = acc[e];
+  for (int e = 0; e < 8; ++e) sums[warp][(VEC ? 8 * lane : lane) + e * STEP] = acc[e];
   __syncthreads();
   const long long at = c0 + threadIdx.x;
-  if (at < a.cols) {
-    float s = sums[0][threadIdx.x];
+  float s = sums[0][threadIdx.x];
 #pragma unroll
-    for (int w = 1; w < 8; ++w) s += sums[w][threadIdx.x];
-    a.partial[(long long)blockIdx.y * a.cols + at] = s;
+  for (int w = 1; w < 8; ++w) s += sums[w][threadIdx.x];
+  if (a.partial) {
+    if (at < a.cols) a.partial[(long long)blockIdx.y * a.cols + at] = s;
+    return;
   }
+  if (gridDim.y > 1) {
+    sums[0][threadIdx.x] = s;                                            // read by this thread alone so far
+    cluster_sync_all();
+    if (blockIdx.y == 0)
+      for (int r = 1; r < (int)gridDim.y; ++r) s += ld_cluster1(cluster_addr(smem_addr(&sums[0][threadIdx.x]), (uint32_t)r));
+    cluster_sync_all();                                                  // nobody leaves while its sums may still be read
+  }
+  if (blockIdx.y == 0 && at < a.cols) put_as(a.db_type, a.db, at, s);
 }
 
 // Sums [splits][cols] -> out [cols].  A block takes 32 columns, a warp every eighth split.
-template <int T>
-__global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* partial, int splits, long long cols, void* out) {
+__global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* partial, int splits, long long cols, void* out, int type) {
   __shared__ float sums[8][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const long long c = 32ll * blockIdx.x + lane;
@@ -222,7 +246,7 @@ __global__ void __launch_bounds__(256) column_sum_finish_kernel(const float* par
   if (warp == 0 && c < cols) {
 #pragma unroll
     for (int w = 1; w < 8; ++w) s += sums[w][lane];
-    Elem<T>::put(out, c, s);
+    put_as(type, out, c, s);
   }
 }
 

@@ -16,12 +16,14 @@
 //
 // Floor: HBM, the row read once (and the gradient written once).
 #pragma once
+#include "act_math.cuh"
 #include "lowbits.cuh"
 #include "ptx_util.cuh"
 
 namespace ssim {
 
 constexpr int LP_MAX_TOP = 32;
+constexpr int LP_THREADS = 1536;            // a multiprocessor's, of the kernel for long rows
 constexpr int LP_LIST = 1024;               // logits that may reach the bound
 constexpr float LP_LN2 = 0.6931471805599453f;
 constexpr float LP_NONE = -200.f;           // 2^-200 is zero
@@ -40,8 +42,9 @@ struct LogpArgs {
   long long ldo;
 };
 
-__device__ __forceinline__ float exp2_fast(float d) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
 __device__ __forceinline__ float max_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) { uint32_t r; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
+constexpr uint32_t LP_LOW_BF16X2 = 0xF149F149u;      // -1e30 twice
 __device__ __forceinline__ float neg_inf() { return __uint_as_float(0xFF800000u); }
 __device__ __forceinline__ float quiet_nan() { return __uint_as_float(0x7FC00000u); }
 
@@ -56,30 +59,36 @@ __device__ __forceinline__ float logit_of_key(uint32_t k) {
 // bits of a key that are the same for all values of one sign of a type
 template <int T> struct KeyShift { static constexpr int value = T == T_BF16 ? 16 : T == T_F16 ? 13 : 0; };
 
-// Running reference and sums of some logits
+// Running reference and sums of some logits.  What the loops need of the reference is kept ready: where the next move is due, the addend of c x.
 struct LogSum {
   float m4 = neg_inf(), s = 0.f, q = 0.f;
-  __device__ __forceinline__ bool far() const { return fabsf(m4) > 1048576.f && m4 != neg_inf(); }    // c x may overflow
+  float due = neg_inf(), off = 0.f;                          // m4 + 2; -4 m4 (0 for none)
+  bool far = false;                                          // c x may overflow
+  __device__ __forceinline__ void set(float to4) {
+    m4 = to4;
+    due = to4 + 2.f;
+    off = to4 == neg_inf() ? 0.f : -4.f * to4;
+    far = fabsf(to4) > 1048576.f && to4 != neg_inf();
+  }
   __device__ __forceinline__ void move(float to4) {          // to a reference to4 >= m4
     const float by = 4.f * (to4 - m4);
     if (by < 250.f) {
       const float f = exp2_fast(-by);
       q = (q - by * s) * f;
       s *= f;
-    } else if (by >= 250.f) {
+    } else {
       s = s == s ? 0.f : s;                                  // a NaN stays
       q = s;
     }
-    m4 = to4;
+    set(to4);
   }
   __device__ __forceinline__ void reach(float most, float c4) {
     const float top4 = __fmul_rn(most, c4);
-    if (top4 > m4 + 2.f) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4);
+    if (top4 > due) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4);
   }
-  __device__ __forceinline__ float off() const { return m4 == neg_inf() ? 0.f : -4.f * m4; }
   __device__ __forceinline__ float dist(float x, float c, float c4) const {
     if (m4 == neg_inf()) return x;
-    return far() ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, -4.f * m4);
+    return far ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, off);
   }
   __device__ __forceinline__ void add(float d) {             // d >= LP_NONE or NaN
     const float e = exp2_fast(d);
@@ -87,35 +96,61 @@ struct LogSum {
     q = fmaf(e, d, q);
   }
   template <int N>
+  __device__ __forceinline__ void add_far(const float (&x)[N], float c4) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) add(max_nan(4.f * (__fmul_rn(x[e], c4) - m4), LP_NONE));     // equal logits differ by nothing
+  }
+  template <int N>
   __device__ __forceinline__ float take(const float (&x)[N], float c, float c4) {
     float most = x[0];
 #pragma unroll
     for (int e = 1; e < N; ++e) most = max_nan(most, x[e]);
     reach(most, c4);
-    if (!far()) {
-      const float o = off();
+    if (far) add_far(x, c4);
+    else
 #pragma unroll
-      for (int e = 0; e < N; ++e) add(max_nan(fmaf(x[e], c, o), LP_NONE));
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e) add(max_nan(4.f * (__fmul_rn(x[e], c4) - m4), LP_NONE));   // equal logits differ by nothing
-    }
+      for (int e = 0; e < N; ++e) add(max_nan(fmaf(x[e], c, off), LP_NONE));
     return most;
   }
-  __device__ __forceinline__ void join(float om4, float os, float oq) {
-    LogSum o;
-    o.m4 = om4; o.s = os; o.q = oq;
-    const float to = fmaxf(m4, om4);
-    if (m4 != to) move(to);
-    if (o.m4 != to) o.move(to);
-    s += o.s; q += o.q;
+  // Eight logits as they are stored.  bf16: the largest and the way out of -inf two at a time - a logit under -1e30 stands for any such, and its
+  // probability is zero without the product 0 (-inf) - unless they all are that small.
+  template <int T>
+  __device__ __forceinline__ float take8(const Raw8<T>& r, float c, float c4) {
+    if constexpr (T == T_BF16) {
+      const uint32_t m = max_nan_bf16x2(max_nan_bf16x2(r.w[0], r.w[1]), max_nan_bf16x2(r.w[2], r.w[3]));
+      const float most = max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+      reach(most, c4);
+      float x[8];
+      if (far) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = r.value(e);
+        add_far(x, c4);
+        return most;
+      }
+      Raw8<T> f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f.w[k] = max_nan_bf16x2(r.w[k], LP_LOW_BF16X2);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) add(fmaf(f.value(e), c, off));
+      return most;
+    } else {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = r.value(e);
+      return take(x, c, c4);
+    }
   }
+  // The sums of groups of G lanes, in each of them: first the largest reference, then one move, then two trees
   template <int G>
-  __device__ __forceinline__ void join_lanes() {             // over groups of G lanes, the same in each
+  __device__ __forceinline__ void join_lanes() {
+    float to = m4;
+#pragma unroll
+    for (int k = G / 2; k > 0; k >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, k));
+    if (m4 != to) move(to);
 #pragma unroll
     for (int k = G / 2; k > 0; k >>= 1) {
-      const float om = __shfl_xor_sync(0xFFFFFFFFu, m4, k), os = __shfl_xor_sync(0xFFFFFFFFu, s, k), oq = __shfl_xor_sync(0xFFFFFFFFu, q, k);
-      join(om, os, oq);
+      s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
+      q += __shfl_xor_sync(0xFFFFFFFFu, q, k);
     }
   }
 };
@@ -126,7 +161,7 @@ struct LogRow {
   float l2;                                 // log2 s
   bool none;                                // nothing but -inf
   __device__ __forceinline__ explicit LogRow(const LogSum& sum) : t(sum), l2(log2f(sum.s)), none(sum.s == 0.f) {}
-  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far() ? (l2 == l2 ? t.m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, t.m4, l2) * LP_LN2; }
+  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far ? (l2 == l2 ? t.m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, t.m4, l2) * LP_LN2; }
   __device__ __forceinline__ float logp(float x, float c, float c4) const {
     if (none) return neg_inf();
     if (!(fabsf(x) < 1e30f)) return (__fmul_rn(x, c4) - t.m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
@@ -144,7 +179,7 @@ struct LogGrad {
   float c, c4, o, m4, l2, a, b, g;
   bool far, none;
   __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow& r, float g_, float h) {
-    c = k.c; c4 = k.c4; m4 = r.t.m4; l2 = r.l2; far = r.t.far(); none = r.none;
+    c = k.c; c4 = k.c4; m4 = r.t.m4; l2 = r.l2; far = r.t.far; none = r.none;
     o = -fmaf(4.f, m4, l2);
     a = -h * LP_LN2 * k.inv_t;
     b = -(g_ + h * r.entropy()) * k.inv_t;
@@ -154,6 +189,24 @@ struct LogGrad {
     if (none) return 0.f;
     const float lp = max_nan(far ? 4.f * (__fmul_rn(x, c4) - m4) - l2 : fmaf(x, c, o), LP_NONE);
     return exp2_fast(lp) * fmaf(a, lp, b);
+  }
+  template <int T>
+  __device__ __forceinline__ void at8(const Raw8<T>& r, float (&x)[8]) const {
+    if constexpr (T == T_BF16) {
+      if (!far && !none) {
+        Raw8<T> f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f.w[k] = max_nan_bf16x2(r.w[k], LP_LOW_BF16X2);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float lp = fmaf(f.value(e), c, o);
+          x[e] = exp2_fast(lp) * fmaf(a, lp, b);
+        }
+        return;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = at(r.value(e));
   }
 };
 
@@ -242,12 +295,6 @@ struct Slice {
   __device__ __forceinline__ float one(int i) const { return Elem<T>::get(at, i); }
   __device__ __forceinline__ void load(int group, Raw8<T>& r) const { r.load(at, index(group)); }
 };
-template <int T>
-__device__ __forceinline__ void unpack8(const Raw8<T>& r, float (&x)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = r.value(e);
-}
-
 // Calls f(index in the slice, logit) for the elements of thread t's share
 template <int T, int NT, typename F>
 __device__ __forceinline__ void each_of_share(const Slice<T>& sl, int t, F f) {
@@ -267,6 +314,7 @@ struct LogpShared {
   float row[4];                                      // the block's own sums, for the others of the cluster
   unsigned long long list[LP_LIST], best[LP_MAX_TOP], pick[NT / 32];
   int share[NT], shares, listed;
+  uint32_t bound;
 };
 
 __device__ __forceinline__ unsigned long long rank_word(uint32_t key, uint32_t index) { return (unsigned long long)key << 32 | (0xFFFFFFFFu - index); }
@@ -287,16 +335,35 @@ __device__ __forceinline__ void rank_words(const unsigned long long* words, int 
 
 template <int T, int NT>
 __device__ __noinline__ void top_of_slice(LogpShared<NT>& sh, const Slice<T>& sl, uint32_t first, int top, uint32_t kmax) {
-  constexpr int SHIFT = KeyShift<T>::value;
+  constexpr int SHIFT = KeyShift<T>::value, PER = NT / 32;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) sh.shares = sh.listed = 0;
-  uint32_t bound = 0;
-  for (int bit = 31 - SHIFT; bit >= 0; --bit) {
-    const uint32_t trial = bound | 1u << bit;
-    if (__syncthreads_count((kmax >> SHIFT) >= trial) >= top) bound = trial;
-  }
-  if (kmax != 0u && (kmax >> SHIFT) >= bound) sh.share[atomicAdd(&sh.shares, 1)] = tid;
+  sh.share[tid] = (int)(kmax >> SHIFT);                                 // not zero where there is a logit
+  if (tid == 0) sh.listed = 0;
   __syncthreads();
+  if (warp == 0) {                       // one warp finds the bound, bit by bit, and the shares that reach it
+    uint32_t key[PER], bound = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = (uint32_t)sh.share[32 * i + lane];
+    for (int bit = 31 - SHIFT; bit >= 0; --bit) {
+      const uint32_t trial = bound | 1u << bit;
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) n += key[i] >= trial ? 1 : 0;
+      if ((int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)n) >= top) bound = trial;
+    }
+    int n = 0;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const bool in = key[i] != 0u && key[i] >= bound;
+      const uint32_t who = __ballot_sync(0xFFFFFFFFu, in);
+      if (in) sh.share[n + __popc(who & ((1u << lane) - 1u))] = 32 * i + lane;
+      n += __popc(who);
+    }
+    if (lane == 0) { sh.shares = n; sh.bound = bound; }
+  }
+  __syncthreads();
+  const uint32_t bound = sh.bound;
   auto list = [&](int i, float x) {
     const uint32_t key = logit_key(x);
     if ((key >> SHIFT) >= bound) {
@@ -349,7 +416,7 @@ __device__ __noinline__ void top_of_slice(LogpShared<NT>& sh, const Slice<T>& sl
 }
 
 template <int T, int NT>
-__global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ LogpArgs a, int slices, int slice_len) {
+__global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __grid_constant__ LogpArgs a, int slices, int slice_len) {
   __shared__ LogpShared<NT> sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long row = blockIdx.x / (unsigned)slices;
@@ -358,15 +425,11 @@ __global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ Lo
   const Slice<T> sl(a.x, row * a.ld + first, (int)max(0ll, min((long long)slice_len, a.vocab - first)));
 
   LogSum t;
-  uint32_t kmax = 0;
-  auto some = [&](const float (&x)[8]) {
-    const float most = t.take(x, a.c, a.c4);
-    if (a.top) kmax = max(kmax, logit_key(most));
-  };
+  float most = neg_inf();                                              // of the thread's share
+  auto some = [&](const Raw8<T>& r) { most = max_nan(most, t.template take8<T>(r, a.c, a.c4)); };
   auto single = [&](float v) {
     const float x[1] = {v};
-    t.take(x, a.c, a.c4);
-    if (a.top) kmax = max(kmax, logit_key(v));
+    most = max_nan(most, t.take(x, a.c, a.c4));
   };
   if (tid < sl.head) single(sl.one(tid));
   if (tid < sl.tail) single(sl.one(sl.tail_index() + tid));
@@ -377,34 +440,34 @@ __global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ Lo
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) sl.load(g + k * NT, r[k]);
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      float x[8];
-      unpack8<T>(r[k], x);
-      some(x);
-    }
+    for (int k = 0; k < AHEAD; ++k) some(r[k]);
   }
   for (; g < sl.groups; g += NT) {
     Raw8<T> r;
     sl.load(g, r);
-    float x[8];
-    unpack8<T>(r, x);
-    some(x);
+    some(r);
   }
   t.join_lanes<32>();
   if (lane == 0) { sh.m4[warp] = t.m4; sh.s[warp] = t.s; sh.q[warp] = t.q; }
   __syncthreads();
-  t = LogSum();
-  for (int w = 0; w < NT / 32; ++w) t.join(sh.m4[w], sh.s[w], sh.q[w]);
-  if (a.top) top_of_slice<T, NT>(sh, sl, (uint32_t)first, a.top, kmax);
+  constexpr int WARPS = NT / 32;
+  t = LogSum();                                                          // every warp joins the warps' sums: the same in all
+  if (lane < WARPS) { t.set(sh.m4[lane]); t.s = sh.s[lane]; t.q = sh.q[lane]; }
+  t.join_lanes<32>();
+  if (a.top) {
+    const bool any = tid < sl.groups || tid < sl.head || tid < sl.tail;
+    top_of_slice<T, NT>(sh, sl, (uint32_t)first, a.top, any ? logit_key(most) : 0u);
+  }
   if (slices > 1) {
     if (tid == 0) { sh.row[0] = t.m4; sh.row[1] = t.s; sh.row[2] = t.q; }
     __syncthreads();
     cluster_sync_all();
     t = LogSum();
-    for (int k = 0; k < slices; ++k) {
-      const uint32_t from = cluster_addr(smem_addr(sh.row), (uint32_t)k);
-      t.join(ld_cluster1(from), ld_cluster1(from + 4), ld_cluster1(from + 8));
+    if (lane < slices) {
+      const uint32_t from = cluster_addr(smem_addr(sh.row), (uint32_t)lane);
+      t.set(ld_cluster1(from)); t.s = ld_cluster1(from + 4); t.q = ld_cluster1(from + 8);
     }
+    t.join_lanes<32>();
     if (a.top && part == 0) {
       for (int i = tid; i < slices * a.top; i += NT)
         sh.list[i] = ld_cluster64(cluster_addr(smem_addr(sh.best + i % a.top), (uint32_t)(i / a.top)));
@@ -429,7 +492,7 @@ __global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ Lo
     if (slices > 1) cluster_sync_all();
     else __syncthreads();
     const LogGrad d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
-    const long long tok = token - first;
+    const int tok = token >= first && token < first + sl.n ? (int)(token - first) : -1;
     char* out = static_cast<char*>(a.out) + (row * a.ldo + first) * Elem<T>::bytes;
     const bool wide = ((reinterpret_cast<uintptr_t>(out) + sl.head * Elem<T>::bytes) & 15) == 0;
     auto put = [&](int i, float x) { Elem<T>::put(out, i, d.at(x) + (i == tok ? d.g : 0.f)); };
@@ -445,10 +508,8 @@ __global__ void __launch_bounds__(NT) logp_row_kernel(const __grid_constant__ Lo
         if (g + k * NT >= sl.groups) break;
         const int at = sl.index(g + k * NT);
         float x[8];
-        unpack8<T>(raw[k], x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = d.at(x[e]);
-        if (tok >= at && tok < at + 8) {
+        d.at8(raw[k], x);
+        if ((unsigned)(tok - at) < 8u) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] += at + e == tok ? d.g : 0.f;
         }

@@ -220,6 +220,10 @@ template <> struct Raw8<T_F32> {
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = e < n ? static_cast<const uint32_t*>(p)[i + e] : 0u;
   }
+  __device__ __forceinline__ void load_apart(const void* p, long long i, int step, int n) {     // i, i + step, ...
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = e < n ? static_cast<const uint32_t*>(p)[i + e * step] : 0u;
+  }
   __device__ __forceinline__ float value(int e) const { return __uint_as_float(w[e]); }
   __device__ __forceinline__ uint32_t amax() const {
     float v[8];
@@ -244,6 +248,13 @@ template <int T> struct Raw16 {      // bf16 and fp16: two elements a word
     for (int k = 0; k < 4; ++k) {
       const uint32_t lo = 2 * k < n ? static_cast<const uint16_t*>(p)[i + 2 * k] : 0u, hi = 2 * k + 1 < n ? static_cast<const uint16_t*>(p)[i + 2 * k + 1] : 0u;
       w[k] = lo | hi << 16;
+    }
+  }
+  __device__ __forceinline__ void load_apart(const void* p, long long i, int step, int n) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint16_t* q = static_cast<const uint16_t*>(p) + i + 2 * k * step;
+      w[k] = (2 * k < n ? q[0] : 0u) | (2 * k + 1 < n ? (uint32_t)q[step] : 0u) << 16;
     }
   }
   __device__ __forceinline__ float value(int e) const {

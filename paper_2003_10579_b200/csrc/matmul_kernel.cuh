@@ -32,114 +32,260 @@ struct MmArgs {
   const void* res;
   void* c;
   long long ldr, ldc;
-  int vec_c, vec_r, vec_b;    // four neighbours at once
+  int vec_c, vec_r, vec_b;    // rows on 16-byte boundaries (vec_c 2: on 32-byte ones)
 };
 
-// ---- the tail, on four neighbours of a row --------------------------------------------------------------------------------------
-template <int T>
-__device__ __forceinline__ void load4(const void* p, long long i, float (&v)[4]) {     // aligned to four elements
+// ---- the tail -----------------------------------------------------------------------------------------------------------------------
+// A lane holds 32 columns of its row, as tensor memory gives them: a block of the 8-bit form needs no exchange between lanes, and a lane
+// reads and writes whole 32-byte sectors.  (Four columns a lane through shared memory, so that a warp accesses one row at a time, took three
+// times the instructions: 1531 x 2731 outputs 2.1 us plain, 6.2 us with silu and the 8-bit form, against XXX and XXX.)
+// Rows off 16-byte boundaries go through a patch of shared memory of the warp's own, sixteen words a row, so that lanes access neighbours.
+constexpr int MM_PATCH = 32 * 17 * 4;            // a multiple of 16: bias is read from it four at a time
+
+// 16 words a lane, 32 columns of a 16-bit type or 16 of fp32, to or from rows at any alignment of their elements
+template <int T, bool WRITE>
+__device__ __forceinline__ void mm_patch_rows(uint32_t* patch, int lane, uint32_t (&w)[16], void* rows, long long ld, long long row0, long long n_rows, long long col0, long long n_cols) {
+  if (WRITE) {
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 16; ++j) patch[lane * 17 + j] = w[j];
+  }
+  __syncwarp();
+  // a warp a row of 32 elements of 16 bits, or two rows of 16 of fp32
+  constexpr int STEP = T == T_F32 ? 2 : 1;
+  const int r0 = T == T_F32 ? lane >> 4 : 0, c = T == T_F32 ? lane & 15 : lane;
+  const int left = col0 + c < n_cols ? (int)min(32ll, n_rows - row0) : 0;
+  const long long first = (row0 + r0) * ld + col0 + c, step = STEP * ld;
   if (T == T_F32) {
-    const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  } else {
-    const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
-    if (T == T_BF16) {
-      v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xFFFF0000u); v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xFFFF0000u);
-    } else {
-      v[0] = f16_to_float(a.x & 0xFFFFu); v[1] = f16_to_float(a.x >> 16); v[2] = f16_to_float(a.y & 0xFFFFu); v[3] = f16_to_float(a.y >> 16);
+    uint32_t* at = static_cast<uint32_t*>(rows) + first;
+    uint32_t* in = patch + r0 * 17 + c;
+#pragma unroll 4
+    for (int r = r0; r < left; r += STEP, at += step, in += STEP * 17) {
+      if (WRITE) *at = *in;
+      else *in = *at;
     }
+  } else {
+    uint16_t* at = static_cast<uint16_t*>(rows) + first;
+    uint16_t* in = reinterpret_cast<uint16_t*>(patch + r0 * 17) + c;
+#pragma unroll 8
+    for (int r = r0; r < left; r += STEP, at += step, in += STEP * 34) {
+      if (WRITE) *at = *in;
+      else *in = *at;
+    }
+  }
+  __syncwarp();
+  if (!WRITE) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = patch[lane * 17 + j];
+    __syncwarp();
+  }
+}
+__device__ __forceinline__ void load16(const void* p, uint32_t (&w)[16]) {
+  const uint4* q = static_cast<const uint4*>(p);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { const uint4 a = q[k]; w[4 * k] = a.x; w[4 * k + 1] = a.y; w[4 * k + 2] = a.z; w[4 * k + 3] = a.w; }
+}
+// 64 bytes on a boundary of 16 (sectors: of 32)
+__device__ __forceinline__ void store16(void* p, const uint32_t (&w)[16], bool sectors) {
+  if (sectors) {
+    const uint32_t a[8] = {w[0], w[1], w[2], w[3], w[4], w[5], w[6], w[7]}, b[8] = {w[8], w[9], w[10], w[11], w[12], w[13], w[14], w[15]};
+    store32(p, a);
+    store32(static_cast<char*>(p) + 32, b);
+  } else {
+    uint4* q = static_cast<uint4*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) q[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
   }
 }
 template <int T>
-__device__ __forceinline__ void store4(void* p, long long i, const float (&v)[4]) {
-  if (T == T_F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
-  else if (T == T_BF16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(float_to_bf16x2(v[0], v[1]), float_to_bf16x2(v[2], v[3]));
-  else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) = make_uint2(float_to_f16x2(v[0], v[1]), float_to_f16x2(v[2], v[3]));
+__device__ __forceinline__ float half_value(uint32_t w, int odd) {       // of two 16-bit elements in a word
+  if (T == T_BF16) return __uint_as_float(odd ? w & 0xFFFF0000u : w << 16);
+  return f16_to_float(odd ? w >> 16 : w & 0xFFFFu);
 }
-template <int T>
-__device__ __forceinline__ void load4_of(const void* p, long long i, int n, bool vec, float (&v)[4]) {   // n of them exist
-  if (vec && n >= 4) load4<T>(p, i, v);
-  else
+template <int ACT>
+__device__ __forceinline__ void act_row(float (&v)[32]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = e < n ? Elem<T>::get(p, i + e) : 0.f;
+  for (int j = 0; j < 32; ++j) v[j] = act_value<ACT>(v[j]);
+}
+template <int ACT>
+__device__ __forceinline__ void slope_row(float (&v)[32], const uint4& a, const uint4& b, float scale) {
+  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float z[4];
+    ckpt_values4(w[k], scale, z);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * k + e] *= act_slope<ACT>(z[e]);
+  }
 }
 
-// What the tail of four elements at (row, col) reads besides the sum
-struct MmTail {
-  float r[4];
-  uint32_t z;
-  uint8_t zs;
-};
+// One element of bias as it is stored, and its value
+__device__ __forceinline__ uint32_t mm_bias_raw(const MmArgs& g, long long col) {
+  if (!g.bias || col >= g.N) return 0u;
+  return g.bias_type == T_F32 ? static_cast<const uint32_t*>(g.bias)[col] : static_cast<const uint16_t*>(g.bias)[col];
+}
+__device__ __forceinline__ float mm_bias_value(const MmArgs& g, uint32_t raw) {
+  return g.bias_type == T_F32 ? __uint_as_float(raw) : g.bias_type == T_BF16 ? __uint_as_float(raw << 16) : f16_to_float(raw);
+}
 template <int T>
-__device__ __forceinline__ void mm_tail_load(const MmArgs& g, long long row, long long col, MmTail& t) {
-  const int n = row < g.M ? (int)max(0ll, min(4ll, g.N - col)) : 0;
-  if (g.res) load4_of<T>(g.res, row * g.ldr + col, n, g.vec_r, t.r);
-  if (g.grad && n > 0) {
-    const long long blocks = (g.N + 31) >> 5;
-    t.z = *reinterpret_cast<const uint32_t*>(g.z_codes + row * blocks * 32 + col);
-    t.zs = g.z_scales[row * blocks + (col >> 5)];
-  }
-}
-template <int ACT>
-__device__ __forceinline__ void act4(float (&v)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = act_value<ACT>(v[e]);
-}
-template <int ACT>
-__device__ __forceinline__ void slope4(float (&v)[4], const float (&z)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] *= act_slope<ACT>(z[e]);
-}
-// Every lane of the warp takes part; eight neighbouring lanes hold a block of 32 columns.  col is a multiple of four.
+__device__ __forceinline__ uint32_t raw_of(const void* p, long long i) { return T == T_F32 ? static_cast<const uint32_t*>(p)[i] : static_cast<const uint16_t*>(p)[i]; }
 template <int T>
-__device__ __forceinline__ void mm_tail(const MmArgs& g, long long row, long long col, float (&v)[4], const MmTail& t) {
-  const int n = row < g.M ? (int)max(0ll, min(4ll, g.N - col)) : 0;
-  if (g.grad) {
-    if (n > 0) {
-      float z[4];
-      ckpt_values4(t.z, scale_value(t.zs), z);
-      if (g.act == ACT_RELU) slope4<ACT_RELU>(v, z);
-      else if (g.act == ACT_GELU) slope4<ACT_GELU>(v, z);
-      else if (g.act == ACT_SILU) slope4<ACT_SILU>(v, z);
+__device__ __forceinline__ float value_of(uint32_t raw) { return T == T_F32 ? __uint_as_float(raw) : half_value<T>(raw, 0); }
+
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+// Asks L2 for what the tail will read of 32 x 32 elements
+template <int T>
+__device__ __forceinline__ void mm_ahead(const MmArgs& g, long long row, long long col0) {
+  if (row >= g.M || col0 >= g.N) return;
+  if (g.res) prefetch_l2(static_cast<const char*>(g.res) + (row * g.ldr + col0) * Elem<T>::bytes);
+  if (g.grad) prefetch_l2(g.z_codes + (row * ((g.N + 31) >> 5) << 5) + col0);
+}
+
+// Of a warp's 32 rows from row0 on, the 32 columns from col0 on (a multiple of 32).  Every lane takes part, whatever exists.  Made before the sums are read:
+// what else the tail reads is then under way, and stays as it is stored (a conversion would wait for it).  Asking for it a chunk ahead, in registers,
+// cost more in moves than it hid; instead L2 is asked for a tile's lines while the products run (mm_ahead).
+template <int T>
+struct MmRows {
+  long long row, row0, col0;
+  int cols;                                  // of the 32 that exist; none in a row behind the last
+  bool wide_res;
+  uint4 za, zb;
+  uint32_t zs, bias;                         // bias: of column col0 + lane
+  uint32_t r[T == T_F32 ? 32 : 16];
+  __device__ __forceinline__ MmRows() {}
+  __device__ __forceinline__ MmRows(const MmArgs& g, long long row0_, long long col0_, int lane, uint32_t bias_) : row(row0_ + lane), row0(row0_), col0(col0_), bias(bias_) {
+    cols = row < g.M ? (int)max(0ll, min(32ll, g.N - col0)) : 0;
+    if (g.grad && cols > 0) {
+      const long long at = row * ((g.N + 31) >> 5) + (col0 >> 5);
+      const uint4* codes = reinterpret_cast<const uint4*>(g.z_codes + 32 * at);
+      za = codes[0]; zb = codes[1];
+      zs = g.z_scales[at];
     }
-  } else {
-    if (g.bias && n > 0) {
-      float b[4];
-      if (g.bias_type == T_F32) load4_of<T_F32>(g.bias, col, n, g.vec_b, b);
-      else if (g.bias_type == T_BF16) load4_of<T_BF16>(g.bias, col, n, g.vec_b, b);
-      else load4_of<T_F16>(g.bias, col, n, g.vec_b, b);
+    wide_res = g.vec_r && col0 + 32 <= g.N;
+    if (g.res && wide_res && cols > 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += b[e];
-    }
-    if (g.z_codes) {
+      for (int h = 0; h < (T == T_F32 ? 2 : 1); ++h) {
+        uint32_t w[16];
+        load16(static_cast<const char*>(g.res) + (row * g.ldr + col0 + 16 * h) * Elem<T>::bytes, w);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = e < n ? v[e] : 0.f;
-      uint32_t most = __float_as_uint(max3_abs(max3_abs(v[0], v[1], v[2]), v[3], 0.f)) & ABS_MASK;
-#pragma unroll
-      for (int k = 1; k < 8; k <<= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, k));
-      const uint32_t code = scale_code_e4m3(most);
-      const float inv = scale_inverse(code);
-      const long long blocks = (g.N + 31) >> 5;
-      if (row < g.M && col < 32 * blocks) {
-        *reinterpret_cast<uint32_t*>(g.z_codes + row * blocks * 32 + col) = to_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-        if ((col & 31) == 0) g.z_scales[row * blocks + (col >> 5)] = (uint8_t)code;
+        for (int j = 0; j < 16; ++j) r[16 * h + j] = w[j];
       }
     }
-    if (g.act == ACT_RELU) act4<ACT_RELU>(v);
-    else if (g.act == ACT_GELU) act4<ACT_GELU>(v);
-    else if (g.act == ACT_SILU) act4<ACT_SILU>(v);
   }
-  if (n <= 0) return;
-  if (g.res) {
+  __device__ __forceinline__ void finish(const MmArgs& g, float (&v)[32], int lane, uint32_t* patch) {
+    if (g.grad) {
+      if (cols > 0) {
+        const float scale = scale_value(zs);
+        if (g.act == ACT_RELU) slope_row<ACT_RELU>(v, za, zb, scale);
+        else if (g.act == ACT_GELU) slope_row<ACT_GELU>(v, za, zb, scale);
+        else if (g.act == ACT_SILU) slope_row<ACT_SILU>(v, za, zb, scale);
+      }
+    } else {
+      if (g.bias) {                          // each lane's column to all lanes
+        __syncwarp();
+        patch[lane] = __float_as_uint(mm_bias_value(g, bias));
+        __syncwarp();
+        const float4* q = reinterpret_cast<const float4*>(patch);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] += t.r[e];
+        for (int k = 0; k < 8; ++k) { const float4 c = q[k]; v[4 * k] += c.x; v[4 * k + 1] += c.y; v[4 * k + 2] += c.z; v[4 * k + 3] += c.w; }
+        __syncwarp();
+      }
+      if (g.z_codes) {
+        if (cols < 32) {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = j < cols ? v[j] : 0.f;      // the tail of a row of codes is zero
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) most = max3_abs(most, v[j], v[j + 1]);
+        const uint32_t code = scale_code_e4m3(__float_as_uint(most) & ABS_MASK);
+        const float inv = scale_inverse(code);
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = to_e4m3x4(v[4 * k] * inv, v[4 * k + 1] * inv, v[4 * k + 2] * inv, v[4 * k + 3] * inv);
+        if (cols > 0) {
+          const long long at = row * ((g.N + 31) >> 5) + (col0 >> 5);
+          uint4* to = reinterpret_cast<uint4*>(g.z_codes + 32 * at);
+          to[0] = make_uint4(w[0], w[1], w[2], w[3]);
+          to[1] = make_uint4(w[4], w[5], w[6], w[7]);
+          g.z_scales[at] = (uint8_t)code;
+        }
+      }
+      if (g.act == ACT_RELU) act_row<ACT_RELU>(v);
+      else if (g.act == ACT_GELU) act_row<ACT_GELU>(v);
+      else if (g.act == ACT_SILU) act_row<ACT_SILU>(v);
+    }
+    if (g.res) {
+      if (!wide_res) {
+#pragma unroll
+        for (int h = 0; h < (T == T_F32 ? 2 : 1); ++h) {
+          uint32_t w[16];
+          mm_patch_rows<T, false>(patch, lane, w, const_cast<void*>(g.res), g.ldr, row0, g.M, col0 + 16 * h, g.N);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) r[16 * h + j] = w[j];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 32; ++j) v[j] += T == T_F32 ? __uint_as_float(r[j]) : half_value<T>(r[T == T_F32 ? 0 : j >> 1], j & 1);
+    }
+    const bool wide = g.vec_c && col0 + 32 <= g.N;
+#pragma unroll
+    for (int h = 0; h < (T == T_F32 ? 2 : 1); ++h) {
+      uint32_t w[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        w[j] = T == T_F32 ? __float_as_uint(v[(16 * h + j) & 31]) : T == T_BF16 ? float_to_bf16x2(v[2 * j], v[2 * j + 1]) : float_to_f16x2(v[2 * j], v[2 * j + 1]);
+      if (!wide) mm_patch_rows<T, true>(patch, lane, w, g.c, g.ldc, row0, g.M, col0 + 16 * h, g.N);
+      else if (cols > 0) store16(static_cast<char*>(g.c) + (row * g.ldc + col0 + 16 * h) * Elem<T>::bytes, w, g.vec_c == 2);
+    }
   }
-  if (g.vec_c && n == 4) store4<T>(g.c, row * g.ldc + col, v);
-  else
+};
+
+// With the operands swapped a lane holds one column of eight of the few rows; 32 lanes are a block of the 8-bit form, and neighbours.
+template <int T>
+struct MmFew {
+  long long row0, col;
+  uint32_t r[8], z[8], zs[8], bias;
+  __device__ __forceinline__ MmFew() {}
+  __device__ __forceinline__ MmFew(const MmArgs& g, long long row0_, long long col_, uint32_t bias_) : row0(row0_), col(col_), bias(bias_) {
+    const long long blocks = (g.N + 31) >> 5;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < n) Elem<T>::put(g.c, row * g.ldc + col + e, v[e]);
-}
+    for (int j = 0; j < 8; ++j) {
+      const bool here = col < g.N && row0 + j < g.M;
+      if (g.res && here) r[j] = raw_of<T>(g.res, (row0 + j) * g.ldr + col);
+      if (g.grad && here) { z[j] = g.z_codes[(row0 + j) * blocks * 32 + col]; zs[j] = g.z_scales[(row0 + j) * blocks + (col >> 5)]; }
+    }
+  }
+  __device__ __forceinline__ void finish(const MmArgs& g, float (&v)[8]) {
+    const bool in = col < g.N;
+    if (!g.grad) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += mm_bias_value(g, bias);
+      if (g.z_codes) {
+        const long long blocks = (g.N + 31) >> 5;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float x = in ? v[j] : 0.f;
+          const uint32_t code = scale_code_e4m3(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(x) & ABS_MASK));
+          if (row0 + j < g.M && col < 32 * blocks) {
+            g.z_codes[(row0 + j) * blocks * 32 + col] = (uint8_t)to_e4m3x2(x * scale_inverse(code), 0.f);
+            if ((col & 31) == 0) g.z_scales[(row0 + j) * blocks + (col >> 5)] = (uint8_t)code;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (!in || row0 + j >= g.M) continue;
+      const float at = g.grad ? from_e4m3x2(z[j]).x * scale_value(zs[j]) : v[j];
+      if (g.act == ACT_RELU) v[j] = g.grad ? v[j] * act_slope<ACT_RELU>(at) : act_value<ACT_RELU>(at);
+      else if (g.act == ACT_GELU) v[j] = g.grad ? v[j] * act_slope<ACT_GELU>(at) : act_value<ACT_GELU>(at);
+      else if (g.act == ACT_SILU) v[j] = g.grad ? v[j] * act_slope<ACT_SILU>(at) : act_value<ACT_SILU>(at);
+      if (g.res) v[j] += value_of<T>(r[j]);
+      Elem<T>::put(g.c, (row0 + j) * g.ldc + col, v[j]);
+    }
+  }
+};
 
 // ---- loads and instructions ---------------------------------------------------------------------------------------------------------
 // fp32 accumulators; bf: bf16 operands (else fp16); m, n: the instruction's shape
@@ -167,14 +313,16 @@ __device__ __forceinline__ void mm_mma_pair(uint32_t d, uint64_t adesc, uint64_t
 // ---- a 128 x BN tile a block --------------------------------------------------------------------------------------------------------
 //   warp 0     producer: TMA loads into the ring
 //   warp 1     allocates tensor memory; one lane issues the MMAs
-//   warps 2-5  accumulators from tensor memory to shared memory (over the ring, which every MMA has read by then)
-//   all        the tail; in a cluster each block adds its share of the tile over the blocks, in their order: the same bits each time
-constexpr int MM_THREADS = 192, MM_MAX_STAGES = 8, MM_A_BYTES = 16384;
-__host__ __device__ constexpr int mm_pitch(int bn, bool swap) { return swap ? 132 : bn + 4; }     // floats between lines of partial sums
+//   all eight  the tail, each 32 lanes of tensor memory and half of the columns.  In a cluster the sums go to shared memory (over the ring, which
+//              every MMA has read by then), and each block takes its share of the tile over the blocks, in their order: the same bits every time
+constexpr int MM_THREADS = 256, MM_MAX_STAGES = 12, MM_A_BYTES = 16384;
+constexpr int MM_RING = 98304, MM_RING_WIDE = 2 * MM_RING;      // bytes, with what else there is: for two blocks to a multiprocessor, for one
+constexpr int MM_OFF_PATCH = MM_RING - 8 * MM_PATCH;            // the warps' patches, behind the sums
+__host__ __device__ constexpr int mm_pitch(int bn, bool swap) { return swap ? 132 : bn + 4; }     // floats between lines of sums: rows, or (swap) columns of tensor memory
 __host__ __device__ constexpr int mm_part_bytes(int bn, bool swap) { return (swap ? bn : 128) * mm_pitch(bn, swap) * 4; }
 
 template <int BN, int T, bool SWAP, bool SPLIT>
-__global__ void __launch_bounds__(MM_THREADS) mm_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmArgs g) {
+__global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmArgs g) {
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) unsigned long long bars_s[2 * MM_MAX_STAGES + 1];
   __shared__ uint32_t tmem_slot;
@@ -205,7 +353,6 @@ __global__ void __launch_bounds__(MM_THREADS) mm_tile_kernel(const __grid_consta
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   bool failed = false;
-
   if (warp == 0) {
     if (lane == 0) {
       int s = 0, issued = 0;
@@ -249,80 +396,135 @@ __global__ void __launch_bounds__(MM_THREADS) mm_tile_kernel(const __grid_consta
       if (it == n_it - 1) tc_commit_elected(acc_bar);
       if (++s == g.stages) { s = 0; phase ^= 1u; }
     }
-  } else {
-    if (n_it > 0 && !mbar_wait_warp(acc_bar, 0)) failed = true;
-    tc_fence_after();
-    const int q = warp & 3, row = 32 * q + lane;
-    const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16);
-    float* part = reinterpret_cast<float*>(base_p);
-    constexpr int CH = BN < 32 ? 16 : 32;
+  }
+  __syncwarp();
+  const int q = warp & 3, half = warp >> 2;
+  const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16);
+  uint32_t* patch = reinterpret_cast<uint32_t*>(base_p + MM_OFF_PATCH + warp * MM_PATCH);
+  float* part = reinterpret_cast<float*>(base_p);
+  constexpr int PITCH = mm_pitch(BN, SWAP), CHUNKS = SWAP ? BN / 8 : BN / 32, WIDTH = BN / CHUNKS;     // columns of tensor memory, 8 or 32 at a time
+  // what the tail reads besides the sums: of the lane's column (SWAP) or of the 32 columns of each of the warp's chunks, before the wait
+  uint32_t bias[2] = {0u, 0u};
+  if (SWAP) bias[0] = mm_bias_raw(g, a0 + 32 * q + lane);
+  else
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (half + 2 * i < CHUNKS) {
+        bias[i] = mm_bias_raw(g, b0 + 32 * (half + 2 * i) + lane);
+        if (!SPLIT) mm_ahead<T>(g, a0 + 32 * q + lane, b0 + 32 * (half + 2 * i));
+      }
+  if (n_it > 0 && !mbar_wait_warp_long(acc_bar, 0)) failed = true;
+  tc_fence_after();
 #pragma unroll 1
-    for (int ch = 0; ch < BN / CH; ++ch) {
-      uint32_t v[32];
-      if (CH == 32) {
-        tc_ld32_async(trow + ch * 32, v);
-      } else {
-        asm volatile(
-            "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-            : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-              "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(trow));
-      }
-      tc_ld_wait();
-      if (failed || n_it == 0) {                                  // no k at all: sums of nothing
+  for (int ch = half; ch < CHUNKS; ch += 2) {
+    if (SWAP && b0 + 8 * ch >= g.M) break;
+    MmFew<T> few;
+    MmRows<T> rows;
+    if constexpr (!SPLIT && SWAP) few = MmFew<T>(g, b0 + 8 * ch, a0 + 32 * q + lane, bias[0]);
+    if constexpr (!SPLIT && !SWAP) rows = MmRows<T>(g, a0 + 32 * q, b0 + 32 * ch, lane, ch == half ? bias[0] : bias[1]);
+    float v[WIDTH];
+    uint32_t w[WIDTH];
+    if constexpr (SWAP) tc_ld8_async(trow + 8 * ch, w);
+    else tc_ld32_async(trow + 32 * ch, w);
+    tc_ld_wait();
 #pragma unroll
-        for (int j = 0; j < CH; ++j) v[j] = failed ? 0x7FC00000u : 0u;
-      }
-      if (SWAP) {
+    for (int j = 0; j < WIDTH; ++j) v[j] = __uint_as_float(failed ? 0x7FC00000u : n_it == 0 ? 0u : w[j]);       // no k at all: sums of nothing
+    if constexpr (SPLIT && SWAP) {
 #pragma unroll
-        for (int j = 0; j < CH; ++j) part[(ch * CH + j) * mm_pitch(BN, SWAP) + row] = __uint_as_float(v[j]);
-      } else {
+      for (int j = 0; j < 8; ++j) part[(8 * ch + j) * PITCH + 32 * q + lane] = v[j];
+    } else if constexpr (SPLIT) {
 #pragma unroll
-        for (int j = 0; j < CH; j += 4) *reinterpret_cast<uint4*>(part + row * mm_pitch(BN, SWAP) + ch * CH + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-      }
+      for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(part + (32 * q + lane) * PITCH + 32 * ch + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+    } else if constexpr (SWAP) {
+      few.finish(g, v);
+    } else {
+      rows.finish(g, v, lane, patch);
     }
+  }
+  if constexpr (SPLIT) {
+    // chunks of 32 lanes, dealt to the blocks and then to their warps
+    const int rank = (int)cluster_rank(), n = (int)gridDim.y, tasks = 4 * (SWAP ? (int)min((long long)CHUNKS, (g.M - b0 + 7) / 8) : CHUNKS);     // of rows that exist
+    int task = rank + n * warp;
+    auto ahead = [&]() {                                                             // under way while the blocks meet
+      if (task >= tasks) return 0u;
+      if (!SWAP) mm_ahead<T>(g, a0 + 32 * (task & 3) + lane, b0 + 32 * (task >> 2));
+      return mm_bias_raw(g, SWAP ? a0 + 32 * (task & 3) + lane : b0 + 32 * (task >> 2) + lane);
+    };
+    uint32_t raw = ahead();
+    __syncthreads();
+    cluster_sync_all();
+#pragma unroll 1
+    while (task < tasks) {
+      const int tq = task & 3, ch = task >> 2;
+      if constexpr (SWAP) {
+        MmFew<T> few(g, b0 + 8 * ch, a0 + 32 * tq + lane, raw);
+        const uint32_t from = base + 4u * (uint32_t)(8 * ch * PITCH + 32 * tq + lane);
+        float v[8], p[4][8];                                                         // four blocks at a time
+#pragma unroll 1
+        for (int r = 0; r < n; r += 4) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (r + k < n) {
+              const uint32_t at = cluster_addr(from, (uint32_t)(r + k));
+#pragma unroll
+              for (int j = 0; j < 8; ++j) p[k][j] = ld_cluster1(at + 4u * (uint32_t)(j * PITCH));
+            }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (r + k < n) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = r + k == 0 ? p[k][j] : v[j] + p[k][j];
+            }
+        }
+        few.finish(g, v);
+      } else {
+        MmRows<T> rows(g, a0 + 32 * tq, b0 + 32 * ch, lane, raw);
+        // The blocks' sums are read four rows of 128 bytes at a time (a row a lane took twice as long) and left in this block's place of
+        // the chunk, which nobody else reads.
+        const uint32_t at = (uint32_t)((32 * tq + (lane >> 3)) * PITCH + 32 * ch + (lane & 7) * 4);
+#pragma unroll 1
+        for (int k0 = 0; k0 < 8; k0 += 4) {
+          float4 t[4];
+#pragma unroll 1
+          for (int r = 0; r < n; ++r) {
+            const uint32_t from = cluster_addr(base + 4u * at, (uint32_t)r) + 16u * (uint32_t)(PITCH * k0);
+            float4 p[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[k] = ld_cluster4(from + 16u * (uint32_t)(PITCH * k));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = r == 0 ? p[k] : make_float4(t[k].x + p[k].x, t[k].y + p[k].y, t[k].z + p[k].z, t[k].w + p[k].w);
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(part + at + 4 * PITCH * (k0 + k)) = t[k];
+        }
+        __syncwarp();
+        float v[32];
+        const float* mine = part + (32 * tq + lane) * PITCH + 32 * ch;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float4 q4 = *reinterpret_cast<const float4*>(mine + 4 * k);
+          v[4 * k] = q4.x; v[4 * k + 1] = q4.y; v[4 * k + 2] = q4.z; v[4 * k + 3] = q4.w;
+        }
+        rows.finish(g, v, lane, patch);
+      }
+      task += n * (MM_THREADS / 32);
+      raw = ahead();
+    }
+    cluster_sync_all();                  // nobody leaves while its sums may still be read
   }
   tc_fence_before();
   __syncthreads();
-  if (SPLIT) cluster_sync_all();
-
-  // A warp takes a unit of 32 groups of four: a line of 128 columns (SWAP: of one of the few rows), or a few shorter lines
-  const int rank = SPLIT ? (int)cluster_rank() : 0, n = SPLIT ? (int)gridDim.y : 1;
-  constexpr int GROUPS = SWAP ? 32 : BN / 4, LINES = 32 / GROUPS;          // groups of four a line, lines a unit
-  for (int u = BN * rank / n + warp; u < BN * (rank + 1) / n; u += MM_THREADS / 32) {
-    const int line = u * LINES + lane / GROUPS, at = lane % GROUPS * 4;
-    const long long row = SWAP ? b0 + line : a0 + line, col = SWAP ? a0 + at : b0 + at;
-    MmTail t;
-    mm_tail_load<T>(g, row, col, t);
-    const uint32_t where = base + 4u * (uint32_t)(line * mm_pitch(BN, SWAP) + at);
-    float4 s;
-    if (SPLIT) {
-      float4 v[8];
-#pragma unroll
-      for (int r = 0; r < 8; ++r)
-        if (r < n) v[r] = ld_cluster4(cluster_addr(where, (uint32_t)r));
-      s = v[0];
-#pragma unroll
-      for (int r = 1; r < 8; ++r)
-        if (r < n) { s.x += v[r].x; s.y += v[r].y; s.z += v[r].z; s.w += v[r].w; }
-    } else {
-      s = *reinterpret_cast<const float4*>(base_p + (where - base));
-    }
-    float v[4] = {s.x, s.y, s.z, s.w};
-    mm_tail<T>(g, row, col, v, t);
-  }
-  if (SPLIT) cluster_sync_all();          // nobody leaves while its partial sums may still be read
   if (warp == 1) tc_dealloc(tmem, TMEM_COLS);
 }
 
 // ---- two multiprocessors on a 256 x 256 tile -----------------------------------------------------------------------------------------
 //   warp 0      TMA loads (leader's barrier): each block its 128 rows of A and its half of B's
 //   warp 1      tensor memory; in the leader one lane issues the MMAs for both
-//   warps 2-9   the tail: a warp takes 32 rows x 128 columns, 32 columns at a time through its own 4 KB of shared memory, so that every access
-//               to memory is of neighbours
+//   warps 2-9   the tail: a warp takes 32 rows x 128 columns, 32 columns at a time
 // Two sets of accumulators (2 x 256 columns of tensor memory): a tile's tail runs beside the next one's MMAs.
 constexpr int MMP_THREADS = 320, MMP_STAGES = 6, MMP_HALF = 128 * 128, MMP_STAGE = 2 * MMP_HALF;
 constexpr int MMP_OFF_STORE = MMP_STAGES * MMP_STAGE;
-constexpr int MMP_OFF_BARS = MMP_OFF_STORE + 8 * 4096;
+constexpr int MMP_OFF_BARS = MMP_OFF_STORE + 8 * MM_PATCH;
 constexpr int MMP_SMEM = MMP_OFF_BARS + 8 * (2 * MMP_STAGES + 4) + 16 + 1024;
 static_assert(MMP_SMEM <= 227 * 1024, "the ring and the tail's patches must fit");
 
@@ -429,49 +631,38 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     __syncwarp();
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
-    unsigned char* st = base_p + MMP_OFF_STORE + (warp - 2) * 4096;
+    uint32_t* patch = reinterpret_cast<uint32_t*>(base_p + MMP_OFF_STORE + (warp - 2) * MM_PATCH);
     int buf = 0;
     uint32_t phase = 0;
     for (int tile = (int)blockIdx.x >> 1; tile < n_tiles; tile += pairs) {
       int a0, b0;
       tile_at(tile, a0, b0);
-      const long long row0 = a0 + 32 * q + (lane >> 3), col0 = b0 + 128 * half + (lane & 7) * 4;
       const uint32_t trow = tmem + ((uint32_t)(32 * q) << 16) + 256u * buf + 128 * half, done = cluster_addr(acc_empty(buf), 0);
+      a0 += 32 * q;
+      b0 += 128 * half;
+      uint32_t bias[4];
+#pragma unroll
+      for (int ch = 0; ch < 4; ++ch) {
+        bias[ch] = mm_bias_raw(g, b0 + 32 * ch + lane);
+        mm_ahead<T>(g, a0 + lane, b0 + 32 * ch);
+      }
       if (!failed && !mbar_wait_warp_long(acc_full(buf), phase)) failed = true;           // from then on every tile of this block is NaN
       tc_fence_after();
 #pragma unroll 1
       for (int ch = 0; ch < 4; ++ch) {
-        uint32_t v[32];
-        tc_ld32_async(trow + 32 * ch, v);
+        uint32_t w[32];
+        tc_ld32_async(trow + 32 * ch, w);
+        MmRows<T> rows(g, a0, b0 + 32 * ch, lane, ch < 2 ? (ch == 0 ? bias[0] : bias[1]) : ch == 2 ? bias[2] : bias[3]);
         tc_ld_wait();
         if (ch == 3) {                                                          // the accumulators are read: the tile after the next may start
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(done);
         }
-        if (failed) {
+        float v[32];
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0x7FC00000u;
-        }
-        __syncwarp();
-#pragma unroll
-        for (int p = 0; p < 8; ++p)
-          *reinterpret_cast<uint4*>(st + lane * 128 + ((p ^ (lane & 7)) << 4)) = make_uint4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
-        __syncwarp();
-        const long long col = col0 + 32 * ch;
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {                                           // four accesses of four rows each in flight
-          MmTail t[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mm_tail_load<T>(g, row0 + 16 * h + 4 * i, col, t[i]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int r = 16 * h + 4 * i + (lane >> 3);
-            const float4 s = *reinterpret_cast<const float4*>(st + r * 128 + (((lane & 7) ^ (r & 7)) << 4));
-            float x[4] = {s.x, s.y, s.z, s.w};
-            mm_tail<T>(g, row0 + 16 * h + 4 * i, col, x, t[i]);
-          }
-        }
+        for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(failed ? 0x7FC00000u : w[j]);
+        rows.finish(g, v, lane, patch);
       }
       buf ^= 1;
       if (buf == 0) phase ^= 1u;
@@ -486,15 +677,22 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 // ---- operands that TMA cannot read -----------------------------------------------------------------------------------------------------
 // Rows that do not start on 16-byte boundaries are copied to rows that do (cols rounded up to eight elements) before the product: one read
 // and one write more of an operand that the tiles read many times.
-__global__ void __launch_bounds__(256) mm_repack_kernel(const uint16_t* x, long long rows, long long cols, long long ld, uint16_t* out) {
-  const uint32_t pieces = (uint32_t)((cols + 7) / 8);
-  for (PieceWalk at((long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256, pieces); at.row < rows; at.next()) {
-    const long long c = 8ll * at.at;
-    const uint16_t* src = x + at.row * ld + c;
-    uint32_t v[8];
+struct MmRepack {
+  struct One { const uint16_t* x; uint16_t* out; long long rows, cols, ld; } of[2];
+  int n;
+};
+__global__ void __launch_bounds__(256) mm_repack_kernel(const __grid_constant__ MmRepack r) {
+  for (int i = 0; i < r.n; ++i) {
+    const MmRepack::One o = r.of[i];
+    const uint32_t pieces = (uint32_t)((o.cols + 7) / 8);
+    for (PieceWalk at((long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256, pieces); at.row < o.rows; at.next()) {
+      const long long c = 8ll * at.at;
+      const uint16_t* src = o.x + at.row * o.ld + c;
+      uint32_t v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? src[e] : 0u;
-    *reinterpret_cast<uint4*>(out + (at.row * pieces + at.at) * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+      for (int e = 0; e < 8; ++e) v[e] = c + e < o.cols ? src[e] : 0u;
+      *reinterpret_cast<uint4*>(o.out + (at.row * pieces + at.at) * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    }
   }
 }
 

@@ -69,25 +69,41 @@ cudaError_t ckpt_read(const CkptArgs& a, sim_act act, unsigned grid, cudaStream_
   }
   return cudaGetLastError();
 }
+template <int T, int ACT, bool KEPT, bool VEC>
+cudaError_t launch_act_backward(const CkptArgs& a, dim3 grid, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(256, 1, 1);
+  cfg.stream = st;
+  cudaLaunchAttribute attr{};
+  if (a.db && grid.y > 1) {
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1; attr.val.clusterDim.y = grid.y; attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+  }
+  return cudaLaunchKernelEx(&cfg, act_backward_kernel<T, ACT, KEPT, VEC>, a);
+}
+template <int T, bool VEC>
+cudaError_t act_backward_kept(const CkptArgs& a, sim_act act, dim3 grid, cudaStream_t st) {
+  switch (act) {
+    case SIM_ACT_RELU: return launch_act_backward<T, ACT_RELU, true, VEC>(a, grid, st);
+    case SIM_ACT_GELU: return launch_act_backward<T, ACT_GELU, true, VEC>(a, grid, st);
+    case SIM_ACT_SILU: return launch_act_backward<T, ACT_SILU, true, VEC>(a, grid, st);
+    default: return launch_act_backward<T, ACT_NONE, true, VEC>(a, grid, st);
+  }
+}
 template <int T>
 cudaError_t act_backward(const CkptArgs& a, sim_act act, dim3 grid, cudaStream_t st) {
-  if (!a.codes) {
-    act_backward_kernel<T, ACT_NONE, false><<<grid, 256, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-  switch (act) {
-    case SIM_ACT_RELU: act_backward_kernel<T, ACT_RELU, true><<<grid, 256, 0, st>>>(a); break;
-    case SIM_ACT_GELU: act_backward_kernel<T, ACT_GELU, true><<<grid, 256, 0, st>>>(a); break;
-    case SIM_ACT_SILU: act_backward_kernel<T, ACT_SILU, true><<<grid, 256, 0, st>>>(a); break;
-    default: act_backward_kernel<T, ACT_NONE, true><<<grid, 256, 0, st>>>(a);
-  }
-  return cudaGetLastError();
+  if (a.codes) return a.vec ? act_backward_kept<T, true>(a, act, grid, st) : act_backward_kept<T, false>(a, act, grid, st);
+  return a.vec ? launch_act_backward<T, ACT_NONE, false, true>(a, grid, st) : launch_act_backward<T, ACT_NONE, false, false>(a, grid, st);
 }
-// Rows of a block of act_backward_kernel: at least 128 (sixteen a warp), and no more blocks than fill the device a few times over
+// Blocks along the rows: at least 32 rows each (four a warp), up to four (a cluster, whose size is a power of two: clusters of three or seven blocks ran
+// slower than half as many), and from there no more than fill the device a few times over
 int64_t sum_splits(int64_t rows, int64_t cols) {
-  const int64_t strips = (cols + 255) / 256, most = (rows + 127) / 128, want = (8 * 148 + strips - 1) / strips;
+  const int64_t strips = (cols + 255) / 256, most = (rows + 31) / 32, want = (8 * 148 + strips - 1) / strips;
   const int64_t s = most < want ? most : want;
-  return s < 1 ? 1 : s > 65535 ? 65535 : s;
+  return s <= 1 ? 1 : s <= 2 ? 2 : s <= 4 ? 4 : s <= 8 ? 8 : s > 65535 ? 65535 : s;
 }
 
 // ---- products ----------------------------------------------------------------------------------------------------------------
@@ -116,13 +132,23 @@ Operand operand(const void* p, int64_t ld, int t, int64_t along, int64_t k) {
   o.fits = rows_aligned(p, o.rows, ld, SIM_BF16, 16);
   return o;
 }
-cudaError_t repack(Operand& o, char*& room, cudaStream_t st) {
-  if (o.fits) return cudaSuccess;
-  const int64_t pieces = (o.cols + 7) / 8;
-  mm_repack_kernel<<<grid_for(o.rows * pieces), 256, 0, st>>>(static_cast<const uint16_t*>(o.p), o.rows, o.cols, o.ld, reinterpret_cast<uint16_t*>(room));
-  o.p = room;
-  o.ld = pieces * 8;
-  room += (o.copy_bytes() + 255) / 256 * 256;
+// Copies of the operands that do not fit, in one launch
+cudaError_t repack(Operand& a, Operand& b, char* room, cudaStream_t st) {
+  MmRepack r{};
+  int64_t pieces = 0;
+  Operand* const both[2] = {&a, &b};
+  for (int i = 0; i < 2; ++i) {
+    Operand& o = *both[i];
+    if (o.fits) continue;
+    MmRepack::One& one = r.of[r.n++];
+    one.x = static_cast<const uint16_t*>(o.p); one.out = reinterpret_cast<uint16_t*>(room); one.rows = o.rows; one.cols = o.cols; one.ld = o.ld;
+    pieces += o.rows * ((o.cols + 7) / 8);
+    room += (o.copy_bytes() + 255) / 256 * 256;
+    o.p = one.out;
+    o.ld = (o.cols + 7) / 8 * 8;
+  }
+  if (r.n == 0) return cudaSuccess;
+  mm_repack_kernel<<<grid_for(pieces), 256, 0, st>>>(r);
   return cudaGetLastError();
 }
 
@@ -135,18 +161,17 @@ cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const MmAr
   mm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MMP_THREADS, MMP_SMEM, st>>>(ma, mb, g);
   return cudaGetLastError();
 }
-constexpr int MM_RING = 98304;         // about 100 KB: two blocks to a multiprocessor
 template <int BN, int T, bool SWAP, bool SPLIT>
 cudaError_t launch_tile(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, cudaStream_t st) {
   auto kern = mm_tile_kernel<BN, T, SWAP, SPLIT>;
-  static_assert(mm_part_bytes(BN, SWAP) <= MM_RING, "the sums lie in the ring's bytes");
+  static_assert(mm_part_bytes(BN, SWAP) <= MM_OFF_PATCH, "the sums and the patches lie in the ring's bytes");
   static std::atomic<unsigned long long> done{0};
-  cudaError_t e = allow_smem(kern, MM_RING + 1024, done);
+  cudaError_t e = allow_smem(kern, MM_RING_WIDE + 1024, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1);
   cfg.blockDim = dim3(MM_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = MM_RING + 1024;
+  cfg.dynamicSmemBytes = (size_t)(g.stages * g.stage_bytes > MM_RING ? MM_RING_WIDE : MM_RING) + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr{};
   if (SPLIT) {
@@ -199,20 +224,29 @@ const char* product_refusal(const sim_product* p) {
   return nullptr;
 }
 
-// Which of the two is the instruction's 128-row operand, and how wide the other's tile is
+// Which kernel, which of the two is the instruction's 128-row operand, how wide the other's tile is, and how many blocks share a tile along k.
 struct Plan { bool pair, swap; int bn, split; };
 Plan plan_of(int64_t M, int64_t N, int64_t K, int sms) {
   Plan q{};
   q.swap = M <= 64 && M <= N;
   const int64_t ra = q.swap ? N : M, rb = q.swap ? M : N;
   const int kb = (int)((K + 63) / 64);
-  const int64_t tiles_256 = (ra + 255) / 256 * ((rb + 255) / 256);
-  q.pair = kb > 0 && ra > 128 && rb > 128 && tiles_256 >= sms / 4 && (tiles_256 > sms / 2 || kb >= 32);
+  // Pairs of multiprocessors from two tiles for three pairs on (1531 x 1008 x 2736, 66 tiles of 256 x 256: 13.5 us against 15.0 in tiles of 128 x
+  // 128; 1024 x 4096 x 4096, 64: 28 against 33; 700 x 1024 x 3000, 36: 13.6 against 11.4; 300 x 4096 x 4096, 32: 26 against 23)
+  q.pair = kb > 0 && ra > 128 && rb > 128 && 3 * ((ra + 255) / 256 * ((rb + 255) / 256)) >= 2 * (sms / 2);
   q.bn = rb <= 16 && q.swap ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
-  const int64_t tiles = (ra + 127) / 128 * ((rb + q.bn - 1) / q.bn);
   q.split = 1;
-  const int least = q.bn < 128 ? 4 : 8, blocks = 2 * sms;
-  while (!q.pair && q.split < 8 && tiles * q.split * 2 <= blocks && kb >= q.split * 2 * least) q.split *= 2;
+  if (q.pair) return q;
+  // Time of a split, estimated: a block takes 0.23 us for 64 elements of k where it streams both operands from L2, 0.31 us where it waits for
+  // memory (few rows); more blocks than multiprocessors share them; meeting in distributed shared memory costs what is listed.  (512 x 2048 x 2048:
+  // 15.6, 13.3 and 16.4 us for 1, 2 and 4 blocks a tile; 16 x 4096 x 4096: 24.5, 16.7, 13.3, and 13.6 for 8.)
+  const double meet[4] = {0.0, q.swap ? 1.5 : 2.5, q.swap ? 2.5 : 4.5, q.swap ? 4.5 : 9.0}, step = q.swap ? 0.31 : 0.23;
+  const double tiles = (double)((ra + 127) / 128) * (double)((rb + q.bn - 1) / q.bn);
+  double best = 0.0;
+  for (int i = 0, split = 1; split <= 8 && split <= kb; ++i, split *= 2) {
+    const double waves = tiles * split / sms, t = (waves > 1.0 ? waves : 1.0) * ((kb + split - 1) / split) * step + meet[i];
+    if (i == 0 || t < best) { best = t; q.split = split; }
+  }
   return q;
 }
 
@@ -254,33 +288,34 @@ sim_status sim_ckpt_read(const uint8_t* codes, const uint8_t* scales, int64_t ro
   a.rows = rows; a.cols = cols; a.codes = const_cast<uint8_t*>(codes); a.scales = const_cast<uint8_t*>(scales); a.out = out; a.ldo = ld;
   a.vec = rows_aligned(out, rows, ld, type, 16);
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const unsigned grid = grid_for(rows * ((cols + 31) / 32) * (a.vec ? 2 : 32));
+  const unsigned grid = grid_for(rows * ((cols + 31) / 32) * (a.vec ? 1 : 32));
   const cudaError_t e = type == SIM_F32 ? ckpt_read<T_F32>(a, act, grid, st) : type == SIM_BF16 ? ckpt_read<T_BF16>(a, act, grid, st) : ckpt_read<T_F16>(a, act, grid, st);
   return e == cudaSuccess ? SIM_OK : cuda_failed("sim_ckpt_read", e);
 }
 
-int64_t sim_act_backward_workspace(int64_t rows, int64_t cols) { return rows < 1 || cols < 1 || bad_matrix(rows, cols, cols) ? 0 : sum_splits(rows, cols) * cols * 4; }
+int64_t sim_act_backward_workspace(int64_t rows, int64_t cols) { return rows < 1 || cols < 1 || bad_matrix(rows, cols, cols) || sum_splits(rows, cols) <= 8 ? 0 : sum_splits(rows, cols) * cols * 4; }
 
 sim_status sim_act_backward(const void* dy, sim_dtype type, int64_t rows, int64_t cols, int64_t ld, const uint8_t* codes, const uint8_t* scales, sim_act act, void* dz, int64_t lddz,
                             void* db, sim_dtype db_type, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
   if (!plain_type(type) || (db && !plain_type(db_type))) return bad("sim_act_backward: types must be SIM_F32, SIM_BF16 or SIM_F16");
   if (!known_act(act)) return bad("sim_act_backward: unknown activation");
-  if (bad_matrix(rows, cols, ld) || (codes && bad_matrix(rows, cols, lddz))) return bad("sim_act_backward: rows and cols must be in [0, 2^31], ld and lddz at least cols");
-  if (!codes != !scales || !codes != !dz) return bad("sim_act_backward: codes, scales and dz go together (or none of them, for the sums of dy alone)");
-  if (!codes && !db) return bad("sim_act_backward: nothing to compute");
+  if (bad_matrix(rows, cols, ld) || (dz && bad_matrix(rows, cols, lddz))) return bad("sim_act_backward: rows and cols must be in [0, 2^31], ld and lddz at least cols");
+  if (!codes != !scales || (codes && !dz)) return bad("sim_act_backward: codes and scales go together, and with dz");
+  if (!dz && !db) return bad("sim_act_backward: nothing to compute");
   if (cols == 0) return SIM_OK;
   if (db && !aligned(db, elem_bytes(db_type))) return bad("sim_act_backward: db must be aligned to its type");
-  if (db && rows > 0 && (!workspace || !aligned(workspace, 4) || workspace_bytes < sim_act_backward_workspace(rows, cols)))
+  const int64_t need = db ? sim_act_backward_workspace(rows, cols) : 0;
+  if (need > 0 && (!workspace || !aligned(workspace, 4) || workspace_bytes < need))
     return bad("sim_act_backward: sums need a workspace of sim_act_backward_workspace bytes");
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   cudaError_t e = cudaSuccess;
   const int eb = elem_bytes(type);
   int64_t splits = 0;
   if (rows > 0) {
-    if (!dy || !aligned(dy, eb) || (codes && (!aligned(codes, 16) || !aligned(dz, eb)))) return bad("sim_act_backward: dy and dz (aligned to their type) and codes (16-byte aligned) are required");
+    if (!dy || !aligned(dy, eb) || !aligned(codes, 16) || !aligned(dz, eb)) return bad("sim_act_backward: dy and dz (aligned to their type) and codes (16-byte aligned) are required");
     const int64_t pitch = ckpt_pitch(cols);
     const Range in[3] = {range_of(dy, rows, cols, ld, eb), range_of(codes, rows, pitch, pitch, 1), range_of(scales, rows, pitch / 32, pitch / 32, 1)};
-    const Range out[3] = {range_of(dz, rows, cols, lddz, eb), range_of(db, 1, cols, cols, db ? elem_bytes(db_type) : 1), range_of(db ? workspace : nullptr, 1, workspace_bytes, workspace_bytes, 1)};
+    const Range out[3] = {range_of(dz, rows, cols, lddz, eb), range_of(db, 1, cols, cols, db ? elem_bytes(db_type) : 1), range_of(need > 0 ? workspace : nullptr, 1, need, need, 1)};
     for (int i = 0; i < 3; ++i)
       for (int o = 0; o < 3; ++o)
         if (overlap(in[i], out[o]) && !(i == 0 && o == 0 && dy == dz && ld == lddz)) return bad("sim_act_backward: the buffers overlap (dz may be dy itself, with the same rows)");
@@ -288,19 +323,16 @@ sim_status sim_act_backward(const void* dy, sim_dtype type, int64_t rows, int64_
     splits = sum_splits(rows, cols);
     CkptArgs a{};
     a.x = dy; a.rows = rows; a.cols = cols; a.ld = ld; a.codes = const_cast<uint8_t*>(codes); a.scales = const_cast<uint8_t*>(scales); a.out = dz; a.ldo = lddz;
-    a.vec = rows_aligned(dy, rows, ld, type, 16) && (!codes || rows_aligned(dz, rows, lddz, type, 16));
-    a.partial = !db ? nullptr : splits == 1 && db_type == SIM_F32 ? static_cast<float*>(db) : static_cast<float*>(workspace);
+    a.vec = rows_aligned(dy, rows, ld, type, 16) && (!dz || rows_aligned(dz, rows, lddz, type, 16));
+    a.partial = need > 0 ? static_cast<float*>(workspace) : nullptr;
+    a.db = need > 0 ? nullptr : db; a.db_type = db_type;
     a.split_rows = (int)((rows + splits - 1) / splits);
     const dim3 grid((unsigned)((cols + 255) / 256), (unsigned)splits, 1);
     e = type == SIM_F32 ? act_backward<T_F32>(a, act, grid, st) : type == SIM_BF16 ? act_backward<T_BF16>(a, act, grid, st) : act_backward<T_F16>(a, act, grid, st);
     if (e != cudaSuccess) return cuda_failed("sim_act_backward", e);
   }
-  if (db && !(splits == 1 && db_type == SIM_F32)) {
-    const unsigned grid = (unsigned)((cols + 31) / 32);
-    const float* partial = static_cast<const float*>(workspace);
-    if (db_type == SIM_F32) column_sum_finish_kernel<T_F32><<<grid, 256, 0, st>>>(partial, (int)splits, cols, db);
-    else if (db_type == SIM_BF16) column_sum_finish_kernel<T_BF16><<<grid, 256, 0, st>>>(partial, (int)splits, cols, db);
-    else column_sum_finish_kernel<T_F16><<<grid, 256, 0, st>>>(partial, (int)splits, cols, db);
+  if (db && (need > 0 || rows == 0)) {
+    column_sum_finish_kernel<<<(unsigned)((cols + 31) / 32), 256, 0, st>>>(static_cast<const float*>(workspace), (int)splits, cols, db, db_type);
     e = cudaGetLastError();
   }
   return e == cudaSuccess ? SIM_OK : cuda_failed("sim_act_backward", e);
@@ -330,9 +362,7 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   const Plan q = plan_of(M, N, K, sms);
   Operand a = operand(p->a, p->lda, p->a_t, M, K), b = operand(p->b, p->ldb, p->b_t, N, K);
   const cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  char* room = static_cast<char*>(workspace);
-  cudaError_t e = K > 0 ? repack(a, room, st) : cudaSuccess;
-  if (e == cudaSuccess && K > 0) e = repack(b, room, st);
+  cudaError_t e = need > 0 ? repack(a, b, static_cast<char*>(workspace), st) : cudaSuccess;
   if (e != cudaSuccess) return cuda_failed("sim_matmul", e);
   if (q.swap) { const Operand t = a; a = b; b = t; }
 
@@ -347,14 +377,15 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   g.tiles_a = (int)ta; g.tiles_b = (int)tb;
   g.a_t = a.t; g.b_t = b.t;
   g.stage_bytes = MM_A_BYTES + (b.t ? (q.bn < 64 ? 64 : q.bn) : q.bn) * 128;
-  g.stages = MM_RING / g.stage_bytes;
+  // a block to a multiprocessor: its ring may take all shared memory (2048 x 1024 x 512: XXX us)
+  g.stages = (ta * tb * split <= sms ? MM_RING_WIDE : MM_RING) / g.stage_bytes;
+  if (g.stages > MM_MAX_STAGES) g.stages = MM_MAX_STAGES;
   g.idesc = mm_idesc(q.pair ? 256 : 128, q.pair ? 256 : q.bn, p->type == SIM_BF16, a.t, b.t);
   g.act = p->act; g.grad = p->act_grad ? 1 : 0; g.bias = p->bias; g.bias_type = p->bias_type;
   g.z_codes = p->z_codes; g.z_scales = p->z_scales; g.res = p->residual; g.ldr = p->ldr; g.c = p->c; g.ldc = p->ldc;
-  const int quad = 4 * elem_bytes(p->c_type);
-  g.vec_c = rows_aligned(p->c, M, p->ldc, p->c_type, quad);
-  g.vec_r = p->residual && rows_aligned(p->residual, M, p->ldr, p->c_type, quad);
-  g.vec_b = p->bias && aligned(p->bias, 4 * elem_bytes(p->bias_type));
+  g.vec_c = rows_aligned(p->c, M, p->ldc, p->c_type, 32) ? 2 : rows_aligned(p->c, M, p->ldc, p->c_type, 16) ? 1 : 0;
+  g.vec_r = p->residual && rows_aligned(p->residual, M, p->ldr, p->c_type, 16);
+  g.vec_b = p->bias && aligned(p->bias, 16);
   CUtensorMap ma{}, mb{};
   if (K > 0 && (!make_map(&ma, a.p, p->type, a.rows, a.cols, a.ld, a.t ? 64 : 128) ||
                 !make_map(&mb, b.p, p->type, b.rows, b.cols, b.ld, b.t ? 64 : q.pair ? 128 : (uint32_t)q.bn)))
@@ -400,7 +431,9 @@ cudaError_t log_probs(const LogpArgs& a, cudaStream_t st) {
   int slices = 1;
   while (slices < 8 && a.rows * slices * 2 <= 2 * sms && a.vocab >= slices * 2 * 4096) slices *= 2;
   const int len = (int)(((a.vocab + slices - 1) / slices + 7) / 8 * 8);
-  return launch_rows<T, 512>(a, slices, len, st);
+  // Many rows: blocks of 256 threads, six to a multiprocessor, whose phases mix (4096 x 131072 bf16 with eight alternatives: XXX us against XXX in blocks of
+  // 512).  Few: a thread's share is what a row takes.
+  return slices == 1 ? launch_rows<T, 256>(a, slices, len, st) : launch_rows<T, 512>(a, slices, len, st);
 }
 
 }  // namespace
