@@ -296,6 +296,11 @@ __device__ __forceinline__ uint64_t mm_desc(uint32_t saddr, int t) { return t ? 
 // sixteen elements of k further: 32 bytes along a row, or sixteen rows of 128 bytes (descriptors count in 16 bytes)
 __device__ __forceinline__ uint32_t mm_desc_step(int t) { return t ? 128u : 2u; }
 
+// The first lane's value, which the compiler then knows to be the same in all: the role of a warp and what its MMAs take stay in uniform registers (a
+// stage of four MMAs was issued in 550 cycles without it)
+template <typename V>
+__device__ __forceinline__ V uniform(V v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+
 // Issued by one elected lane of a converged warp
 __device__ __forceinline__ void mm_mma(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -321,6 +326,36 @@ constexpr int MM_OFF_PATCH = MM_RING - 8 * MM_PATCH;            // the warps' pa
 __host__ __device__ constexpr int mm_pitch(int bn, bool swap) { return swap ? 132 : bn + 4; }     // floats between lines of sums: rows, or (swap) columns of tensor memory
 __host__ __device__ constexpr int mm_part_bytes(int bn, bool swap) { return (swap ? bn : 128) * mm_pitch(bn, swap) * 4; }
 
+// Columns [col, col + 32) of rows [row, row + 32) of the sums that the n blocks of a cluster hold in shared memory at `part`, added in the blocks'
+// order; a lane gets its row.  Read four rows of 128 bytes at a time (a row a lane took twice as long) and left in this block's place of the
+// chunk, which nobody else reads.
+template <int PITCH>
+__device__ __forceinline__ void mm_sum_chunk(float* part, uint32_t part_addr, int row, int col, int n, int lane, float (&v)[32]) {
+  const uint32_t at = (uint32_t)((row + (lane >> 3)) * PITCH + col + (lane & 7) * 4);
+#pragma unroll 1
+  for (int k0 = 0; k0 < 8; k0 += 4) {
+    float4 t[4];
+#pragma unroll 1
+    for (int r = 0; r < n; ++r) {
+      const uint32_t from = cluster_addr(part_addr + 4u * at, (uint32_t)r) + 16u * (uint32_t)(PITCH * k0);
+      float4 p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) p[k] = ld_cluster4(from + 16u * (uint32_t)(PITCH * k));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] = r == 0 ? p[k] : make_float4(t[k].x + p[k].x, t[k].y + p[k].y, t[k].z + p[k].z, t[k].w + p[k].w);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(part + at + 4 * PITCH * (k0 + k)) = t[k];
+  }
+  __syncwarp();
+  const float* mine = part + (row + lane) * PITCH + col;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float4 q = *reinterpret_cast<const float4*>(mine + 4 * k);
+    v[4 * k] = q.x; v[4 * k + 1] = q.y; v[4 * k + 2] = q.z; v[4 * k + 3] = q.w;
+  }
+}
+
 template <int BN, int T, bool SWAP, bool SPLIT>
 __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ MmArgs g) {
   extern __shared__ unsigned char smem_raw[];
@@ -328,7 +363,7 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
   __shared__ uint32_t tmem_slot;
   const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
   unsigned char* base_p = smem_raw + (base - raw);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const uint32_t bars = smem_addr(bars_s);
   auto full = [&](int s) { return bars + 8u * s; };
   auto empty = [&](int s) { return bars + 8u * (MM_MAX_STAGES + s); };
@@ -341,39 +376,43 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
   const int a0 = (band * 8 + in_band % band_rows) * 128, b0 = in_band / band_rows * BN;
   const int k_begin = SPLIT ? (int)blockIdx.y * g.kb_split : 0, n_it = (SPLIT ? min(g.kb, k_begin + g.kb_split) : g.kb) - k_begin;
 
+  // the loads of one stage, which the producer has found empty
+  auto load = [&](int it, int s) {
+    const uint32_t at = base + (uint32_t)(s * g.stage_bytes), to_b = at + MM_A_BYTES;
+    const int k0 = (k_begin + it) * 64;
+    mbar_arrive_expect_tx(full(s), (uint32_t)g.stage_bytes);
+    if (g.a_t) {
+      tma_load_2d(at, &map_a, a0, k0, full(s));
+      tma_load_2d(at + 8192, &map_a, a0 + 64, k0, full(s));
+    } else {
+      tma_load_2d(at, &map_a, k0, a0, full(s));
+    }
+    if (g.b_t) {
+      tma_load_2d(to_b, &map_b, b0, k0, full(s));
+      if (BN > 64) tma_load_2d(to_b + 8192, &map_b, b0 + 64, k0, full(s));
+    } else {
+      tma_load_2d(to_b, &map_b, k0, b0, full(s));
+    }
+  };
   if (tid == 0) {
     for (int s = 0; s < g.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     mbar_init(acc_bar, 1);
     mbar_fence_init();
-    if (n_it > 0) { prefetch_map(&map_a); prefetch_map(&map_b); }
+    for (int it = 0; it < min(n_it, g.stages); ++it) load(it, it);       // the first round of the ring needs nobody else
   }
   if (warp == 1) tc_alloc(smem_addr(&tmem_slot), TMEM_COLS);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_slot;
+  const uint32_t tmem = uniform(tmem_slot);
   bool failed = false;
   if (warp == 0) {
     if (lane == 0) {
-      int s = 0, issued = 0;
-      uint32_t phase = 1;
-      for (int it = 0; it < n_it; ++it) {
-        if (!mbar_wait(empty(s), phase)) { failed = true; break; }
-        const uint32_t at = base + (uint32_t)(s * g.stage_bytes), to_b = at + MM_A_BYTES;
-        const int k0 = (k_begin + it) * 64;
-        mbar_arrive_expect_tx(full(s), (uint32_t)g.stage_bytes);
-        if (g.a_t) {
-          tma_load_2d(at, &map_a, a0, k0, full(s));
-          tma_load_2d(at + 8192, &map_a, a0 + 64, k0, full(s));
-        } else {
-          tma_load_2d(at, &map_a, k0, a0, full(s));
-        }
-        if (g.b_t) {
-          tma_load_2d(to_b, &map_b, b0, k0, full(s));
-          if (BN > 64) tma_load_2d(to_b + 8192, &map_b, b0 + 64, k0, full(s));
-        } else {
-          tma_load_2d(to_b, &map_b, k0, b0, full(s));
-        }
+      int s = 0, issued = min(n_it, g.stages);
+      uint32_t phase = 0;
+      for (int it = g.stages; it < n_it; ++it) {
+        if (!mbar_try_wait(empty(s), phase) && !mbar_wait(empty(s), phase)) { failed = true; break; }
+        load(it, s);
         issued = it + 1;
         if (++s == g.stages) { s = 0; phase ^= 1u; }
       }
@@ -387,7 +426,7 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
     int s = 0;
     uint32_t phase = 0;
     for (int it = 0; it < n_it; ++it) {
-      if (!mbar_wait_warp(full(s), phase)) { failed = true; break; }
+      if (!mbar_wait_all(full(s), phase)) { failed = true; break; }
       tc_fence_after();
       const uint32_t at = (uint32_t)(s * g.stage_bytes) >> 4;
 #pragma unroll
@@ -479,32 +518,8 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
         few.finish(g, v);
       } else {
         MmRows<T> rows(g, a0 + 32 * tq, b0 + 32 * ch, lane, raw);
-        // The blocks' sums are read four rows of 128 bytes at a time (a row a lane took twice as long) and left in this block's place of
-        // the chunk, which nobody else reads.
-        const uint32_t at = (uint32_t)((32 * tq + (lane >> 3)) * PITCH + 32 * ch + (lane & 7) * 4);
-#pragma unroll 1
-        for (int k0 = 0; k0 < 8; k0 += 4) {
-          float4 t[4];
-#pragma unroll 1
-          for (int r = 0; r < n; ++r) {
-            const uint32_t from = cluster_addr(base + 4u * at, (uint32_t)r) + 16u * (uint32_t)(PITCH * k0);
-            float4 p[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p[k] = ld_cluster4(from + 16u * (uint32_t)(PITCH * k));
-#pragma unroll
-            for (int k = 0; k < 4; ++k) t[k] = r == 0 ? p[k] : make_float4(t[k].x + p[k].x, t[k].y + p[k].y, t[k].z + p[k].z, t[k].w + p[k].w);
-          }
-#pragma unroll
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(part + at + 4 * PITCH * (k0 + k)) = t[k];
-        }
-        __syncwarp();
         float v[32];
-        const float* mine = part + (32 * tq + lane) * PITCH + 32 * ch;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float4 q4 = *reinterpret_cast<const float4*>(mine + 4 * k);
-          v[4 * k] = q4.x; v[4 * k + 1] = q4.y; v[4 * k + 2] = q4.z; v[4 * k + 3] = q4.w;
-        }
+        mm_sum_chunk<PITCH>(part, base, 32 * tq, 32 * ch, n, lane, v);
         rows.finish(g, v, lane, patch);
       }
       task += n * (MM_THREADS / 32);
@@ -522,11 +537,14 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
 //   warp 1      tensor memory; in the leader one lane issues the MMAs for both
 //   warps 2-9   the tail: a warp takes 32 rows x 128 columns, 32 columns at a time
 // Two sets of accumulators (2 x 256 columns of tensor memory): a tile's tail runs beside the next one's MMAs.
+// (Two pairs of a cluster sharing a tile along k were built and dropped: 256 x 8192 x 8192 38.9 -> 35.0 us, 300 x 4096 x 4096 21.8 -> 21.1, others slower;
+// clusters of four blocks of this size fit the device 32 times at most.)
 constexpr int MMP_THREADS = 320, MMP_STAGES = 6, MMP_HALF = 128 * 128, MMP_STAGE = 2 * MMP_HALF;
 constexpr int MMP_OFF_STORE = MMP_STAGES * MMP_STAGE;
 constexpr int MMP_OFF_BARS = MMP_OFF_STORE + 8 * MM_PATCH;
 constexpr int MMP_SMEM = MMP_OFF_BARS + 8 * (2 * MMP_STAGES + 4) + 16 + 1024;
 static_assert(MMP_SMEM <= 227 * 1024, "the ring and the tail's patches must fit");
+
 
 template <int T>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MMP_THREADS, 1)
@@ -534,7 +552,7 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;      // the same offset in both blocks
   unsigned char* base_p = smem_raw + (base - raw);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane = tid & 31, warp = uniform(tid >> 5);
   const uint32_t rank = cluster_rank();
   const uint32_t bars = base + MMP_OFF_BARS;
   auto full = [&](int s) { return bars + 8u * s; };                             // both blocks' operands have landed: the leader's count
@@ -557,7 +575,7 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   __syncthreads();
   cluster_sync_all();                                                           // barriers of both blocks are set up
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uniform(*tmem_slot);
   const int n_tiles = g.tiles_a * g.tiles_b, pairs = (int)gridDim.x >> 1;
   bool failed = false;
 
@@ -607,11 +625,11 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
       uint32_t acc_phase = 1;
       bool there = false;                                                       // the stage's operands are known to have landed
       for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
-        if (!mbar_wait_warp(acc_empty(buf), acc_phase)) { failed = true; break; }
+        if (!mbar_wait_all(acc_empty(buf), acc_phase)) { failed = true; break; }
         tc_fence_after();
         const uint32_t d = tmem + 256u * buf;
         for (int it = 0; it < g.kb; ++it) {
-          if (!there && !mbar_wait_warp(full(r.s), r.phase)) { failed = true; break; }
+          if (!there && !mbar_wait_all(full(r.s), r.phase)) { failed = true; break; }
           tc_fence_after();
           const uint32_t at = (uint32_t)(r.s * (MMP_STAGE / 16));
           mm_mma_pair(d, adesc + at, bdesc + at, g.idesc, it > 0 ? 1u : 0u);

@@ -234,19 +234,24 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int sms) {
   // Pairs of multiprocessors from two tiles for three pairs on (1531 x 1008 x 2736, 66 tiles of 256 x 256: 13.5 us against 15.0 in tiles of 128 x
   // 128; 1024 x 4096 x 4096, 64: 28 against 33; 700 x 1024 x 3000, 36: 13.6 against 11.4; 300 x 4096 x 4096, 32: 26 against 23)
   q.pair = kb > 0 && ra > 128 && rb > 128 && 3 * ((ra + 255) / 256 * ((rb + 255) / 256)) >= 2 * (sms / 2);
-  q.bn = rb <= 16 && q.swap ? 16 : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
   q.split = 1;
+  if (const char* e = getenv("MMPLAN")) { if (atoi(e) >= 2) { q.pair = kb > 0 && ra > 128 && rb > 128; } else q.pair = false; }
   if (q.pair) return q;
-  // Time of a split, estimated: a block takes 0.23 us for 64 elements of k where it streams both operands from L2, 0.31 us where it waits for
-  // memory (few rows); more blocks than multiprocessors share them; meeting in distributed shared memory costs what is listed.  (512 x 2048 x 2048:
-  // 15.6, 13.3 and 16.4 us for 1, 2 and 4 blocks a tile; 16 x 4096 x 4096: 24.5, 16.7, 13.3, and 13.6 for 8.)
-  const double meet[4] = {0.0, q.swap ? 1.5 : 2.5, q.swap ? 2.5 : 4.5, q.swap ? 4.5 : 9.0}, step = q.swap ? 0.31 : 0.23;
-  const double tiles = (double)((ra + 127) / 128) * (double)((rb + q.bn - 1) / q.bn);
+  // Else the time of each tile width and split, estimated (us).  64 elements of k cost a block 0.25 (few rows, whose weights come from memory: 0.3), more
+  // blocks than multiprocessors take turns, the tail costs 0.6 for each 64 columns, meeting in distributed shared memory what is listed.
+  // (512 x 2048 x 2048: 13.5, 11.8 and 16 us for 1, 2 and 4 blocks a tile of 128 x 128, 12.1 in tiles of 128 x 64; 2048 x 1024 x 512: 9.2, and 7.9
+  // in tiles of 128 x 64; 2000 x 2000 x 704: 13.5, and 16.4; 16 x 4096 x 4096: 24.5, 16.7, 12.6, and 13.6 for 8.)
+  const double meet[4] = {0.0, q.swap ? 1.5 : 2.5, q.swap ? 2.5 : 4.5, q.swap ? 4.5 : 9.0}, step = q.swap ? 0.3 : 0.25;
+  const int widest = q.swap ? (rb <= 16 ? 16 : rb <= 32 ? 32 : 64) : rb <= 32 ? 32 : rb <= 64 ? 64 : 128;
   double best = 0.0;
-  for (int i = 0, split = 1; split <= 8 && split <= kb; ++i, split *= 2) {
-    const double waves = tiles * split / sms, t = (waves > 1.0 ? waves : 1.0) * ((kb + split - 1) / split) * step + meet[i];
-    if (i == 0 || t < best) { best = t; q.split = split; }
+  for (int bn = widest; bn >= (q.swap ? widest : 32); bn /= 2) {
+    const double tiles = (double)((ra + 127) / 128) * (double)((rb + bn - 1) / bn);
+    for (int i = 0, split = 1; split <= 8 && (split == 1 || split <= kb); ++i, split *= 2) {
+      const double t = std::ceil(tiles * split / (q.swap ? 1.3 * sms : sms)) * (((kb + split - 1) / split) * step + (q.swap ? 0.0 : bn / 64 * 0.6)) + meet[i];
+      if (q.bn == 0 || t < best) { best = t; q.split = split; q.bn = bn; }
+    }
   }
+  if (getenv("MMBN")) { q.bn = atoi(getenv("MMBN")); q.split = atoi(getenv("MMSPLIT")); }
   return q;
 }
 
@@ -378,7 +383,7 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   g.a_t = a.t; g.b_t = b.t;
   g.stage_bytes = MM_A_BYTES + (b.t ? (q.bn < 64 ? 64 : q.bn) : q.bn) * 128;
   // a block to a multiprocessor: its ring may take all shared memory (2048 x 1024 x 512: XXX us)
-  g.stages = (ta * tb * split <= sms ? MM_RING_WIDE : MM_RING) / g.stage_bytes;
+  g.stages = (ta * tb * split <= sms && !getenv("MMNARROW") ? MM_RING_WIDE : MM_RING) / g.stage_bytes;
   if (g.stages > MM_MAX_STAGES) g.stages = MM_MAX_STAGES;
   g.idesc = mm_idesc(q.pair ? 256 : 128, q.pair ? 256 : q.bn, p->type == SIM_BF16, a.t, b.t);
   g.act = p->act; g.grad = p->act_grad ? 1 : 0; g.bias = p->bias; g.bias_type = p->bias_type;
