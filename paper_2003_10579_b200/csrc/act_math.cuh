@@ -27,20 +27,19 @@ __device__ __forceinline__ float act_value(float z) {
   if (ACT == ACT_SILU) return z * logistic2(LOG2E * z);
   return z;
 }
-// The derivative; relu's at zero is zero.
+// The derivative at a finite z; relu's at zero is zero.  With q = s(u): (z s(u))' = q (1 + z u'(z) (1 - q)).  Beyond the limits it is 0 or 1, and the powers
+// of z would only raise the error of 1 - q.
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
-  if (ACT == ACT_RELU) return z > 0.f ? 1.f : z != z ? z : 0.f;
+  if (ACT == ACT_RELU) return z > 0.f ? 1.f : 0.f;
   if (ACT == ACT_GELU) {
-    const float t = fminf(fmaxf(z, -10.f), 10.f);                      // beyond, it is 0 or 1, and the cube would only raise the error of 1 - q
-    const float q = logistic2(t * fmaf(LOG2E * GELU_C * GELU_A * t, t, LOG2E * GELU_C));
-    const float d = fmaf(t * q * (1.f - q), fmaf(3.f * GELU_C * GELU_A * t, t, GELU_C), q);
-    return z != z ? z : d;
+    const float t = fminf(fmaxf(z, -10.f), 10.f), t2 = t * t;
+    const float q = logistic2(t * fmaf(LOG2E * GELU_C * GELU_A, t2, LOG2E * GELU_C));
+    return q * fmaf(t * fmaf(3.f * GELU_C * GELU_A, t2, GELU_C), 1.f - q, 1.f);
   }
   if (ACT == ACT_SILU) {
-    const float t = fminf(fmaxf(z, -80.f), 80.f);
-    const float q = logistic2(LOG2E * t), d = fmaf(t * q, 1.f - q, q);
-    return z != z ? z : d;
+    const float t = fminf(fmaxf(z, -80.f), 80.f), q = logistic2(LOG2E * t);
+    return q * fmaf(t, 1.f - q, 1.f);
   }
   return 1.f;
 }

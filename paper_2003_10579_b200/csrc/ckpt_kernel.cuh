@@ -188,15 +188,30 @@ __global__ void __launch_bounds__(256, 3) act_backward_kernel(const __grid_const
     for (int k = 0; k < AHEAD; ++k) {
       const long long row = r + 8 * k;
       const int m = row < r1 ? n : 0;
-      float d[8];
+      float d[8];                                                          // what does not exist was read as zeros
 #pragma unroll
       for (int e = 0; e < 8; ++e) d[e] = g[k].value(e);
       if constexpr (KEPT) {
         float z[8];
-        ckpt_values4(code[k].x, 1.f, z);
-        ckpt_values4(code[k].y, 1.f, z + 4);
+        bool lost = false;                                                 // a NaN block
+        if (VEC) {
+          const float s = scale_value(scale[k][0]);
+          ckpt_values4(code[k].x, s, z);
+          ckpt_values4(code[k].y, s, z + 4);
+          lost = scale[k][0] == 255u;
+        } else {
+          ckpt_values4(code[k].x, 1.f, z);
+          ckpt_values4(code[k].y, 1.f, z + 4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) d[e] *= act_slope<ACT>(z[e] * scale_value(scale[k][VEC ? 0 : e]));
+          for (int e = 0; e < 8; ++e) { z[e] *= scale_value(scale[k][VEC ? 0 : e]); lost |= scale[k][VEC ? 0 : e] == 255u; }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] *= act_slope<ACT>(z[e]);
+        if (lost) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (scale[k][VEC ? 0 : e] == 255u) d[e] = __uint_as_float(0x7FC00000u);
+        }
       }
       if (KEPT || a.out) {
         char* to = static_cast<char*>(a.out) + row * a.ldo * EB;
@@ -207,7 +222,7 @@ __global__ void __launch_bounds__(256, 3) act_backward_kernel(const __grid_const
             if (e < m) Elem<T>::put(to, c + e * STEP, d[e]);
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += e < m ? d[e] : 0.f;
+      for (int e = 0; e < 8; ++e) acc[e] += d[e];                          // zeros (or, of a tail, columns that are not there) add nothing that counts
     }
   }
   if (!a.partial && !a.db) return;

@@ -179,6 +179,10 @@ struct MmRows {
         if (g.act == ACT_RELU) slope_row<ACT_RELU>(v, za, zb, scale);
         else if (g.act == ACT_GELU) slope_row<ACT_GELU>(v, za, zb, scale);
         else if (g.act == ACT_SILU) slope_row<ACT_SILU>(v, za, zb, scale);
+        if (zs == 255u) {                    // a NaN block
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = scale;
+        }
       }
     } else {
       if (g.bias) {                          // each lane's column to all lanes
@@ -281,6 +285,7 @@ struct MmFew {
       if (g.act == ACT_RELU) v[j] = g.grad ? v[j] * act_slope<ACT_RELU>(at) : act_value<ACT_RELU>(at);
       else if (g.act == ACT_GELU) v[j] = g.grad ? v[j] * act_slope<ACT_GELU>(at) : act_value<ACT_GELU>(at);
       else if (g.act == ACT_SILU) v[j] = g.grad ? v[j] * act_slope<ACT_SILU>(at) : act_value<ACT_SILU>(at);
+      if (g.grad && zs[j] == 255u) v[j] = at;                // a NaN block
       if (g.res) v[j] += value_of<T>(r[j]);
       Elem<T>::put(g.c, (row0 + j) * g.ldc + col, v[j]);
     }
@@ -321,7 +326,7 @@ __device__ __forceinline__ void mm_mma_pair(uint32_t d, uint64_t adesc, uint64_t
 //   all eight  the tail, each 32 lanes of tensor memory and half of the columns.  In a cluster the sums go to shared memory (over the ring, which
 //              every MMA has read by then), and each block takes its share of the tile over the blocks, in their order: the same bits every time
 constexpr int MM_THREADS = 256, MM_MAX_STAGES = 12, MM_A_BYTES = 16384;
-constexpr int MM_RING = 98304, MM_RING_WIDE = 2 * MM_RING;      // bytes, with what else there is: for two blocks to a multiprocessor, for one
+constexpr int MM_RING = 98304, MM_RING_WIDE = 2 * MM_RING, MM_RING_NARROW = 73728;    // bytes, with what else there is: for two blocks to a multiprocessor, for one, for three
 constexpr int MM_OFF_PATCH = MM_RING - 8 * MM_PATCH;            // the warps' patches, behind the sums
 __host__ __device__ constexpr int mm_pitch(int bn, bool swap) { return swap ? 132 : bn + 4; }     // floats between lines of sums: rows, or (swap) columns of tensor memory
 __host__ __device__ constexpr int mm_part_bytes(int bn, bool swap) { return (swap ? bn : 128) * mm_pitch(bn, swap) * 4; }
@@ -699,17 +704,48 @@ struct MmRepack {
   struct One { const uint16_t* x; uint16_t* out; long long rows, cols, ld; } of[2];
   int n;
 };
+// 16 bytes from any even address, from the two aligned pieces that hold them (5003 x 2051 from memory: 8.7 us, element by element 8.9; from L2)
+__device__ __forceinline__ uint4 unaligned16(const uint16_t* p) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+  const uint4* q = reinterpret_cast<const uint4*>(a & ~(uintptr_t)15);
+  const uint4 lo = q[0], hi = q[1];
+  uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  const int by = (int)(a & 15) >> 1;                       // elements
+  if (by & 4)
+#pragma unroll
+    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+  if (by & 2)
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+  if (by & 1)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 __global__ void __launch_bounds__(256) mm_repack_kernel(const __grid_constant__ MmRepack r) {
   for (int i = 0; i < r.n; ++i) {
     const MmRepack::One o = r.of[i];
     const uint32_t pieces = (uint32_t)((o.cols + 7) / 8);
+    const uintptr_t first = reinterpret_cast<uintptr_t>(o.x), last = reinterpret_cast<uintptr_t>(o.x + (o.rows - 1) * o.ld + o.cols);
     for (PieceWalk at((long long)blockIdx.x * 256 + threadIdx.x, (long long)gridDim.x * 256, pieces); at.row < o.rows; at.next()) {
       const long long c = 8ll * at.at;
       const uint16_t* src = o.x + at.row * o.ld + c;
-      uint32_t v[8];
+      const uintptr_t from = reinterpret_cast<uintptr_t>(src) & ~(uintptr_t)15;
+      uint4 v;
+      if (from >= first && from + 32 <= last) {              // both pieces lie inside the matrix
+        v = unaligned16(src);
+        if (c + 8 > o.cols) {                                // what follows a row is not its own
+          uint32_t* w = &v.x;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = c + e < o.cols ? src[e] : 0u;
-      *reinterpret_cast<uint4*>(o.out + (at.row * pieces + at.at) * 8) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+          for (int k = 0; k < 4; ++k) w[k] &= c + 2 * k + 1 < o.cols ? 0xFFFFFFFFu : c + 2 * k < o.cols ? 0xFFFFu : 0u;
+        }
+      } else {
+        uint32_t e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = c + k < o.cols ? src[k] : 0u;
+        v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+      }
+      *reinterpret_cast<uint4*>(o.out + (at.row * pieces + at.at) * 8) = v;
     }
   }
 }

@@ -164,14 +164,14 @@ cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const MmAr
 template <int BN, int T, bool SWAP, bool SPLIT>
 cudaError_t launch_tile(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, cudaStream_t st) {
   auto kern = mm_tile_kernel<BN, T, SWAP, SPLIT>;
-  static_assert(mm_part_bytes(BN, SWAP) <= MM_OFF_PATCH, "the sums and the patches lie in the ring's bytes");
+  static_assert(mm_part_bytes(BN, SWAP) <= (SWAP ? MM_RING_NARROW : MM_OFF_PATCH), "the sums and the patches lie in the ring's bytes");
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = allow_smem(kern, MM_RING_WIDE + 1024, done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1);
   cfg.blockDim = dim3(MM_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)(g.stages * g.stage_bytes > MM_RING ? MM_RING_WIDE : MM_RING) + 1024;
+  cfg.dynamicSmemBytes = (size_t)(SWAP ? g.stages * g.stage_bytes : g.stages * g.stage_bytes > MM_RING ? MM_RING_WIDE : MM_RING) + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr{};
   if (SPLIT) {
@@ -382,8 +382,11 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   g.tiles_a = (int)ta; g.tiles_b = (int)tb;
   g.a_t = a.t; g.b_t = b.t;
   g.stage_bytes = MM_A_BYTES + (b.t ? (q.bn < 64 ? 64 : q.bn) : q.bn) * 128;
-  // a block to a multiprocessor: its ring may take all shared memory (2048 x 1024 x 512: XXX us)
-  g.stages = (ta * tb * split <= sms && !getenv("MMNARROW") ? MM_RING_WIDE : MM_RING) / g.stage_bytes;
+  // One block to a multiprocessor: its ring may take all shared memory (2048 x 1024 x 512: 10.4 -> 9.2 us).  Few rows and more blocks than two to a
+  // multiprocessor hold: rings for three (1 x 1000 x 50000, 391 blocks: 38.3 -> XXX us).
+  const int64_t blocks = ta * tb * split;
+  const int ring = blocks <= sms ? MM_RING_WIDE : q.swap && blocks > 2 * sms ? MM_RING_NARROW : MM_RING;
+  g.stages = ring / g.stage_bytes;
   if (g.stages > MM_MAX_STAGES) g.stages = MM_MAX_STAGES;
   g.idesc = mm_idesc(q.pair ? 256 : 128, q.pair ? 256 : q.bn, p->type == SIM_BF16, a.t, b.t);
   g.act = p->act; g.grad = p->act_grad ? 1 : 0; g.bias = p->bias; g.bias_type = p->bias_type;

@@ -92,6 +92,24 @@ def test_gradient_against_differences(B):
         close(dz, (act(a, V + e) - act(a, V - e)) / (2 * e), 2.0**-14 + 1e-8, a)
 
 
+@pytest.mark.parametrize("cols", [96, 70])
+@pytest.mark.parametrize("a", ["none", "relu", "gelu", "silu"])
+def test_a_nan_block_stays_one(B, a, cols):
+    """The gradient through a block that could not be kept is NaN, its neighbours' is not, and so are the columns' sums."""
+    x = matrix(40, cols, torch.bfloat16, 8)
+    x[3, 40] = float("inf")
+    dy, q = matrix(40, cols, torch.bfloat16, 9), B.checkpoint(x)
+    dz, db = B.act_backward(dy, q, a)
+    bad = torch.zeros(40, cols, dtype=torch.bool, device=DEV)
+    bad[3, 32:64] = True
+    assert torch.equal(torch.isnan(dz), bad) and torch.equal(torch.isnan(db), bad.any(0))
+    w = matrix(24, cols, torch.bfloat16, 10)
+    for rows in (slice(0, 40), slice(0, 4)):
+        part = B.Checkpoint(q.codes, q.scales, 40 if rows.stop == 40 else 4, cols)
+        dx = B.linear_backward(matrix(40, 24, torch.bfloat16, 11)[rows], part, w, x_act=a, need="x")[0]
+        assert torch.equal(torch.isnan(dx), bad[rows]) or a == "none"
+
+
 def test_nothing(B):
     for rows, cols in ((0, 5), (0, 64)):
         x = torch.zeros(rows, cols, device=DEV)
