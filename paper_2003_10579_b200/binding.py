@@ -494,6 +494,7 @@ def _mx_bytes(rows, cols, layout):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _NO_STREAM = contextlib.nullcontext()
 
 
@@ -509,7 +510,9 @@ def _given(stream, device, *used):
 
 def _empty(rows, cols, dtype, device, stream):
     """A new matrix (with strides given torch takes 0.8 us less than torch.empty does)."""
-    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+    if stream is None:
+        return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
         return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
 
 
@@ -517,7 +520,7 @@ def _on(device, stream, call, *args):
     """call(*args, stream) with `device` current; stream None: the device's current one."""
     index = device.index
     st = _raw_stream(index) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         return call(*args, st)
     with torch.cuda.device(index):
         return call(*args, st)
@@ -746,7 +749,7 @@ _ALL, _HALF = tuple(DTYPES), (torch.bfloat16, torch.float16)
 
 def _plain(x, what, dtypes=_ALL):
     """A CUDA matrix (or vector: one row), possibly without elements, neighbours along the last dimension -> (rows, cols, elements between rows)."""
-    if not torch.is_tensor(x) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
         raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, " or ".join(str(d)[6:] for d in dtypes)))
     if x.dim() == 2:
         rows, cols = x.shape
@@ -760,10 +763,10 @@ def _plain(x, what, dtypes=_ALL):
     return rows, cols, ld
 
 
-def _same(device, **tensors):
-    for name, t in tensors.items():
+def _same(device, *tensors):
+    for t in tensors:
         if t is not None and t.device != device:
-            raise ValueError("%s must be on %s" % (name, device))
+            raise ValueError("all tensors must be on %s" % device)
 
 
 def _result(out, rows, cols, dtypes, device, stream, what="out"):
@@ -781,9 +784,13 @@ def _result(out, rows, cols, dtypes, device, stream, what="out"):
 def checkpoint(x, *, stream=None):
     """The 8-bit form of a matrix (or vector: one row) of float32, bfloat16 or float16."""
     rows, cols, ld = _plain(x, "x")
-    with _NO_STREAM if stream is None else _given(stream, x.device, x):
-        q = Checkpoint.empty(rows, cols, x.device)
-    _check(_on(x.device, stream, lib.sim_ckpt_write, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, q.codes_ptr, q.scales_ptr))
+    device = x.device
+    if stream is None:
+        q = Checkpoint.empty(rows, cols, device)
+    else:
+        with _given(stream, device, x):
+            q = Checkpoint.empty(rows, cols, device)
+    _check(_on(device, stream, lib.sim_ckpt_write, x.data_ptr(), DTYPES[x.dtype], rows, cols, ld, q.codes_ptr, q.scales_ptr))
     return q
 
 
@@ -854,7 +861,7 @@ def act_backward(dy, z, act, *, bias=True, dtype=torch.float32, out=None, stream
 def _side(x, what, dtypes=_HALF):
     """An operand of a product, its rows along either dimension -> (rows, cols, elements between its rows in memory, whether those lie along the
     first dimension's neighbours)."""
-    if not torch.is_tensor(x) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
+    if not isinstance(x, torch.Tensor) or not x.is_cuda or x.dtype not in dtypes or x.dim() not in (1, 2):
         raise ValueError("%s must be a CUDA tensor of %s with one or two dimensions" % (what, " or ".join(str(d)[6:] for d in dtypes)))
     if x.dim() == 2:
         rows, cols = x.shape
@@ -900,7 +907,7 @@ def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None
     kinds = (kind, torch.float32)
     if (out.dtype if out is not None else dtype or kind) not in kinds:
         raise ValueError("the result is float32 or of the operands' type")
-    _same(device, w=w, bias=bias, residual=residual)
+    _same(device, w, bias, residual)
     if bias is not None and (bias.dtype not in kinds or bias.dim() != 1 or bias.numel() != N or (N > 1 and bias.stride(0) != 1)):
         raise ValueError("bias must be a contiguous vector of %d of float32 or the operands' type" % N)
     if stream is not None:
@@ -941,7 +948,7 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
             raise ValueError("x_act belongs to a Checkpoint: a tensor x is the layer's input itself")
     if Nw != N or Mx != M or Kx != K or x.device != device:
         raise ValueError("dy [%d, %d], w [%d, %d] and x [%d, %d] do not belong together, or are on several devices" % (M, N, Nw, K, Mx, Kx))
-    _same(device, w=w, residual=residual)
+    _same(device, w, residual)
     kinds = (dy.dtype, torch.float32)
     if dtype not in kinds or not need or any(n not in "xwb" for n in need):
         raise ValueError("dtype is float32 or dy's, need is made of x, w and b")

@@ -246,7 +246,9 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int sms) {
   double best = 0.0;
   for (int bn = widest; bn >= (q.swap ? widest : 32); bn /= 2) {
     const double tiles = (double)((ra + 127) / 128) * (double)((rb + bn - 1) / bn);
-    for (int i = 0, split = 1; split <= 8 && (split == 1 || split <= kb); ++i, split *= 2) {
+    // (few rows, a tile for each multiprocessor: memory is busy without a split; 1 x 1024 x 50000 in four parts 37.3 us, whole 22.3)
+    const int most = q.swap && tiles >= sms ? 1 : 8;
+    for (int i = 0, split = 1; split <= most && (split == 1 || split <= kb); ++i, split *= 2) {
       const double t = std::ceil(tiles * split / (q.swap ? 1.3 * sms : sms)) * (((kb + split - 1) / split) * step + (q.swap ? 0.0 : bn / 64 * 0.6)) + meet[i];
       if (q.bn == 0 || t < best) { best = t; q.split = split; q.bn = bn; }
     }
@@ -383,7 +385,7 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   g.a_t = a.t; g.b_t = b.t;
   g.stage_bytes = MM_A_BYTES + (b.t ? (q.bn < 64 ? 64 : q.bn) : q.bn) * 128;
   // One block to a multiprocessor: its ring may take all shared memory (2048 x 1024 x 512: 10.4 -> 9.2 us).  Few rows and more blocks than two to a
-  // multiprocessor hold: rings for three (1 x 1000 x 50000, 391 blocks: 38.3 -> XXX us).
+  // multiprocessor hold: rings for three (1 x 4096 x 50000, 391 blocks: 102 -> 71 us with the tiles whole).
   const int64_t blocks = ta * tb * split;
   const int ring = blocks <= sms ? MM_RING_WIDE : q.swap && blocks > 2 * sms ? MM_RING_NARROW : MM_RING;
   g.stages = ring / g.stage_bytes;
