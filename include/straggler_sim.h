@@ -186,6 +186,14 @@ sim_status sim_eval_loss(sim_handle* h, float* loss);
 sim_status sim_eval_loss_mxfp4(sim_handle* h, float* loss);
 
 /*
+ * What one replica's current parameters make of samples [first, first + rows) of the data set (SOFTMAX and MLP2; SIM_ERR_ARG otherwise): the log probability of
+ * the sample's label and the entropy of its classes into DEVICE buffers [rows], the `top` likeliest classes and their log probabilities into
+ * [rows][top] (see sim_log_probs; any may be NULL).  fp32 logits, the MLP's hidden layer with bf16 operands as in its gradients.  The mean of -logp over
+ * all samples is the risk that sim_eval_loss gives.  The first call of a handle allocates room.  Enqueued on the handle's stream; does not wait.
+ */
+sim_status sim_eval_log_probs(sim_handle* h, int32_t replica, int64_t first, int64_t rows, int32_t top, float* logp, float* entropy, int32_t* top_ids, float* top_logp);
+
+/*
  * Error against wall clock, the two metrics of Section 2.3 recorded together inside sim_run: with every > 0 the
  * full-data risk F(w_j) (Eq. 1, as sim_eval_loss computes it) of every replica is recorded before the first update
  * (entry 0: F(w_0) at time 0) and after every `every`-th update (entry i: after i * every updates, at the clock of

@@ -29,7 +29,7 @@ EXPORTS = ["sim_create", "sim_set_params", "sim_set_adasync", "sim_set_adasync_l
            "sim_noalloc_last_error", "sim_adamw_create", "sim_adamw_step", "sim_adamw_step_device", "sim_adamw_destroy",
            "sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_mx_quantize", "sim_mx_dequantize", "sim_mx_matmul", "sim_set_adamw", "sim_eval_loss_mxfp4",
            "sim_ckpt_codes_bytes", "sim_ckpt_scales_bytes", "sim_ckpt_write", "sim_ckpt_read", "sim_act_backward_workspace", "sim_act_backward",
-           "sim_matmul_workspace", "sim_matmul", "sim_log_probs"]
+           "sim_matmul_workspace", "sim_matmul", "sim_log_probs", "sim_eval_log_probs"]
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # SIM_F32, SIM_BF16, SIM_F16
 MXFP4 = 3
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -125,6 +125,7 @@ def _load():
     L.sim_matmul_workspace.argtypes = [vp]           # a sim_product
     L.sim_matmul.argtypes = [vp, vp, i64, vp]
     L.sim_log_probs.argtypes = [vp, C.c_int, i64, i64, i64, vp, i32, C.c_float, i32] + [vp] * 8 + [i64, vp]
+    L.sim_eval_log_probs.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp]
     sizes = ("sim_mx_codes_bytes", "sim_mx_scales_bytes", "sim_ckpt_codes_bytes", "sim_ckpt_scales_bytes", "sim_act_backward_workspace", "sim_matmul_workspace")
     for name in EXPORTS:
         if name not in ("sim_n_params", "sim_last_error", "sim_destroy", "sim_noalloc_last_error", "sim_adamw_destroy") + sizes:
@@ -250,6 +251,22 @@ class Simulation:
         else:
             torch.cuda.synchronize()
         return out.cpu().numpy() if to_numpy else out
+
+    def log_probs(self, replica=0, first=0, rows=None, top=0, to_numpy=True):
+        """What a replica's current parameters make of samples [first, first + rows) (default: all behind first) of the data set, softmax and MLP models: dict of
+        logp (of the labels) and entropy [rows], and for top > 0 top_ids and top_logp [rows, top]."""
+        rows = (self._keep[0].shape[0] if self._keep else 0) - first if rows is None else rows
+        n = max(rows, 0)
+        out = {"logp": torch.empty((n,), dtype=torch.float32, device=self.device), "entropy": torch.empty((n,), dtype=torch.float32, device=self.device)}
+        if top > 0:
+            out["top_ids"] = torch.empty((n, top), dtype=torch.int32, device=self.device)
+            out["top_logp"] = torch.empty((n, top), dtype=torch.float32, device=self.device)
+        _check(lib.sim_eval_log_probs(self._h, replica, first, rows, top, *[_ptr(out.get(k)) for k in ("logp", "entropy", "top_ids", "top_logp")]), self._h)
+        if self.stream is not None:
+            self.stream.synchronize()
+        else:
+            torch.cuda.synchronize()
+        return {k: v.cpu().numpy() for k, v in out.items()} if to_numpy else out
 
     def error_curve(self, grid):
         """Mean minibatch loss over replicas against simulated wall clock at the times in `grid`."""

@@ -16,6 +16,7 @@
 #include "mlp_tc_kernel.cuh"
 #include "eval_kernel.cuh"
 #include "mx_eval_kernel.cuh"
+#include "predict_kernel.cuh"
 
 using namespace ssim;
 
@@ -95,6 +96,8 @@ struct sim_handle {
   uint8_t* mx_x = nullptr; uint8_t* mx_x_new = nullptr; uint8_t* mx_xs = nullptr; uint8_t* mx_w = nullptr; uint8_t* mx_ws = nullptr;
   float* mx_params = nullptr; float* mx_z = nullptr; double* mx_partial = nullptr;
   long long mx_chunk = 0, mx_ldz = 0;   // rows of data a product, logits between rows of mx_z
+  // log probabilities of samples under one replica: its parameters, W1 in bf16, and of a stretch of rows h and the logits (made on the first call)
+  float* lp_params = nullptr; __nv_bfloat16* lp_w1 = nullptr; float* lp_hidden = nullptr; float* lp_z = nullptr;
   TraceBuffers tr;
   bool poisoned = false;
   bool in_arena = false;      // buffers come from the creating thread's DeviceArena and are not freed one by one
@@ -355,6 +358,7 @@ void free_all(sim_handle* h) {
   cudaFree(h->tr.new_slot); cudaFree(h->risk); cudaFree(h->mlp_eval_part);
   cudaFree(h->adam_m); cudaFree(h->adam_v); cudaFree(h->adam_bias); cudaFree(h->mx_x_new); cudaFree(h->mx_xs); cudaFree(h->mx_w); cudaFree(h->mx_ws);
   cudaFree(h->mx_params); cudaFree(h->mx_z); cudaFree(h->mx_partial);
+  cudaFree(h->lp_params); cudaFree(h->lp_w1); cudaFree(h->lp_hidden); cudaFree(h->lp_z);
 }
 
 // MLP: bf16 copy of the data, per-update scratch and the bf16 shadow of the initial W1, made on first use
@@ -846,6 +850,63 @@ sim_status sim_eval_loss_mxfp4(sim_handle* h, float* loss) {
   const sim_model mdl = h->prob.model;
   if (mdl != SIM_LSQ && mdl != SIM_LOGISTIC && mdl != SIM_SOFTMAX) return fail(h, SIM_ERR_ARG, "the risk in MXFP4 needs a linear model (LSQ, logistic or softmax)");
   return eval_mxfp4(h, loss);
+}
+
+sim_status sim_eval_log_probs(sim_handle* h, int32_t replica, int64_t first, int64_t rows, int32_t top, float* logp, float* entropy, int32_t* top_ids, float* top_logp) {
+  if (!h) return fail(nullptr, SIM_ERR_ARG, "handle is NULL");
+  const sim_model mdl = h->prob.model;
+  if (mdl != SIM_SOFTMAX && mdl != SIM_MLP2) return fail(h, SIM_ERR_ARG, "log probabilities need a softmax or an MLP model");
+  const int C = h->prob.n_classes, d = h->prob.d, H = mdl == SIM_MLP2 ? h->prob.hidden : 0;
+  if (replica < 0 || replica >= h->R) return fail(h, SIM_ERR_ARG, "replica must be one of the handle's");
+  if (first < 0 || rows < 0 || first > h->prob.n || rows > h->prob.n - first) return fail(h, SIM_ERR_ARG, "first and rows must lie in the data set");
+  if (top < 0 || top > C) return fail(h, SIM_ERR_ARG, "top must be in [0, n_classes]");
+  if (h->poisoned) return fail(h, SIM_ERR_STATE, "the handle failed earlier");
+  if (rows == 0) return SIM_OK;
+  if ((top > 0) != (top_ids || top_logp)) return fail(h, SIM_ERR_ARG, "top_ids and top_logp go with top");
+  const long long chunk = h->prob.n < 65536 ? h->prob.n : 65536, w1 = (long long)d * H;
+  auto room = [&](auto** p, size_t count) { return *p ? cudaSuccess : dev_alloc(p, count, h->stream, false); };
+  CUDA_TRY(h, room(&h->lp_params, (size_t)h->n_params));
+  CUDA_TRY(h, room(&h->lp_z, (size_t)chunk * C));
+  if (mdl == SIM_MLP2) {
+    CUDA_TRY(h, ensure_mlp_scratch(h));
+    CUDA_TRY(h, room(&h->lp_w1, (size_t)w1));
+    CUDA_TRY(h, room(&h->lp_hidden, (size_t)chunk * H));
+  }
+  const float* w = h->lp_params;
+  if (h->uses_pool) {
+    gather_params_kernel<<<148, 256, 0, h->stream>>>(h->pool + (size_t)replica * h->n_slots * h->slot_stride, h->cur_slot + replica, h->lp_params, h->n_params, h->slot_stride, h->n_slots, 1,
+                                                      w1, mdl == SIM_MLP2 ? H : 1);
+    CUDA_TRY(h, cudaGetLastError());
+  } else {
+    w = h->w_state + (size_t)replica * h->n_params;
+  }
+  if (mdl == SIM_MLP2) {
+    round_bf16_kernel<<<592, 256, 0, h->stream>>>(w, w1, h->lp_w1);
+    CUDA_TRY(h, cudaGetLastError());
+  }
+  for (long long at = 0; at < rows; at += chunk) {
+    const long long n = rows - at < chunk ? rows - at : chunk, row0 = first + at;
+    const float* x = h->prob.X + row0 * d;
+    const unsigned grid = (unsigned)((n + 31) / 32);
+    sim_status st;
+    if (mdl == SIM_MLP2) {            // h = relu(x W1 + b1) with bf16 operands, as in the gradients; the rest in fp32
+      sim_product p{};
+      p.M = n; p.N = H; p.K = d; p.type = SIM_BF16;
+      p.a = h->mlp.Xq + row0 * d; p.lda = d;
+      p.b = h->lp_w1; p.ldb = H; p.b_t = 1;
+      p.bias = w + w1; p.bias_type = SIM_F32; p.act = SIM_ACT_RELU;
+      p.c = h->lp_hidden; p.c_type = SIM_F32; p.ldc = H;
+      if ((st = sim_matmul(&p, nullptr, 0, h->stream)) != SIM_OK) return fail(h, st, sim_last_error(nullptr));
+      row_logits_kernel<<<grid, 256, 0, h->stream>>>(h->lp_hidden, n, H, w + w1 + H, 1, C, w + w1 + H + (long long)H * C, C, h->lp_z);
+    } else {
+      row_logits_kernel<<<grid, 256, 0, h->stream>>>(x, n, d, w, d, 1, nullptr, C, h->lp_z);
+    }
+    CUDA_TRY(h, cudaGetLastError());
+    st = sim_log_probs(h->lp_z, SIM_F32, n, C, C, h->prob.label + row0, 4, 1.f, top, logp ? logp + at : nullptr, entropy ? entropy + at : nullptr, nullptr, top_ids ? top_ids + at * top : nullptr,
+                       top_logp ? top_logp + at * top : nullptr, nullptr, nullptr, nullptr, 0, h->stream);
+    if (st != SIM_OK) return fail(h, st, sim_last_error(nullptr));
+  }
+  return SIM_OK;
 }
 
 sim_status sim_set_adamw(sim_handle* h, double beta1, double beta2, double eps, float weight_decay) {
