@@ -68,7 +68,7 @@ struct LogSum {
     m4 = to4;
     due = to4 + 2.f;
     off = to4 == neg_inf() ? 0.f : -4.f * to4;
-    far = fabsf(to4) > 1048576.f && to4 != neg_inf();
+    far = fabsf(to4) > 67108864.f && to4 != neg_inf();     // up to there the rounding of m4 moves d by 16 at most, for all logits alike
   }
   __device__ __forceinline__ void move(float to4) {          // to a reference to4 >= m4
     const float by = 4.f * (to4 - m4);
@@ -327,6 +327,7 @@ __device__ __forceinline__ void rank_words(const unsigned long long* words, int 
   for (int i = threadIdx.x; i < n; i += NT) {
     const unsigned long long w = words[i];
     int above = 0;
+#pragma unroll 8
     for (int j = 0; j < n; ++j) above += words[j] > w ? 1 : 0;
     if (w && above < top) best[above] = w;
   }
@@ -442,10 +443,14 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) some(r[k]);
   }
-  for (; g < sl.groups; g += NT) {
-    Raw8<T> r;
-    sl.load(g, r);
-    some(r);
+  if (g < sl.groups) {                                                  // the last few, also together
+    Raw8<T> r[AHEAD - 1];
+#pragma unroll
+    for (int k = 0; k < AHEAD - 1; ++k)
+      if (g + k * NT < sl.groups) sl.load(g + k * NT, r[k]);
+#pragma unroll
+    for (int k = 0; k < AHEAD - 1; ++k)
+      if (g + k * NT < sl.groups) some(r[k]);
   }
   t.join_lanes<32>();
   if (lane == 0) { sh.m4[warp] = t.m4; sh.s[warp] = t.s; sh.q[warp] = t.q; }

@@ -38,7 +38,7 @@ struct MmArgs {
 // ---- the tail -----------------------------------------------------------------------------------------------------------------------
 // A lane holds 32 columns of its row, as tensor memory gives them: a block of the 8-bit form needs no exchange between lanes, and a lane
 // reads and writes whole 32-byte sectors.  (Four columns a lane through shared memory, so that a warp accesses one row at a time, took three
-// times the instructions: 1531 x 2731 outputs 2.1 us plain, 6.2 us with silu and the 8-bit form, against XXX and XXX.)
+// times the instructions: 1531 x 2731 outputs 2.1 us plain, 6.2 us with silu and the 8-bit form, against 1.1 and 3.4.)
 // Rows off 16-byte boundaries go through a patch of shared memory of the warp's own, sixteen words a row, so that lanes access neighbours.
 constexpr int MM_PATCH = 32 * 17 * 4;            // a multiple of 16: bias is read from it four at a time
 
