@@ -381,29 +381,33 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
   const int a0 = (band * 8 + in_band % band_rows) * 128, b0 = in_band / band_rows * BN;
   const int k_begin = SPLIT ? (int)blockIdx.y * g.kb_split : 0, n_it = (SPLIT ? min(g.kb, k_begin + g.kb_split) : g.kb) - k_begin;
 
-  // the loads of one stage, which the producer has found empty
-  auto load = [&](int it, int s) {
+  // the loads of one stage, which the producer has found empty, by the lane that is `on` of a converged warp
+  auto load = [&](uint32_t on, int it, int s) {
     const uint32_t at = base + (uint32_t)(s * g.stage_bytes), to_b = at + MM_A_BYTES;
     const int k0 = (k_begin + it) * 64;
-    mbar_arrive_expect_tx(full(s), (uint32_t)g.stage_bytes);
+    mbar_arrive_expect_tx_if(on, full(s), (uint32_t)g.stage_bytes);
     if (g.a_t) {
-      tma_load_2d(at, &map_a, a0, k0, full(s));
-      tma_load_2d(at + 8192, &map_a, a0 + 64, k0, full(s));
+      tma_load_2d_if(on, at, &map_a, a0, k0, full(s));
+      tma_load_2d_if(on, at + 8192, &map_a, a0 + 64, k0, full(s));
     } else {
-      tma_load_2d(at, &map_a, k0, a0, full(s));
+      tma_load_2d_if(on, at, &map_a, k0, a0, full(s));
     }
     if (g.b_t) {
-      tma_load_2d(to_b, &map_b, b0, k0, full(s));
-      if (BN > 64) tma_load_2d(to_b + 8192, &map_b, b0 + 64, k0, full(s));
+      tma_load_2d_if(on, to_b, &map_b, b0, k0, full(s));
+      if (BN > 64) tma_load_2d_if(on, to_b + 8192, &map_b, b0 + 64, k0, full(s));
     } else {
-      tma_load_2d(to_b, &map_b, k0, b0, full(s));
+      tma_load_2d_if(on, to_b, &map_b, k0, b0, full(s));
     }
   };
-  if (tid == 0) {
-    for (int s = 0; s < g.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    mbar_init(acc_bar, 1);
-    mbar_fence_init();
-    for (int it = 0; it < min(n_it, g.stages); ++it) load(it, it);       // the first round of the ring needs nobody else
+  const uint32_t on = lane == 0;
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int s = 0; s < g.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+      mbar_init(acc_bar, 1);
+      mbar_fence_init();
+    }
+    __syncwarp();
+    for (int it = 0; it < min(n_it, g.stages); ++it) load(on, it, it);       // the first round of the ring needs nobody else
   }
   if (warp == 1) tc_alloc(smem_addr(&tmem_slot), TMEM_COLS);
   tc_fence_before();
@@ -412,33 +416,35 @@ __global__ void __launch_bounds__(MM_THREADS, 2) mm_tile_kernel(const __grid_con
   const uint32_t tmem = uniform(tmem_slot);
   bool failed = false;
   if (warp == 0) {
-    if (lane == 0) {
-      int s = 0, issued = min(n_it, g.stages);
-      uint32_t phase = 0;
-      for (int it = g.stages; it < n_it; ++it) {
-        if (!mbar_try_wait(empty(s), phase) && !mbar_wait(empty(s), phase)) { failed = true; break; }
-        load(it, s);
-        issued = it + 1;
-        if (++s == g.stages) { s = 0; phase ^= 1u; }
-      }
-      if (failed)     // let what is in flight land (a bounded time) before the block gives up its shared memory
-        for (int it = max(0, issued - g.stages); it < issued; ++it) mbar_wait(full(it % g.stages), (uint32_t)((it / g.stages) & 1), 1u << 14);
+    int s = 0, issued = min(n_it, g.stages);
+    uint32_t phase = 0;
+    for (int it = g.stages; it < n_it; ++it) {
+      if (!mbar_wait_all(empty(s), phase)) { failed = true; break; }
+      load(on, it, s);
+      issued = it + 1;
+      if (++s == g.stages) { s = 0; phase ^= 1u; }
     }
-    __syncwarp();
+    if (failed)     // let what is in flight land (a bounded time) before the block gives up its shared memory
+      for (int it = max(0, issued - g.stages); it < issued; ++it) mbar_wait_all(full(it % g.stages), (uint32_t)((it / g.stages) & 1), 1u << 14);
   } else if (warp == 1) {
     const uint64_t adesc = mm_desc(base, g.a_t), bdesc = mm_desc(base + MM_A_BYTES, g.b_t);
     const uint32_t astep = mm_desc_step(g.a_t), bstep = mm_desc_step(g.b_t);
     int s = 0;
     uint32_t phase = 0;
+    bool there = false;                      // the stage's operands are known to have landed
     for (int it = 0; it < n_it; ++it) {
-      if (!mbar_wait_all(full(s), phase)) { failed = true; break; }
+      if (!there && !mbar_wait_all(full(s), phase)) { failed = true; break; }
       tc_fence_after();
       const uint32_t at = (uint32_t)(s * g.stage_bytes) >> 4;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) mm_mma(tmem, adesc + at + k * astep, bdesc + at + k * bstep, g.idesc, it > 0 || k > 0 ? 1u : 0u);
-      tc_commit_elected(empty(s));
-      if (it == n_it - 1) tc_commit_elected(acc_bar);
+      mm_mma(tmem, adesc + at, bdesc + at, g.idesc, it > 0 ? 1u : 0u);
+      mm_mma(tmem, adesc + at + astep, bdesc + at + bstep, g.idesc, 1u);
+      const int s_now = s;
       if (++s == g.stages) { s = 0; phase ^= 1u; }
+      there = __all_sync(0xFFFFFFFFu, mbar_test(full(s), phase));                   // looked at while this stage's MMAs are queued
+      mm_mma(tmem, adesc + at + 2 * astep, bdesc + at + 2 * bstep, g.idesc, 1u);
+      mm_mma(tmem, adesc + at + 3 * astep, bdesc + at + 3 * bstep, g.idesc, 1u);
+      tc_commit_elected(empty(s_now));
+      if (it == n_it - 1) tc_commit_elected(acc_bar);
     }
   }
   __syncwarp();
@@ -592,34 +598,33 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
   };
 
   if (warp == 0) {
-    if (lane == 0) {
-      Ring r(1);
-      for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
-        int a0, b0;
-        tile_at(tile, a0, b0);
-        b0 += (int)rank * 128;
-        for (int it = 0; it < g.kb; ++it, r.step<MMP_STAGES>()) {
-          if (!mbar_wait(empty(r.s), r.phase)) { failed = true; break; }
-          const uint32_t at = base + (uint32_t)r.s * MMP_STAGE, to_b = at + MMP_HALF, bar = cluster_addr(full(r.s), 0);
-          const int k0 = it * 64;
-          if (rank == 0) mbar_arrive_expect_tx(full(r.s), 2u * MMP_STAGE);
-          if (g.a_t) {
-            tma_load_2d_pair(at, &map_a, a0, k0, bar);
-            tma_load_2d_pair(at + 8192, &map_a, a0 + 64, k0, bar);
-          } else {
-            tma_load_2d_pair(at, &map_a, k0, a0, bar);
-          }
-          if (g.b_t) {
-            tma_load_2d_pair(to_b, &map_b, b0, k0, bar);
-            tma_load_2d_pair(to_b + 8192, &map_b, b0 + 64, k0, bar);
-          } else {
-            tma_load_2d_pair(to_b, &map_b, k0, b0, bar);
-          }
+    const uint32_t on = lane == 0, on_leader = on && rank == 0;
+    Ring r(1);
+    for (int tile = (int)blockIdx.x >> 1; tile < n_tiles && !failed; tile += pairs) {
+      int a0, b0;
+      tile_at(tile, a0, b0);
+      b0 += (int)rank * 128;
+      for (int it = 0; it < g.kb; ++it, r.step<MMP_STAGES>()) {
+        if (!mbar_wait_all(empty(r.s), r.phase)) { failed = true; break; }
+        const uint32_t at = base + (uint32_t)r.s * MMP_STAGE, to_b = at + MMP_HALF, bar = cluster_addr(full(r.s), 0);
+        const int k0 = it * 64;
+        mbar_arrive_expect_tx_if(on_leader, full(r.s), 2u * MMP_STAGE);
+        if (g.a_t) {
+          tma_load_2d_pair_if(on, at, &map_a, a0, k0, bar);
+          tma_load_2d_pair_if(on, at + 8192, &map_a, a0 + 64, k0, bar);
+        } else {
+          tma_load_2d_pair_if(on, at, &map_a, k0, a0, bar);
+        }
+        if (g.b_t) {
+          tma_load_2d_pair_if(on, to_b, &map_b, b0, k0, bar);
+          tma_load_2d_pair_if(on, to_b + 8192, &map_b, b0 + 64, k0, bar);
+        } else {
+          tma_load_2d_pair_if(on, to_b, &map_b, k0, b0, bar);
         }
       }
-      if (failed)
-        for (int i = 0; i < 1000; ++i) __nanosleep(1000);                       // let what is in flight land
     }
+    if (failed)
+      for (int i = 0; i < 1000; ++i) __nanosleep(1000);                         // let what is in flight land
     __syncwarp();
   } else if (warp == 1) {
     if (rank == 0) {
