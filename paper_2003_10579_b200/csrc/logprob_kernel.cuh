@@ -308,6 +308,21 @@ __device__ __forceinline__ void each_of_share(const Slice<T>& sl, int t, F f) {
   if (t < sl.tail) f(sl.tail_index() + t, sl.one(sl.tail_index() + t));
 }
 
+// Eight results that nobody reads soon
+template <int T>
+__device__ __forceinline__ void put8_past(void* p, long long i, const float (&v)[8]) {
+  if (T == T_F32) {
+    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p) + i);
+    __stcs(q, make_float4(v[0], v[1], v[2], v[3]));
+    __stcs(q + 1, make_float4(v[4], v[5], v[6], v[7]));
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = T == T_BF16 ? float_to_bf16x2(v[2 * k], v[2 * k + 1]) : float_to_f16x2(v[2 * k], v[2 * k + 1]);
+    __stcs(reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i), make_uint4(w[0], w[1], w[2], w[3]));
+  }
+}
+
 template <int NT>
 struct LogpShared {
   float m4[NT / 32], s[NT / 32], q[NT / 32];
@@ -503,22 +518,23 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     auto put = [&](int i, float x) { Elem<T>::put(out, i, d.at(x) + (i == tok ? d.g : 0.f)); };
     if (tid < sl.head) put(tid, sl.one(tid));
     if (tid < sl.tail) put(sl.tail_index() + tid, sl.one(sl.tail_index() + tid));
-    for (g = tid; g < sl.groups; g += AHEAD * NT) {
+    // from the end of the row: what was read last is what L2 still holds when the rows of all blocks are more than it takes; the gradient goes out past it
+    for (g = sl.groups - 1 - tid; g >= 0; g -= AHEAD * NT) {
       Raw8<T> raw[AHEAD];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k)
-        if (g + k * NT < sl.groups) sl.load(g + k * NT, raw[k]);
+        if (g - k * NT >= 0) sl.load(g - k * NT, raw[k]);
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        if (g + k * NT >= sl.groups) break;
-        const int at = sl.index(g + k * NT);
+        if (g - k * NT < 0) break;
+        const int at = sl.index(g - k * NT);
         float x[8];
         d.at8(raw[k], x);
         if ((unsigned)(tok - at) < 8u) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] += at + e == tok ? d.g : 0.f;
         }
-        if (wide) Elem<T>::put8(out, at, x);
+        if (wide) put8_past<T>(out, at, x);
         else
 #pragma unroll
           for (int e = 0; e < 8; ++e) Elem<T>::put(out, at + e, x[e]);

@@ -439,8 +439,8 @@ cudaError_t log_probs(const LogpArgs& a, cudaStream_t st) {
   int slices = 1;
   while (slices < 8 && a.rows * slices * 2 <= 2 * sms && a.vocab >= slices * 2 * 4096) slices *= 2;
   const int len = (int)(((a.vocab + slices - 1) / slices + 7) / 8 * 8);
-  // Many rows: blocks of 256 threads, six to a multiprocessor, whose phases mix (4096 x 131072 bf16 with eight alternatives: 220 us against 233 in blocks of
-  // 512).  Few: a thread's share is what a row takes.
+  // Many rows: blocks of 256 threads, six to a multiprocessor, whose phases mix (4096 x 131072 bf16 with eight alternatives: 220 us against 243 in blocks of
+  // 512; with the gradient, rows of 20, 100 and 256 KB: 245, 361 and 541 us against 341, 366 and 525).  Few: a thread's share is what a row takes.
   return slices == 1 ? launch_rows<T, 256>(a, slices, len, st) : launch_rows<T, 512>(a, slices, len, st);
 }
 
