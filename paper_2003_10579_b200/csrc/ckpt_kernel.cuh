@@ -5,8 +5,10 @@
 // the block exceeds 448 times it; elements are rounded to nearest even (lowbits.cuh).  33/32 of a byte an element.
 //
 // Each of the three kernels is one pass whose floor is HBM: what it reads and writes once.  Rows that start on 16-byte boundaries move in
-// whole 32-byte sectors, a thread a block or half a block; others go a warp to a block of 32, a lane an element, which still reads and
-// writes neighbours together.
+// whole 32-byte sectors, a thread a block; others go a warp to a block of 32, a lane an element, which still reads and writes neighbours together.
+// Measured at 16384 x 11264 bf16 (floors 86, 86, 143 us): written in 82 us, read through gelu in 124 (two special-function instructions an element keep that
+// unit 61 % busy), dz and its sums through gelu in 218 (issue slots 60 %, 26 instructions an element; HBM 50 %); without an activation 22 us for 33 M
+// elements read and 42 us for 92 M summed.
 #pragma once
 #include "act_math.cuh"
 #include "lowbits.cuh"
@@ -136,7 +138,7 @@ __global__ void __launch_bounds__(256) ckpt_read_kernel(const __grid_constant__ 
 
 // dz = dy act'(z) and the sums of dz (before it is rounded) over the rows.  A block takes 256 columns and split_rows rows, a warp every
 // eighth of these, a lane eight columns.  What a lane reads stays packed until its row's turn, so that the loads of two rows are
-// in flight and three blocks fit a multiprocessor.  The eight warps' sums meet in shared memory in the order of the warps; the blocks' in
+// in flight and three blocks fit a multiprocessor (four rows, or two worked on while the next two load, spill: 351 us; at two blocks 311).  The eight warps' sums meet in shared memory in the order of the warps; the blocks' in
 // the order of the splits, where there are at most eight in the distributed shared memory of a cluster, else in a second kernel: the same
 // bits every time.  KEPT = false: no z, only the sums of dy, and dz (if there is one) is a copy of dy.
 template <int T, int ACT, bool KEPT, bool VEC>
