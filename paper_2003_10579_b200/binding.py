@@ -827,7 +827,9 @@ def _scratch(nbytes, device, stream):
     """Room that a call uses until it is done (None for none)."""
     if nbytes == 0:
         return None
-    with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+    if stream is None:
+        return torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
+    with torch.cuda.stream(stream):
         return torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
 
 
@@ -848,7 +850,8 @@ def _sums(dy, rows, cols, ld, z, code, dz, lddz, db, device, stream):
 
 def _vector(out, n, dtypes, device, stream, what):
     if out is None:
-        return _empty(1, n, dtypes[0], device, stream)[0]
+        with _NO_STREAM if stream is None else torch.cuda.stream(stream):
+            return torch.empty_strided((n,), (1,), dtype=dtypes[0], device=device)
     if not out.is_cuda or out.device != device or out.dtype not in dtypes or out.dim() != 1 or out.numel() != n or not out.is_contiguous():
         raise ValueError("%s must be a contiguous vector of %d on %s" % (what, n, device))
     if stream is not None:
@@ -901,13 +904,18 @@ _PRODUCT = struct.Struct("@qqqiPqiPqiPiiiPPPqPiq")          # a sim_product; mad
 assert _PRODUCT.size == C.sizeof(SimProduct)
 
 
+def _room(p, ld, t, along, k):
+    """What sim_matmul_workspace counts for an operand: nothing where its rows in memory start on 16-byte boundaries, else their copy."""
+    rows, cols = (k, along) if t else (along, k)
+    return 0 if p & 15 == 0 and (rows <= 1 or ld & 7 == 0) else (rows * ((cols + 7) // 8) * 16 + 255) // 256 * 256
+
+
 def _product(device, stream, M, N, K, dtype, a, lda, a_t, b, ldb, b_t, c, ldc, bias=None, act=0, act_grad=False, z=None, residual=None, ldr=0):
     p = _PRODUCT.pack(M, N, K, DTYPES[dtype], a, lda, a_t, b, ldb, b_t, *((0, 0) if bias is None else (bias.data_ptr(), DTYPES[bias.dtype])), act, act_grad,
                       *((0, 0) if z is None else (z.codes_ptr, z.scales_ptr)), 0 if residual is None else residual.data_ptr(), ldr, c.data_ptr(), DTYPES[c.dtype], ldc)
-    # rows on 16-byte boundaries need no room; the library is asked for the rest
-    room = 0 if (a | b | (lda | ldb) * 2) & 15 == 0 else lib.sim_matmul_workspace(p)
-    ws = _scratch(room, device, stream).data_ptr() if room else None
-    _check(_on(device, stream, lib.sim_matmul, p, ws, room))
+    room = 0 if (a | b | (lda | ldb) * 2) & 15 == 0 else _room(a, lda, a_t, M, K) + _room(b, ldb, b_t, N, K)
+    ws = _scratch(room, device, stream)
+    _check(_on(device, stream, lib.sim_matmul, p, None if ws is None else ws.data_ptr(), room))
 
 
 def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None, out=None, stream=None):

@@ -712,7 +712,7 @@ struct MmRepack {
   struct One { const uint16_t* x; uint16_t* out; long long rows, cols, ld; } of[2];
   int n;
 };
-// 16 bytes from any even address, from the two aligned pieces that hold them (5003 x 2051 from memory: 8.7 us, element by element 8.9; from L2)
+// 16 bytes from any even address, from the two aligned pieces that hold them (5003 x 2051 from memory: 8.7 us, element by element 8.9)
 __device__ __forceinline__ uint4 unaligned16(const uint16_t* p) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p);
   const uint4* q = reinterpret_cast<const uint4*>(a & ~(uintptr_t)15);

@@ -77,6 +77,14 @@ def test_matmul(B):
     assert call(M=0, c=None) == 0 and call(N=0, b=None) == 0
 
 
+def test_the_binding_counts_a_products_room_as_the_library_does(B):
+    for a, lda, a_t, b, ldb, b_t in ((F, 32, 0, F * 2, 32, 0), (F + 2, 32, 0, F * 2, 32, 0), (F, 33, 0, F * 2 + 8, 40, 0), (F, 64, 1, F * 2, 49, 1), (F, 71, 1, F * 2, 56, 1)):
+        p = product(B, a=a, lda=lda, a_t=a_t, b=b, ldb=ldb, b_t=b_t, c=F * 3)
+        assert B.lib.sim_matmul_workspace(C.byref(p)) == B._room(a, lda, a_t, 64, 32) + B._room(b, ldb, b_t, 48, 32)
+    one = product(B, M=1, lda=32, a=F, K=31, b=F * 2, ldb=31)
+    assert B.lib.sim_matmul_workspace(C.byref(one)) == B._room(F, 32, 0, 1, 31) + B._room(F * 2, 31, 0, 48, 31) > 0
+
+
 def test_log_probs(B):
     L = B.lib
 
