@@ -954,12 +954,31 @@ def linear(x, w, bias=None, *, act="none", residual=None, keep=False, dtype=None
     return (out, z) if keep else out
 
 
+def _span(t):
+    """(first byte, behind the last, bytes between rows, bytes of a row) of a matrix or vector that has neighbours along its last dimension or its first."""
+    eb = t.element_size()
+    (ld, cols), last = max(zip(t.stride(), reversed(t.shape))) if t.dim() == 2 else (0, 0), sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1
+    return t.data_ptr(), t.data_ptr() + last * eb, ld * eb, cols * eb
+
+
+def _apart(written, others, what):
+    if written is None or written.numel() == 0:
+        return
+    lo, hi, pitch, width = _span(written)
+    for t in others:
+        if t is not None and t.numel() and t.device == written.device:
+            a, b, p, w = _span(t)
+            between = p == pitch > 0 and width <= (a - lo) % p <= p - w           # column slices of one buffer
+            if a < hi and lo < b and not between:
+                raise ValueError("%s overlaps a tensor that is still to be read, or another result" % what)
+
+
 def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=torch.float32, out=None, stream=None):
     """(dx, dw, db) of linear(x, w, bias) from dy [tokens, out], w [out, in] and x: the tensor [tokens, in] itself, or a Checkpoint.  With a
     Checkpoint v the layer's input was x_act(v) and is taken as x_act of the kept values, rounded to dy's type; dx is then the gradient by v,
     (dy w) x_act'(v).  residual [tokens, in]: added to dx (the gradient that reached the input another way).  dx has dy's type, dw [out, in]
     and db [out] have dtype (float32 or dy's).  need: which of them ("x", "w", "b"); the others are None.  out: (dx, dw, db) to write
-    into, each may be None."""
+    into, each may be None; none may lie over a tensor that another of the three still needs."""
     code = _act_code(x_act)
     M, N, lda, a_t = _side(dy, "dy")
     Nw, K, ldb, b_t = _side(w, "w", (dy.dtype,))
@@ -980,6 +999,12 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     if stream is not None:
         _given(stream, device, *(t for t in (dy, x, w, residual) if t is not None))
     dx, dw, db = out or (None, None, None)
+    if out:                                  # what is written first must leave what is read, or stays, alone: db, dx, dw in this order
+        left = ([dy] if "x" in need or "w" in need else []) + ([w, residual] if "x" in need else []) + ([] if kept or "w" not in need else [x])
+        _apart(db if "b" in need else None, left, "db")
+        _apart(dx if "x" in need else None, [] if kept or "w" not in need else [x], "dx")
+        _apart(dw if "w" in need else None, [t for n, t in (("x", dx), ("b", db)) if n in need], "dw")
+        _apart(dx if "x" in need else None, [db] if "b" in need else [], "dx")
     if "b" in need:
         if a_t:
             raise ValueError("db needs dy with neighbouring elements along its last dimension")

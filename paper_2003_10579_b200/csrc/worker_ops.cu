@@ -29,14 +29,21 @@ bool bad_matrix(int64_t rows, int64_t cols, int64_t ld) {
 }
 // rows on boundaries of `to` bytes
 bool rows_aligned(const void* p, int64_t rows, int64_t ld, sim_dtype t, int to) { return aligned(p, to) && (rows <= 1 || ld * elem_bytes(t) % to == 0); }
-// the bytes from the first element of a matrix to behind its last, and whether two such ranges share one
-struct Range { uintptr_t from, to; };
+// A matrix in memory, first byte to behind the last, rows of `width` bytes `pitch` apart; and whether two share a byte.  Rows as far apart in both, as of
+// column slices of one buffer, may lie between one another.
+struct Range { uintptr_t from, to, pitch, width; };
 Range range_of(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-  if (!p || rows < 1 || cols < 1) return Range{a, a};
-  return Range{a, a + (uintptr_t)(((rows - 1) * ld + cols) * bytes)};
+  if (!p || rows < 1 || cols < 1) return Range{a, a, 0, 0};
+  return Range{a, a + (uintptr_t)(((rows - 1) * ld + cols) * bytes), (uintptr_t)(ld * bytes), (uintptr_t)(cols * bytes)};
 }
-bool overlap(const Range& a, const Range& b) { return a.from < b.to && b.from < a.to; }
+bool overlap(const Range& a, const Range& b) {
+  if (!(a.from < b.to && b.from < a.to)) return false;
+  if (a.from == a.to || b.from == b.to) return false;
+  if (a.pitch != b.pitch) return true;
+  const uintptr_t P = a.pitch, apart = b.from >= a.from ? (b.from - a.from) % P : (P - (a.from - b.from) % P) % P;      // of b's rows behind a's
+  return apart < a.width || apart + b.width > P;
+}
 
 int sm_count() {
   int dev = 0, sms = 148;

@@ -107,3 +107,24 @@ def test_refusals_on_the_device(B):
                  lambda: B.log_probs(x, temperature=0.0), lambda: B.checkpoint_read(q, out=q.codes.view(torch.bfloat16)[:64].view(2, 32).repeat(2, 1)[:3])):
         with pytest.raises((B.SimError, ValueError)):
             call()
+
+
+def test_results_in_buffers_that_are_read_or_shared(B):
+    """Column slices of one buffer hold operand and result; a gradient over the input that another gradient still needs is refused, over one that nothing needs it is not."""
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    T, n = 70, 64
+    x, w, dy = normal(gen, T, n), normal(gen, n, n), normal(gen, T, n)
+    want = B.linear_backward(dy, x, w)
+    buf = torch.zeros(T, 4 * n, dtype=torch.bfloat16, device=DEV)
+    buf[:, n: 2 * n] = x
+    B.linear(buf[:, n: 2 * n], w, act="gelu", out=buf[:, 2 * n: 3 * n])
+    dx, dw, db = B.linear_backward(dy, buf[:, n: 2 * n], w, out=(buf[:, :n], None, None))
+    assert torch.equal(buf[:, 2 * n: 3 * n], B.linear(x, w, act="gelu")) and torch.equal(buf[:, n: 2 * n], x) and not buf[:, 3 * n:].any()
+    assert all(torch.equal(a, b) for a, b in zip((dx, dw, db), want))
+    one = torch.empty(T, n, dtype=torch.bfloat16, device=DEV)
+    for out in ((x, None, None), (x[:, :], None, None), (None, None, w[0]), (None, None, dy[0]), (one, one[:n], None), (one, None, one[0]), (None, one[:n], one[1])):
+        with pytest.raises((ValueError, B.SimError)):
+            B.linear_backward(dy, x, w, out=out, dtype=torch.bfloat16)
+    assert torch.equal(buf[:, n: 2 * n], x)
+    got = B.linear_backward(dy, x, w, need="x", out=(x, None, None))[0]
+    assert got is x and torch.equal(x, want[0])

@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 F = 0x100000                      # never dereferenced: every case below fails validation first
 
@@ -75,6 +76,34 @@ def test_matmul(B):
     assert room == 64 * 32 * 2 and L.sim_matmul_workspace(C.byref(product(B))) == 0
     assert call(lda=33) == 1 and call(F * 9, room - 1, lda=33) == 1 and call(F * 9 + 16, room, lda=33) == 1 and call(F * 3, room, lda=33) == 1 and b"workspace" in L.sim_last_error(None)
     assert call(M=0, c=None) == 0 and call(N=0, b=None) == 0
+
+
+def test_columns_of_one_buffer_do_not_overlap(B):
+    """c in columns beside a's (or behind, or wrapped into the next row's start) is no overlap, one element more is.  Nothing is launched: the calls that pass this
+    check fail the one of the workspace."""
+    L = B.lib
+
+    def call(c, N, ldc=100, lda=100):
+        p = product(B, a=F, lda=lda, c=c, ldc=ldc, N=N, b=F * 2 + 2, ldb=33)
+        assert L.sim_matmul(C.byref(p), None, 0, None) == 1
+        return b"workspace" in L.sim_last_error(None)
+
+    assert call(F + 64, 48) and call(F + 64, 68) and not call(F + 62, 48) and not call(F + 64, 69)
+    assert call(F - 200 * 3 + 64, 68) and not call(F - 200 * 3 + 64, 69) and not call(F - 2, 5) and call(F - 10, 5)
+    assert not call(F + 64, 48, ldc=104) and not call(F + 64, 48, lda=104)
+
+
+def test_spans_of_tensors(B):
+    buf = torch.zeros(5, 100, dtype=torch.bfloat16)
+    ok, bad = ((buf[:, :32], buf[:, 32:80]), (buf[:, 32:], buf[:, :32]), (buf[:2], buf[2:]), (buf[0], buf[1]), (buf.t()[:32], buf[:, 32:]), (buf[:1, 3:4], buf[:, 4:])), (
+        (buf[:, :33], buf[:, 32:80]), (buf[:, 32:], buf[:, :33]), (buf[:3], buf[2:]), (buf, buf), (buf.t()[:33], buf[:, 32:]), (buf[0, :5], buf[0, 4:]))
+    for a, b in ok:
+        B._apart(a, [None, b], "a")
+        B._apart(b, [a], "b")
+    for a, b in bad:
+        for u, v in ((a, b), (b, a)):
+            with pytest.raises(ValueError):
+                B._apart(u, [v], "u")
 
 
 def test_the_binding_counts_a_products_room_as_the_library_does(B):
