@@ -159,45 +159,57 @@ cudaError_t repack(Operand& a, Operand& b, char* room, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// Launches a product; `copied`: behind copies of its operands, which it awaits itself
+template <typename K>
+cudaError_t launch_mm(K kern, dim3 grid, int threads, size_t smem, int cluster_x, int cluster_y, bool copied, const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, cudaStream_t st) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2] = {};
+  unsigned n = 0;
+  if (cluster_x * cluster_y > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)cluster_x; attr[n].val.clusterDim.y = (unsigned)cluster_y; attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (copied) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kern, ma, mb, g);
+}
 template <int T>
-cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int sms, cudaStream_t st) {
+cudaError_t launch_pair(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int sms, bool copied, cudaStream_t st) {
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = allow_smem(mm_pair_kernel<T>, MMP_SMEM, done);
   if (e != cudaSuccess) return e;
   const long long tiles = (long long)g.tiles_a * g.tiles_b, pairs = sms / 2;
-  mm_pair_kernel<T><<<(unsigned)(2 * (tiles < pairs ? tiles : pairs)), MMP_THREADS, MMP_SMEM, st>>>(ma, mb, g);
-  return cudaGetLastError();
+  return launch_mm(mm_pair_kernel<T>, dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)), 1, 1), MMP_THREADS, MMP_SMEM, 1, 1, copied, ma, mb, g, st);    // in clusters of two, as declared
 }
 template <int BN, int T, bool SWAP, bool SPLIT>
-cudaError_t launch_tile(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, cudaStream_t st) {
+cudaError_t launch_tile(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, bool copied, cudaStream_t st) {
   auto kern = mm_tile_kernel<BN, T, SWAP, SPLIT>;
   static_assert(mm_part_bytes(BN, SWAP) <= (SWAP ? MM_RING_NARROW : MM_OFF_PATCH), "the sums and the patches lie in the ring's bytes");
   static std::atomic<unsigned long long> done{0};
   cudaError_t e = allow_smem(kern, MM_RING_WIDE + 1024, done);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1);
-  cfg.blockDim = dim3(MM_THREADS, 1, 1);
-  cfg.dynamicSmemBytes = (size_t)(SWAP ? g.stages * g.stage_bytes : g.stages * g.stage_bytes > MM_RING ? MM_RING_WIDE : MM_RING) + 1024;
-  cfg.stream = st;
-  cudaLaunchAttribute attr{};
-  if (SPLIT) {
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 1; attr.val.clusterDim.y = (unsigned)split; attr.val.clusterDim.z = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-  }
-  return cudaLaunchKernelEx(&cfg, kern, ma, mb, g);
+  const int ring = SWAP ? g.stages * g.stage_bytes : g.stages * g.stage_bytes > MM_RING ? MM_RING_WIDE : MM_RING;
+  return launch_mm(kern, dim3((unsigned)(g.tiles_a * g.tiles_b), (unsigned)split, 1), MM_THREADS, (size_t)ring + 1024, 1, split, copied, ma, mb, g, st);
 }
 template <int BN, int T, bool SWAP>
-cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, cudaStream_t st) {
-  return split > 1 ? launch_tile<BN, T, SWAP, true>(ma, mb, g, split, st) : launch_tile<BN, T, SWAP, false>(ma, mb, g, split, st);
+cudaError_t launch_split(const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, bool copied, cudaStream_t st) {
+  return split > 1 ? launch_tile<BN, T, SWAP, true>(ma, mb, g, split, copied, st) : launch_tile<BN, T, SWAP, false>(ma, mb, g, split, copied, st);
 }
 template <int T>
-cudaError_t launch_product(bool pair, bool swap, int bn, const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, int sms, cudaStream_t st) {
-  if (pair) return launch_pair<T>(ma, mb, g, sms, st);
-  if (swap) return bn == 16 ? launch_split<16, T, true>(ma, mb, g, split, st) : bn == 32 ? launch_split<32, T, true>(ma, mb, g, split, st) : launch_split<64, T, true>(ma, mb, g, split, st);
-  return bn == 32 ? launch_split<32, T, false>(ma, mb, g, split, st) : bn == 64 ? launch_split<64, T, false>(ma, mb, g, split, st) : launch_split<128, T, false>(ma, mb, g, split, st);
+cudaError_t launch_product(bool pair, bool swap, int bn, const CUtensorMap& ma, const CUtensorMap& mb, const MmArgs& g, int split, int sms, bool copied, cudaStream_t st) {
+  if (pair) return launch_pair<T>(ma, mb, g, sms, copied, st);
+  if (swap) return bn == 16 ? launch_split<16, T, true>(ma, mb, g, split, copied, st) : bn == 32 ? launch_split<32, T, true>(ma, mb, g, split, copied, st) : launch_split<64, T, true>(ma, mb, g, split, copied, st);
+  return bn == 32 ? launch_split<32, T, false>(ma, mb, g, split, copied, st) : bn == 64 ? launch_split<64, T, false>(ma, mb, g, split, copied, st) : launch_split<128, T, false>(ma, mb, g, split, copied, st);
 }
 
 const char* product_refusal(const sim_product* p) {
@@ -405,8 +417,8 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   if (K > 0 && (!make_map(&ma, a.p, p->type, a.rows, a.cols, a.ld, a.t ? 64 : 128) ||
                 !make_map(&mb, b.p, p->type, b.rows, b.cols, b.ld, b.t ? 64 : q.pair ? 128 : (uint32_t)q.bn)))
     return record_error(SIM_ERR_CUDA, "sim_matmul: the driver refused a tensor map");
-  e = p->c_type == SIM_F32 ? launch_product<T_F32>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, st)
-      : p->c_type == SIM_BF16 ? launch_product<T_BF16>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, st) : launch_product<T_F16>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, st);
+  e = p->c_type == SIM_F32 ? launch_product<T_F32>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, need > 0, st)
+      : p->c_type == SIM_BF16 ? launch_product<T_BF16>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, need > 0, st) : launch_product<T_F16>(q.pair, q.swap, q.bn, ma, mb, g, split, sms, need > 0, st);
   return e == cudaSuccess ? SIM_OK : cuda_failed("sim_matmul", e);
 }
 

@@ -128,3 +128,26 @@ def test_results_in_buffers_that_are_read_or_shared(B):
     assert torch.equal(buf[:, n: 2 * n], x)
     got = B.linear_backward(dy, x, w, need="x", out=(x, None, None))[0]
     assert got is x and torch.equal(x, want[0])
+
+
+def test_copied_operands_replayed(B):
+    """Operands off 16-byte boundaries, whose copies the products overtake: captured once, replayed behind one another over changing inputs."""
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    for T, fin, fout in ((37, 333, 1003), (1800, 521, 2049)):
+        x, w, dy = normal(gen, T, fin), normal(gen, fout, fin, scale=0.05), normal(gen, T, fout)
+        B.linear_backward(dy, x, w)                  # loads the kernels
+        B.linear(x, w)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            y = B.linear(x, w, act="silu")
+            got = (y,) + B.linear_backward(dy, x, w)
+        runs = [(normal(gen, T, fin), normal(gen, fout, fin, scale=0.05), normal(gen, T, fout)) for _ in range(4)]
+        want = [(B.linear(a, b, act="silu"),) + B.linear_backward(c, a, b) for a, b, c in runs]
+        out = []
+        for a, b, c in runs:
+            x.copy_(a), w.copy_(b), dy.copy_(c)
+            g.replay()
+            out.append([t.clone() for t in got])
+        torch.cuda.synchronize()
+        for o, e in zip(out, want):
+            assert all(torch.equal(u, v) for u, v in zip(o, e))
