@@ -833,9 +833,13 @@ def _scratch(nbytes, device, stream):
         return torch.empty_strided((nbytes,), (1,), dtype=torch.uint8, device=device)
 
 
+def _pitch(cols):
+    return -(-cols // 8) * 8 if cols <= 64 else -(-cols // 64) * 64
+
+
 def _padded(rows, cols, dtype, device, stream):
-    """(a matrix whose rows start on 16-byte boundaries, the elements between them)"""
-    ld = -(-cols // 8) * 8
+    """(a matrix whose rows start on 16-byte boundaries, and on lines where they are longer than one, the elements between them)"""
+    ld = _pitch(cols)
     with _NO_STREAM if stream is None else torch.cuda.stream(stream):
         return torch.empty_strided((rows, cols), (ld, 1), dtype=dtype, device=device), ld
 
@@ -907,7 +911,7 @@ assert _PRODUCT.size == C.sizeof(SimProduct)
 def _room(p, ld, t, along, k):
     """What sim_matmul_workspace counts for an operand: nothing where its rows in memory start on 16-byte boundaries, else their copy."""
     rows, cols = (k, along) if t else (along, k)
-    return 0 if p & 15 == 0 and (rows <= 1 or ld & 7 == 0) else (rows * ((cols + 7) // 8) * 16 + 255) // 256 * 256
+    return 0 if p & 15 == 0 and (rows <= 1 or ld & 7 == 0) else (rows * _pitch(cols) * 2 + 255) // 256 * 256
 
 
 def _product(device, stream, M, N, K, dtype, a, lda, a_t, b, ldb, b_t, c, ldc, bias=None, act=0, act_grad=False, z=None, residual=None, ldr=0):

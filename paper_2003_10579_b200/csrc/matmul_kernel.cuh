@@ -13,6 +13,8 @@
 // about 4 us of launch, set-up and tail (2048 x 1024 x 512 7.7 us, 600^3 6.7); few rows the weights' way from memory (1 x 4096 x 12288 20.3 us, floor 15.4).
 // Waits are bounded; where one runs out the tile is written as NaN.
 #pragma once
+#include <type_traits>
+
 #include "act_math.cuh"
 #include "ckpt_kernel.cuh"
 #include "lowbits.cuh"
@@ -58,22 +60,25 @@ __device__ __forceinline__ void mm_patch_rows(uint32_t* patch, int lane, uint32_
   constexpr int STEP = T == T_F32 ? 2 : 1;
   const int r0 = T == T_F32 ? lane >> 4 : 0, c = T == T_F32 ? lane & 15 : lane;
   const int left = col0 + c < n_cols ? (int)min(32ll, n_rows - row0) : 0;
-  const long long first = (row0 + r0) * ld + col0 + c, step = STEP * ld;
-  if (T == T_F32) {
-    uint32_t* at = static_cast<uint32_t*>(rows) + first;
-    uint32_t* in = patch + r0 * 17 + c;
-#pragma unroll 4
-    for (int r = r0; r < left; r += STEP, at += step, in += STEP * 17) {
-      if (WRITE) *at = *in;
-      else *in = *at;
-    }
-  } else {
-    uint16_t* at = static_cast<uint16_t*>(rows) + first;
-    uint16_t* in = reinterpret_cast<uint16_t*>(patch + r0 * 17) + c;
+  const long long step = STEP * ld;
+  using E = typename std::conditional<T == T_F32, uint32_t, uint16_t>::type;
+  constexpr int PITCH = 68 / sizeof(E);      // of the patch's rows
+  E* at = static_cast<E*>(rows) + ((row0 + r0) * ld + col0 + c);
+  E* in = reinterpret_cast<E*>(patch) + r0 * PITCH + c;
+  if (WRITE) {
 #pragma unroll 8
-    for (int r = r0; r < left; r += STEP, at += step, in += STEP * 34) {
-      if (WRITE) *at = *in;
-      else *in = *at;
+    for (int r = r0; r < left; r += STEP, at += step, in += STEP * PITCH) *at = *in;
+  } else {
+    // sixteen loads under way (one behind the other, each waiting for its place in the patch: 1531 x 2731 x 1001 with a residual 32.4 us, 23.0 so)
+#pragma unroll 1
+    for (int r = r0; r < 32; r += 16 * STEP) {
+      E t[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t[i] = r + i * STEP < left ? at[i * step] : (E)0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) in[i * STEP * PITCH] = t[i];
+      at += 16 * step;
+      in += 16 * STEP * PITCH;
     }
   }
   __syncwarp();
@@ -312,7 +317,7 @@ __device__ __forceinline__ V uniform(V v) { return __shfl_sync(0xFFFFFFFFu, v, 0
 // Where operands are copied first, the product is launched while the copy runs and sets itself up; the warp that loads the operands, the only one that touches
 // what the copy writes, waits here until all of that is done, and the others for it at a barrier: no wait with a limit begins before.  The copy itself
 // is launched behind everything before it, so what else the product reads and writes is in order.  Without a copy this returns at once.  (37 x 2051 x 5003
-// 24.1 -> 22.5 us, a block of 1531 x 1001 x 2731 forward and backward 227 -> 215.)
+// 24.1 -> 22.5 us, a block of 1531 x 1001 x 2731 forward and backward 227 -> 215; both since faster by their copies' rows on lines.)
 __device__ __forceinline__ void await_copies() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // Issued by one elected lane of a converged warp
@@ -714,10 +719,10 @@ mm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 }
 
 // ---- operands that TMA cannot read -----------------------------------------------------------------------------------------------------
-// Rows that do not start on 16-byte boundaries are copied to rows that do (cols rounded up to eight elements) before the product: one read
+// Rows that do not start on 16-byte boundaries are copied to rows that do before the product: one read
 // and one write more of an operand that the tiles read many times.
 struct MmRepack {
-  struct One { const uint16_t* x; uint16_t* out; long long rows, cols, ld; } of[2];
+  struct One { const uint16_t* x; uint16_t* out; long long rows, cols, ld, pitch; } of[2];
   int n;
 };
 // 16 bytes from any even address, from the two aligned pieces that hold them (5003 x 2051 from memory: 8.7 us, element by element 8.9)
@@ -762,7 +767,7 @@ __global__ void __launch_bounds__(256) mm_repack_kernel(const __grid_constant__ 
         for (int k = 0; k < 8; ++k) e[k] = c + k < o.cols ? src[k] : 0u;
         v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
       }
-      *reinterpret_cast<uint4*>(o.out + (at.row * pieces + at.at) * 8) = v;
+      *reinterpret_cast<uint4*>(o.out + at.row * o.pitch + c) = v;
     }
   }
 }

@@ -132,7 +132,10 @@ struct Operand {
   int64_t along;               // rows of c's side: what a tile counts
   int t;
   bool fits;                   // TMA can read it
-  int64_t copy_bytes() const { return fits ? 0 : rows * ((cols + 7) / 8 * 8) * 2; }
+  // of a copy: rows of more than a line of memory start on lines (2300 x 5000 x 900 with its rows on 16-byte
+  // boundaries 37 us, on lines 23.4; 1531 x 2736 x 1001 16.8 and 15.2: a box's rows else take parts of two lines each)
+  int64_t pitch() const { return cols <= 64 ? (cols + 7) / 8 * 8 : (cols + 63) / 64 * 64; }
+  int64_t copy_bytes() const { return fits ? 0 : rows * pitch() * 2; }
 };
 Operand operand(const void* p, int64_t ld, int t, int64_t along, int64_t k) {
   Operand o{p, t ? k : along, t ? along : k, ld, along, t ? 1 : 0, true};
@@ -148,11 +151,11 @@ cudaError_t repack(Operand& a, Operand& b, char* room, cudaStream_t st) {
     Operand& o = *both[i];
     if (o.fits) continue;
     MmRepack::One& one = r.of[r.n++];
-    one.x = static_cast<const uint16_t*>(o.p); one.out = reinterpret_cast<uint16_t*>(room); one.rows = o.rows; one.cols = o.cols; one.ld = o.ld;
+    one.x = static_cast<const uint16_t*>(o.p); one.out = reinterpret_cast<uint16_t*>(room); one.rows = o.rows; one.cols = o.cols; one.ld = o.ld; one.pitch = o.pitch();
     pieces += o.rows * ((o.cols + 7) / 8);
     room += (o.copy_bytes() + 255) / 256 * 256;
     o.p = one.out;
-    o.ld = (o.cols + 7) / 8 * 8;
+    o.ld = one.pitch;
   }
   if (r.n == 0) return cudaSuccess;
   mm_repack_kernel<<<grid_for(pieces), 256, 0, st>>>(r);
@@ -250,9 +253,10 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int sms) {
   q.swap = M <= 64 && M <= N;
   const int64_t ra = q.swap ? N : M, rb = q.swap ? M : N;
   const int kb = (int)((K + 63) / 64);
-  // Pairs of multiprocessors from two tiles for three pairs on (1531 x 1008 x 2736, 66 tiles of 256 x 256: 13.5 us against 15.0 in tiles of 128 x
-  // 128; 1024 x 4096 x 4096, 64: 28 against 33; 700 x 1024 x 3000, 36: 13.6 against 11.4; 300 x 4096 x 4096, 32: 26 against 23)
-  q.pair = kb > 0 && ra > 128 && rb > 128 && 3 * ((ra + 255) / 256 * ((rb + 255) / 256)) >= 2 * (sms / 2);
+  // Pairs of multiprocessors where tiles of 128 x 128 would take turns (1008 x 1531 x 2736, 176 such tiles: 13.9 us against 18.1; 2048 x 2048 x 1200, 160:
+  // 16.1 against 16.0; 1536 x 8192 x 1664, 156: 42.7 against 44.1; 1800 x 64 x 1400, 165: 7.4 against 6.9; 1531 x 1008 x 2736, 264: 11.8 against 13.8).  Where each has a multiprocessor, not
+  // (640 x 8192 x 3000, 120 tiles: 43 against 33; 300 x 4096 x 4096, 96: 24.6 against 18.5; 700 x 1024 x 3000, 144: 12.1 against 8.9)
+  q.pair = kb > 0 && ra > 128 && rb > 128 && (ra + 127) / 128 * ((rb + 127) / 128) > sms;
   q.split = 1;
   if (q.pair) return q;
   // Else the time of each tile width and split, estimated (us).  64 elements of k cost a block 0.25 (few rows, whose weights come from memory: 0.3), more
