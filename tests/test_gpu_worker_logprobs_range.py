@@ -1,0 +1,76 @@
+"""Gradients of log probabilities at the ends of what a call takes, against 64 bits: masks beside large derivatives and low temperatures.
+
+Tolerances, relative to a probability where nothing else is said.  In powers of two a logit is d = c x - m, c rounded once (2^-24 of it), m exact: what
+is common to a row's logits cancels, so a logit's numerator is off by e = 2^-24 (2 |log2 p| + 40) (c and one rounding of d, |d| <= |log2 p| + log2 s, log2 s <= 33
+with m up to 16 below the largest) and by the power's own 2^-22.  A sum adds n = 1 + vocab / 128 terms one by one and then a tree of less than 32 levels, and
+is moved to another m a few times (2^-20 in all): S = (n + 32) 2^-24 + 2^-20 + the mean of e.  So a probability is off by P = e + S + 2^-21, its logarithm by as much,
+and the entropy, logarithms of at most L = 2 log2(vocab) + 10 so weighed, by 2 R (L + 2), R = S + 40 2^-24.  A gradient is (exp2(d) (a d + b) + g) / T, its own
+rounding 2^-22 of |a| (|d| + 33) + |b|; then half a step of its type.  A power under 2^-126 may be taken as zero: p is off by 2^-125 at most (s >= 1/2)."""
+import numpy as np
+import pytest
+import torch
+
+from worker_ref import EPS, TINY, close, f64
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2003_10579_b200 import binding
+    return binding
+
+
+def rows_of(x, T):
+    """log p, p, entropy of finite or masked (-inf) logits as they are stored; the mean of e."""
+    l = x / T
+    top = l.max(1, keepdims=True)
+    lp = (l - top) - np.log(np.exp(l - top).sum(1, keepdims=True))
+    p = np.exp(lp)
+    lp = np.where(p > 0, lp, 0.0)
+    return lp, p, -(p * lp).sum(1)
+
+
+def expect(x, t, T, g, h):
+    """The gradient and its tolerance."""
+    lp, p, H = rows_of(x, T)
+    rows, vocab = x.shape
+    e = 2.0**-24 * (2 * np.abs(lp) / np.log(2) + 40)
+    S = ((33 + vocab / 128) * 2.0**-24 + 2.0**-20 + (p * e).sum(1))[:, None]
+    P, L, R = e + S + 2.0**-21, 2 * np.log2(vocab) + 10, S + 40 * 2.0**-24
+    d = -p * g[:, None] - h[:, None] * p * (lp + H[:, None])
+    ag, ah, size = np.abs(g)[:, None], np.abs(h)[:, None], np.abs(lp) + H[:, None]
+    tol = p * (ag * P + ah * (size * P + P + 2 * R * (L + 2))) + (2.0**-22 * p + 2.0**-125) * (ag + ah * (size + 66 + 33))
+    r = np.arange(rows)
+    d[r, t] += g
+    tol[r, t] += 2.0**-22 * np.abs(g)
+    return d / T, tol / T, p
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("vocab", [100, 1031, 5003, 50021])
+@pytest.mark.parametrize("T,weight", [(0.001, 1e3), (0.001, 1e6), (0.01, 1e5), (0.1, 1e8), (1.0, 1e9)])
+def test_masked_logits_beside_large_derivatives_by_entropy(B, dt, vocab, T, weight):
+    """What is masked has probability zero and no gradient, however large its factor would be."""
+    gen = torch.Generator(device=DEV).manual_seed(vocab)
+    x = (torch.randn(5, vocab, generator=gen, device=DEV) * T).to(dt)          # spread by one once divided by T: many classes count
+    x[0, ::3] = float("-inf")
+    x[1, vocab // 2:] = torch.finfo(dt).min
+    x[2, 1::2] = -60000.0 if dt == torch.float16 else -1.5e30
+    x[3] = float("-inf")
+    x[3, vocab // 2] = 0.5
+    t = torch.tensor([1, 0, 2, vocab // 2, 3], device=DEV)
+    g = torch.tensor([1.0, -2.0, 0.5, 1.0, 3.0], device=DEV)
+    h = torch.tensor([1.0, -1.0, 1.0, 1.0, 0.5], device=DEV) * weight
+    want, tol, p = expect(f64(x), t.cpu().numpy(), T, f64(g), f64(h))
+    if dt == torch.float16:                                                     # beyond the type's largest number: infinite
+        big = np.abs(want) > 60000.0
+        want, tol = np.where(big, 0.0, want), np.where(big, 0.0, tol)
+    for got in (B.log_probs(x, t, temperature=T, d_logp=g, d_entropy=h).dlogits, B.log_probs_backward(x, t, g, h, temperature=T)):
+        d = f64(got)
+        assert not np.isnan(d).any() and (d[p == 0] == 0).all()
+        if dt == torch.float16:
+            d = np.where(big, 0.0, d)
+        close(d, want, tol + (EPS[dt] + 2.0**-22) * np.abs(want) + TINY[dt], "dlogits")
