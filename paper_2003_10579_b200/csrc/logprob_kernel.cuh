@@ -176,26 +176,28 @@ struct LogRow {
   }
 };
 
-// The gradient by a logit: p (a lp + b), lp = log2 p; at the token plus g / T
+// The gradient by a logit, p (a lp + b) with lp = log2 p = d - log2 s, as 2^d (a' d + b'), a' = a / s, b' = (b - a log2 s) / s; at the token plus g / T.  d is what the sums
+// took: log2 s joined to the addend of c x loses its digits beside a far reference (logits around 1e6: p off by 1.6 %, and a row's gradients then
+// do not sum to zero).
 struct LogGrad {
-  float c, c4, o, m4, l2, a, b, g;
-  uint32_t low;                             // twice, in bf16: a logit whose lp is LP_NONE or below, by the rounding's step at most
+  float c, c4, off, m4, a, b, g;            // a and b: the ones above with a dash
+  uint32_t low;                             // twice, in bf16: a logit whose d is LP_NONE or below, by the rounding's step at most
   bool far, none;
   __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow& r, float g_, float h) {
-    c = k.c; c4 = k.c4; m4 = r.t.m4; l2 = r.l2; far = r.t.far; none = r.none;
-    o = -fmaf(4.f, m4, l2);
-    a = -h * LP_LN2 * k.inv_t;
-    b = -(g_ + h * r.entropy()) * k.inv_t;
+    c = k.c; c4 = k.c4; off = r.t.off; m4 = r.t.m4; far = r.t.far; none = r.none;
+    const float by_lp = -h * LP_LN2 * k.inv_t, inv_s = 1.f / r.t.s;
+    a = by_lp * inv_s;
+    b = (-(g_ + h * r.entropy()) * k.inv_t - by_lp * r.l2) * inv_s;
     g = none ? 0.f : g_ * k.inv_t;
-    const uint32_t w = __float_as_uint((LP_NONE - o) / c);
+    const uint32_t w = __float_as_uint((LP_NONE - off) / c);
     low = ((int32_t)w < 0 ? (w + 0xFFFFu) >> 16 : w >> 16) * 0x10001u;          // rounded down
   }
   __device__ __forceinline__ float at(float x) const {
     if (none) return 0.f;
-    const float lp = max_nan(far ? 4.f * (__fmul_rn(x, c4) - m4) - l2 : fmaf(x, c, o), LP_NONE);
-    return exp2_fast(lp) * fmaf(a, lp, b);
+    const float d = max_nan(far ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, off), LP_NONE);
+    return exp2_fast(d) * fmaf(a, d, b);
   }
-  // bf16: logits are kept at `low` or above two at a time, so that no lp is far below LP_NONE: with -inf, or a mask's lowest number, a lp + b could be
+  // bf16: logits are kept at `low` or above two at a time, so that no d is far below LP_NONE: with -inf, or a mask's lowest number, a d + b could be
   // infinite beside the probability zero (-1e30 as the least: NaN from d_entropy = 342 on at T = 0.001)
   template <int T>
   __device__ __forceinline__ void at8(const Raw8<T>& r, float (&x)[8]) const {
@@ -206,8 +208,8 @@ struct LogGrad {
         for (int k = 0; k < 4; ++k) f.w[k] = max_nan_bf16x2(r.w[k], low);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float lp = fmaf(f.value(e), c, o);
-          x[e] = exp2_fast(lp) * fmaf(a, lp, b);
+          const float d = fmaf(f.value(e), c, off);
+          x[e] = exp2_fast(d) * fmaf(a, d, b);
         }
         return;
       }

@@ -74,3 +74,29 @@ def test_masked_logits_beside_large_derivatives_by_entropy(B, dt, vocab, T, weig
         if dt == torch.float16:
             d = np.where(big, 0.0, d)
         close(d, want, tol + (EPS[dt] + 2.0**-22) * np.abs(want) + TINY[dt], "dlogits")
+
+
+@pytest.mark.parametrize("vocab,rows", [(10, 6), (700, 6), (3001, 6), (20011, 4), (50021, 3), (9001, 300)])
+@pytest.mark.parametrize("dt,off,spread,T", [(torch.float32, 1e4, 2.5, 1.0), (torch.float32, -1e4, 2.5, 1.0), (torch.float32, 1e6, 2.5, 1.0), (torch.float32, 1e8, 25.0, 1.0), (torch.float32, 300.0, 0.02, 0.01),
+                                             (torch.float32, 1e6, 0.1, 0.01), (torch.float16, 6e4, 32.0, 1.0), (torch.float16, 6e4, 32.0, 50.0), (torch.float16, 6e4, 32.0, 0.001), (torch.bfloat16, 1e6, 8000.0, 1000.0),
+                                             (torch.bfloat16, 3e4, 100.0, 1.0)])
+def test_rows_far_from_zero(B, dt, off, spread, T, vocab, rows):
+    """An offset that all logits of a row share changes nothing but lse, and takes no digits from probabilities and gradients."""
+    gen = torch.Generator(device=DEV).manual_seed(vocab + rows)
+    x = (torch.randn(rows, vocab, generator=gen, device=DEV, dtype=torch.float64) * spread + off).to(dt)
+    t = torch.randint(0, vocab, (rows,), generator=gen, device=DEV)
+    t[0] = x[0].argmax()
+    g, h = torch.randn(rows, generator=gen, device=DEV), torch.randn(rows, generator=gen, device=DEV)
+    X, tok = f64(x), t.cpu().numpy()
+    lp, p, H = rows_of(X, T)
+    lp_t = (X / T - (X / T).max(1, keepdims=True))[np.arange(rows), tok] - np.log(np.exp(X / T - (X / T).max(1, keepdims=True)).sum(1))
+    S = (33 + vocab / 128) * 2.0**-24 + 2.0**-20 + 80 * 2.0**-24
+    for gg, hh in ((g, h), (g, torch.zeros_like(h)), (torch.zeros_like(g), h)):
+        got = B.log_probs(x, t, temperature=T, d_logp=gg, d_entropy=hh)
+        want, tol, _ = expect(X, tok, T, f64(gg), f64(hh))
+        close(got.dlogits, want, tol + (EPS[dt] + 2.0**-22) * np.abs(want) + TINY[dt], "dlogits")
+        if dt == torch.float32:                      # a row's gradient sums to nothing
+            assert (np.abs(f64(got.dlogits).sum(1)) <= tol.sum(1) + 2.0**-23 * np.abs(want).sum(1)).all()
+    close(got.logp, lp_t, S + 2.0**-22 * np.abs(lp_t), "logp")
+    close(got.entropy, H, 2 * S * (2 * np.log2(vocab) + 12), "entropy")
+    close(got.lse, (X / T).max(1) + np.log(np.exp(X / T - (X / T).max(1, keepdims=True)).sum(1)), S + 2.0**-22 * np.abs(X / T).max(1) + 2.0**-22 * 40, "lse")
