@@ -5,7 +5,8 @@
 // one pass over the row with running m, s, q a thread.  m being whole, moving it scales s and q exactly, and a thread moves it only
 // when a logit is over 2^8 times (in 2^d) beyond it, so the rescaling's exponential is rare.  s and q are fp32: a thread adds at most
 // vocab / threads terms, then the threads meet in a tree.  m is kept in quarters, m4 = m / 4: a row of nothing but the lowest fp32
-// number would overflow as c x.
+// number would overflow as c x.  Where m is beyond 2^28 the reference is the largest logit x0 itself, d = c (x - x0): c x is then rounded to steps of 16 and
+// more, and fp32 logits one step apart would come out up to 32 off, or equal.
 //
 // The gradient by x_v is (g (1[v = token] - p_v) - h p_v (log p_v + H)) / T: a second look at the row, which L2 still holds.
 //
@@ -63,18 +64,21 @@ template <int T> struct KeyShift { static constexpr int value = T == T_BF16 ? 16
 
 // Running reference and sums of some logits.  What the loops need of the reference is kept ready: where the next move is due, the addend of c x.
 struct LogSum {
-  float m4 = neg_inf(), s = 0.f, q = 0.f;
+  float s = 0.f, q = 0.f;
   float due = neg_inf(), off = 0.f;                          // m4 + 2; -4 m4 (0 for none)
-  bool far = false;                                          // c x may overflow
-  __device__ __forceinline__ void set(float to4) {
-    m4 = to4;
-    due = to4 + 2.f;
-    off = to4 == neg_inf() ? 0.f : -4.f * to4;
-    far = fabsf(to4) > 67108864.f && to4 != neg_inf();     // up to there the rounding of m4 moves d by 16 at most, for all logits alike
+  bool far = false;                                          // the reference is a logit: off, m4 its product with c4, due just below that
+  __device__ __forceinline__ float m4(float c4) const { return far ? __fmul_rn(off, c4) : due == neg_inf() ? due : -0.25f * off; }     // a register less where the sums are taken
+  static __device__ __forceinline__ bool is_far(float to4) { return fabsf(to4) > 67108864.f && to4 != neg_inf(); }       // up to there the rounding of m4 moves d by 16 at most, for all logits alike
+  __device__ __forceinline__ void set(float to4, float x) {  // x: the logit that gave to4, or a far reference's off
+    far = is_far(to4);
+    due = far ? fmaf(fabsf(to4), -2.384185791015625e-7f, to4) : to4 + 2.f;
+    off = far ? (fabsf(to4) <= 3.4e38f ? x : to4) : to4 == neg_inf() ? 0.f : -4.f * to4;      // a product beyond the range counts as infinite
   }
-  __device__ __forceinline__ void move(float to4) {          // to a reference to4 >= m4
-    const float by = 4.f * (to4 - m4);
-    if (by < 250.f) {
+  __device__ __forceinline__ void move(float to4, float x, float c4) {          // to a reference to4 >= m4
+    const float c = 4.f * c4;
+    if (far && is_far(to4) && !(x > off)) return;            // its product rounded alike
+    const float by = !is_far(to4) ? (far ? -fmaf(off, c, -4.f * to4) : fmaf(4.f, to4, off)) : far ? (x - off) * c : fmaf(x, c, off);
+    if (by < 250.f && due != neg_inf()) {
       const float f = exp2_fast(-by);
       q = (q - by * s) * f;
       s *= f;
@@ -82,25 +86,22 @@ struct LogSum {
       s = s == s ? 0.f : s;                                  // a NaN stays
       q = s;
     }
-    set(to4);
+    set(to4, x);
   }
   __device__ __forceinline__ void reach(float most, float c4) {
     const float top4 = __fmul_rn(most, c4);
-    if (top4 > due) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4);
+    if (top4 > due) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4, most, c4);
   }
-  __device__ __forceinline__ float dist(float x, float c, float c4) const {
-    if (m4 == neg_inf()) return x;
-    return far ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, off);
-  }
+  __device__ __forceinline__ float dist(float x, float c) const { return far ? (x - off) * c : fmaf(x, c, off); }
   __device__ __forceinline__ void add(float d) {             // d >= LP_NONE or NaN
     const float e = exp2_fast(d);
     s += e;
     q = fmaf(e, d, q);
   }
   template <int N>
-  __device__ __forceinline__ void add_far(const float (&x)[N], float c4) {
+  __device__ __forceinline__ void add_far(const float (&x)[N], float c) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) add(max_nan(4.f * (__fmul_rn(x[e], c4) - m4), LP_NONE));     // equal logits differ by nothing
+    for (int e = 0; e < N; ++e) add(max_nan((x[e] - off) * c, LP_NONE));
   }
   template <int N>
   __device__ __forceinline__ float take(const float (&x)[N], float c, float c4) {
@@ -108,7 +109,7 @@ struct LogSum {
 #pragma unroll
     for (int e = 1; e < N; ++e) most = max_nan(most, x[e]);
     reach(most, c4);
-    if (far) add_far(x, c4);
+    if (far) add_far(x, c);
     else
 #pragma unroll
       for (int e = 0; e < N; ++e) add(max_nan(fmaf(x[e], c, off), LP_NONE));
@@ -126,7 +127,7 @@ struct LogSum {
       if (far) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = r.value(e);
-        add_far(x, c4);
+        add_far(x, c);
         return most;
       }
       Raw8<T> f;
@@ -144,11 +145,17 @@ struct LogSum {
   }
   // The sums of groups of G lanes, in each of them: first the largest reference, then one move, then two trees
   template <int G>
-  __device__ __forceinline__ void join_lanes() {
-    float to = m4;
+  __device__ __forceinline__ void join_lanes(float c4) {
+    const float mine = m4(c4);
+    float to = mine, x = off;
 #pragma unroll
     for (int k = G / 2; k > 0; k >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, k));
-    if (m4 != to) move(to);
+    if (__any_sync(0xFFFFFFFFu, is_far(to))) {               // several logits may have this product: the largest
+      x = mine == to ? off : neg_inf();
+#pragma unroll
+      for (int k = G / 2; k > 0; k >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, k));
+    }
+    if (mine != to || far) move(to, x, c4);
 #pragma unroll
     for (int k = G / 2; k > 0; k >>= 1) {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
@@ -160,14 +167,14 @@ struct LogSum {
 // What a row's sums say
 struct LogRow {
   LogSum t;
-  float l2;                                 // log2 s
+  float m4, l2;                             // l2: log2 s
   bool none;                                // nothing but -inf
-  __device__ __forceinline__ explicit LogRow(const LogSum& sum) : t(sum), l2(log2f(sum.s)), none(sum.s == 0.f) {}
-  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far ? (l2 == l2 ? t.m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, t.m4, l2) * LP_LN2; }
+  __device__ __forceinline__ LogRow(const LogSum& sum, float c4) : t(sum), m4(sum.m4(c4)), l2(log2f(sum.s)), none(sum.s == 0.f) {}
+  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far ? (l2 == l2 ? m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, m4, l2) * LP_LN2; }
   __device__ __forceinline__ float logp(float x, float c, float c4) const {
     if (none) return neg_inf();
-    if (!(fabsf(x) < 1e30f)) return (__fmul_rn(x, c4) - t.m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
-    const float lp = (t.dist(x, c, c4) - l2) * LP_LN2;
+    if (!t.far && !(fabsf(x) < 1e30f)) return (__fmul_rn(x, c4) - m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
+    const float lp = t.far ? ((x - t.off) * c4 - 0.25f * l2) * (4.f * LP_LN2) : (t.dist(x, c) - l2) * LP_LN2;
     return lp > 0.f ? 0.f : lp;                              // by rounding only
   }
   __device__ __forceinline__ float entropy() const {
@@ -180,11 +187,11 @@ struct LogRow {
 // took: log2 s joined to the addend of c x loses its digits beside a far reference (logits around 1e6: p off by 1.6 %, and a row's gradients then
 // do not sum to zero).
 struct LogGrad {
-  float c, c4, off, m4, a, b, g;            // a and b: the ones above with a dash
+  float c, off, a, b, g;                    // a and b: the ones above with a dash
   uint32_t low;                             // twice, in bf16: a logit whose d is LP_NONE or below, by the rounding's step at most
   bool far, none;
   __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow& r, float g_, float h) {
-    c = k.c; c4 = k.c4; off = r.t.off; m4 = r.t.m4; far = r.t.far; none = r.none;
+    c = k.c; off = r.t.off; far = r.t.far; none = r.none;
     const float by_lp = -h * LP_LN2 * k.inv_t, inv_s = 1.f / r.t.s;
     a = by_lp * inv_s;
     b = (-(g_ + h * r.entropy()) * k.inv_t - by_lp * r.l2) * inv_s;
@@ -194,7 +201,7 @@ struct LogGrad {
   }
   __device__ __forceinline__ float at(float x) const {
     if (none) return 0.f;
-    const float d = max_nan(far ? 4.f * (__fmul_rn(x, c4) - m4) : fmaf(x, c, off), LP_NONE);
+    const float d = max_nan(far ? (x - off) * c : fmaf(x, c, off), LP_NONE);
     return exp2_fast(d) * fmaf(a, d, b);
   }
   // bf16: logits are kept at `low` or above two at a time, so that no d is far below LP_NONE: with -inf, or a mask's lowest number, a d + b could be
@@ -246,8 +253,8 @@ __global__ void __launch_bounds__(128) logp_short_kernel(const __grid_constant__
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = live && i * G + lane < vocab ? Elem<T>::get(a.x, base + i * G + lane) : neg_inf();
   t.take(x, a.c, a.c4);
-  if (G > 1) t.join_lanes<G>();
-  const LogRow r(t);
+  if (G > 1) t.join_lanes<G>(a.c4);
+  const LogRow r(t, a.c4);
   const long long token = live ? token_of(a, row) : -1;
   if (live && lane == 0) write_row<T>(a, r, row, token);
   if (a.top) {
@@ -334,7 +341,7 @@ __device__ __forceinline__ void put8_past(void* p, long long i, const float (&v)
 
 template <int NT>
 struct LogpShared {
-  float m4[NT / 32], s[NT / 32], q[NT / 32];
+  float m4[NT / 32], s[NT / 32], q[NT / 32], off[NT / 32];
   float row[4];                                      // the block's own sums, for the others of the cluster
   unsigned long long list[LP_LIST], best[LP_MAX_TOP], pick[NT / 32];
   int share[NT], shares, listed;
@@ -476,27 +483,27 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     for (int k = 0; k < AHEAD - 1; ++k)
       if (g + k * NT < sl.groups) some(r[k]);
   }
-  t.join_lanes<32>();
-  if (lane == 0) { sh.m4[warp] = t.m4; sh.s[warp] = t.s; sh.q[warp] = t.q; }
+  t.join_lanes<32>(a.c4);
+  if (lane == 0) { sh.m4[warp] = t.m4(a.c4); sh.s[warp] = t.s; sh.q[warp] = t.q; sh.off[warp] = t.off; }
   __syncthreads();
   constexpr int WARPS = NT / 32;
   t = LogSum();                                                          // every warp joins the warps' sums: the same in all
-  if (lane < WARPS) { t.set(sh.m4[lane]); t.s = sh.s[lane]; t.q = sh.q[lane]; }
-  t.join_lanes<32>();
+  if (lane < WARPS) { t.set(sh.m4[lane], sh.off[lane]); t.s = sh.s[lane]; t.q = sh.q[lane]; }
+  t.join_lanes<32>(a.c4);
   if (a.top) {
     const bool any = tid < sl.groups || tid < sl.head || tid < sl.tail;
     top_of_slice<T, NT>(sh, sl, (uint32_t)first, a.top, any ? logit_key(most) : 0u);
   }
   if (slices > 1) {
-    if (tid == 0) { sh.row[0] = t.m4; sh.row[1] = t.s; sh.row[2] = t.q; }
+    if (tid == 0) { sh.row[0] = t.m4(a.c4); sh.row[1] = t.s; sh.row[2] = t.q; sh.row[3] = t.off; }
     __syncthreads();
     cluster_sync_all();
     t = LogSum();
     if (lane < slices) {
       const uint32_t from = cluster_addr(smem_addr(sh.row), (uint32_t)lane);
-      t.set(ld_cluster1(from)); t.s = ld_cluster1(from + 4); t.q = ld_cluster1(from + 8);
+      t.set(ld_cluster1(from), ld_cluster1(from + 12)); t.s = ld_cluster1(from + 4); t.q = ld_cluster1(from + 8);
     }
-    t.join_lanes<32>();
+    t.join_lanes<32>(a.c4);
     if (a.top && part == 0) {
       for (int i = tid; i < slices * a.top; i += NT)
         sh.list[i] = ld_cluster64(cluster_addr(smem_addr(sh.best + i % a.top), (uint32_t)(i / a.top)));
@@ -505,7 +512,7 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     cluster_sync_all();                                                  // the others' sums and lists have been read
     if (a.top && part == 0) rank_words<NT>(sh.list, slices * a.top, a.top, sh.best);
   }
-  const LogRow r(t);
+  const LogRow r(t, a.c4);
   const long long token = token_of(a, row);
   if (part == 0) {
     if (tid == 0) write_row<T>(a, r, row, token);

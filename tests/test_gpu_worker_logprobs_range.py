@@ -100,3 +100,59 @@ def test_rows_far_from_zero(B, dt, off, spread, T, vocab, rows):
     close(got.logp, lp_t, S + 2.0**-22 * np.abs(lp_t), "logp")
     close(got.entropy, H, 2 * S * (2 * np.log2(vocab) + 12), "entropy")
     close(got.lse, (X / T).max(1) + np.log(np.exp(X / T - (X / T).max(1, keepdims=True)).sum(1)), S + 2.0**-22 * np.abs(X / T).max(1) + 2.0**-22 * 40, "lse")
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 12), (4, 100), (4, 900), (4, 3001), (3, 20011), (300, 9001)])
+@pytest.mark.parametrize("middle,T", [(2e8, 1.0), (-1e9, 1.0), (1e8, 0.1), (-3e6, 0.01), (1.8606e8, 1.0), (-1.8606e8, 1.0), (7e12, 1000.0), (2e37, 1.0), (-2e38, 1.0)])
+@pytest.mark.parametrize("order", ["mixed", "rising", "falling"])
+def test_logits_a_few_steps_apart_beyond_2_to_the_28(B, rows, vocab, middle, T, order):
+    """fp32 logits around masks like -1e9: neighbours are many nats apart, and still told apart.  1.8606e8 is where references begin to be logits."""
+    gen = torch.Generator().manual_seed(vocab)
+    step = np.spacing(np.float32(abs(middle)))
+    k = torch.randint(-9, 10, (rows, vocab), generator=gen).double()
+    k = k if order == "mixed" else k.sort(1, descending=order == "falling")[0]
+    x = (middle + float(step) * k).float().cuda()
+    x[1, : vocab // 2] = float("-inf")
+    X, t = f64(x), torch.randint(vocab // 2, vocab, (rows,), generator=gen).cuda()
+    t[0] = x[0].argmax()
+    g, h = torch.randn(rows, generator=gen).cuda(), torch.randn(rows, generator=gen).cuda()
+    tok = t.cpu().numpy()
+    top = min(4, vocab)
+    got = B.log_probs(x, t, temperature=T, top=top, d_logp=g, d_entropy=h)
+    with np.errstate(invalid="ignore"):
+        lp, p, H = rows_of(X, T)
+        want, tol, _ = expect(X, tok, T, f64(g), f64(h))
+    low = (X / T - (X / T).max(1, keepdims=True)) - np.log(p.max(1, keepdims=True) ** -1)
+    S = (33 + vocab / 128) * 2.0**-24 + 2.0**-20 + 80 * 2.0**-24
+    close(got.dlogits, want, tol + 2.0**-22 * np.abs(want) + TINY[torch.float32], "dlogits")
+    lp_t = low[np.arange(rows), tok]
+    close(got.logp, lp_t, S + 2.0**-21 * np.abs(lp_t), "logp")
+    close(got.entropy, H, 2 * S * (2 * np.log2(vocab) + 12), "entropy")
+    close(got.lse, (X / T).max(1) - np.log(p.max(1)), S + 2.0**-21 * np.abs(X / T).max(1, where=np.isfinite(X), initial=0), "lse")
+    ids = np.argsort(-X, axis=1, kind="stable")[:, :top]
+    assert np.array_equal(got.top_ids.cpu().numpy(), ids)
+    at = np.take_along_axis(low, ids, 1)
+    close(got.top_logp, at, S + 2.0**-21 * np.abs(at), "top_logp")
+
+
+@pytest.mark.parametrize("vocab", [100, 900, 3001, 20011])
+def test_some_logits_beyond_2_to_the_28(B, vocab):
+    """A mask added in fp32 leaves numbers around -1e9 beside the ones that count, wherever they stand and whichever come first."""
+    gen = torch.Generator().manual_seed(vocab)
+    x = torch.randn(6, vocab, generator=gen)
+    x[0, ::2] -= 1e9
+    x[1, : vocab - 1] -= 1e9
+    x[2, 1:] -= 1e9
+    x[3] = x[3] * 100 - 1e9
+    x[4, vocab // 2:] += 1e9
+    x[5, vocab // 3] = 3e8
+    x = x.cuda()
+    t = x.argmax(1)
+    g, h = torch.randn(6, generator=gen).cuda(), torch.randn(6, generator=gen).cuda()
+    X, tok = f64(x), t.cpu().numpy()
+    got = B.log_probs(x, t, d_logp=g, d_entropy=h)
+    want, tol, p = expect(X, tok, 1.0, f64(g), f64(h))
+    close(got.dlogits, want, tol + 2.0**-22 * np.abs(want) + TINY[torch.float32], "dlogits")
+    S = (33 + vocab / 128) * 2.0**-24 + 2.0**-20 + 80 * 2.0**-24
+    close(got.logp, np.log(p.max(1)), S + 2.0**-21 * np.abs(np.log(p.max(1))), "logp")
+    close(got.entropy, rows_of(X, 1.0)[2], 2 * S * (2 * np.log2(vocab) + 12), "entropy")
