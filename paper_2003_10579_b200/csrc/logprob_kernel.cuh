@@ -72,7 +72,7 @@ struct LogSum {
   __device__ __forceinline__ void set(float to4, float x) {  // x: the logit that gave to4, or a far reference's off
     far = is_far(to4);
     due = far ? fmaf(fabsf(to4), -2.384185791015625e-7f, to4) : to4 + 2.f;
-    off = far ? (fabsf(to4) <= 3.4e38f ? x : to4) : to4 == neg_inf() ? 0.f : -4.f * to4;      // a product beyond the range counts as infinite
+    off = far ? (to4 - to4 == 0.f ? x : quiet_nan()) : to4 == neg_inf() ? 0.f : -4.f * to4;   // a product beyond the range counts as infinite: every distance is NaN
   }
   __device__ __forceinline__ void move(float to4, float x, float c4) {          // to a reference to4 >= m4
     const float c = 4.f * c4;

@@ -156,3 +156,20 @@ def test_some_logits_beyond_2_to_the_28(B, vocab):
     S = (33 + vocab / 128) * 2.0**-24 + 2.0**-20 + 80 * 2.0**-24
     close(got.logp, np.log(p.max(1)), S + 2.0**-21 * np.abs(np.log(p.max(1))), "logp")
     close(got.entropy, rows_of(X, 1.0)[2], 2 * S * (2 * np.log2(vocab) + 12), "entropy")
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [12, 100, 900, 3001, 20011])
+def test_logits_beyond_the_range_once_divided(B, dt, vocab):
+    """2e38 / 0.1 counts as infinite: the row is NaN; -2e38 / 0.1 as -inf: no probability, and a row of nothing else has no entropy and no gradient."""
+    x = torch.zeros(4, vocab, dtype=dt, device=DEV)
+    x[0, vocab // 2] = 2e38
+    x[1] = 2e38
+    x[2] = -2e38
+    x[3, 1:] = -2e38
+    t = torch.tensor([vocab // 2, 0, 1, 0], device=DEV)
+    one = torch.ones(4, device=DEV)
+    got = B.log_probs(x, t, temperature=0.1, d_logp=one, d_entropy=one)
+    assert all(torch.isnan(r[:2]).all() for r in (got.logp, got.entropy, got.lse, got.dlogits))
+    assert got.logp[2] == got.lse[2] == float("-inf") and got.entropy[2] == 0 and got.logp[3] == 0 and got.entropy[3] == 0 and got.lse[3] == 0
+    assert (got.dlogits[2:] == 0).all()
