@@ -5,8 +5,8 @@
 // one pass over the row with running m, s, q a thread.  m being whole, moving it scales s and q exactly, and a thread moves it only
 // when a logit is over 2^8 times (in 2^d) beyond it, so the rescaling's exponential is rare.  s and q are fp32: a thread adds at most
 // vocab / threads terms, then the threads meet in a tree.  m is kept in quarters, m4 = m / 4: a row of nothing but the lowest fp32
-// number would overflow as c x.  Where m is beyond 2^28 the reference is the largest logit x0 itself, d = c (x - x0): c x is then rounded to steps of 16 and
-// more, and fp32 logits one step apart would come out up to 32 off, or equal.
+// number would overflow as c x.  Where m is beyond 2^28 c x is rounded to steps of 16 and more: fp32 logits one step apart would come out up to 32 off, or equal, so
+// that there the reference is the largest logit x0 itself, d = c (x - x0).  16-bit logits of that size are 2^17 and more apart where they differ.
 //
 // The gradient by x_v is (g (1[v = token] - p_v) - h p_v (log p_v + H)) / T: a second look at the row, which L2 still holds.
 //
@@ -62,23 +62,28 @@ __device__ __forceinline__ float logit_of_key(uint32_t k) {
 // bits of a key that are the same for all values of one sign of a type
 template <int T> struct KeyShift { static constexpr int value = T == T_BF16 ? 16 : T == T_F16 ? 13 : 0; };
 
-// Running reference and sums of some logits.  What the loops need of the reference is kept ready: where the next move is due, the addend of c x.
+// Running reference and sums of some logits of type T.  What the loops need of the reference is kept ready: where the next move is due, the addend of c x.
+template <int T>
 struct LogSum {
-  float s = 0.f, q = 0.f;
+  static constexpr bool FINE = T == T_F32;                   // a far reference is a logit (16-bit logits take their products' differences: 2 % faster)
+  float m4 = neg_inf(), s = 0.f, q = 0.f;
   float due = neg_inf(), off = 0.f;                          // m4 + 2; -4 m4 (0 for none)
-  bool far = false;                                          // the reference is a logit: off, m4 its product with c4, due just below that
-  __device__ __forceinline__ float m4(float c4) const { return far ? __fmul_rn(off, c4) : due == neg_inf() ? due : -0.25f * off; }     // a register less where the sums are taken
+  bool far = false;                                          // c x may overflow; FINE: off is the reference, m4 its product with c4, due just below that
   static __device__ __forceinline__ bool is_far(float to4) { return fabsf(to4) > 67108864.f && to4 != neg_inf(); }       // up to there the rounding of m4 moves d by 16 at most, for all logits alike
-  __device__ __forceinline__ void set(float to4, float x) {  // x: the logit that gave to4, or a far reference's off
+  __device__ __forceinline__ void set(float to4, float x) {  // FINE: x is the logit that gave to4, or a far reference's off
+    m4 = to4;
     far = is_far(to4);
-    due = far ? fmaf(fabsf(to4), -2.384185791015625e-7f, to4) : to4 + 2.f;
-    off = far ? (to4 - to4 == 0.f ? x : quiet_nan()) : to4 == neg_inf() ? 0.f : -4.f * to4;   // a product beyond the range counts as infinite: every distance is NaN
+    due = FINE && far ? fmaf(fabsf(to4), -2.384185791015625e-7f, to4) : to4 + 2.f;
+    off = FINE && far ? (to4 - to4 == 0.f ? x : quiet_nan()) : to4 == neg_inf() ? 0.f : -4.f * to4;   // a product beyond the range counts as infinite: every distance is NaN
   }
   __device__ __forceinline__ void move(float to4, float x, float c4) {          // to a reference to4 >= m4
-    const float c = 4.f * c4;
-    if (far && is_far(to4) && !(x > off)) return;            // its product rounded alike
-    const float by = !is_far(to4) ? (far ? -fmaf(off, c, -4.f * to4) : fmaf(4.f, to4, off)) : far ? (x - off) * c : fmaf(x, c, off);
-    if (by < 250.f && due != neg_inf()) {
+    float by = 4.f * (to4 - m4);
+    if (FINE && (far || is_far(to4))) {
+      const float c = 4.f * c4;
+      if (far && is_far(to4) && !(x > off)) return;          // its product rounded alike
+      by = !is_far(to4) ? -fmaf(off, c, -4.f * to4) : far ? (x - off) * c : m4 == neg_inf() ? 250.f : fmaf(x, c, off);
+    }
+    if (by < 250.f) {
       const float f = exp2_fast(-by);
       q = (q - by * s) * f;
       s *= f;
@@ -92,16 +97,17 @@ struct LogSum {
     const float top4 = __fmul_rn(most, c4);
     if (top4 > due) move(fabsf(top4) < 1048576.f ? rintf(4.f * top4) * 0.25f : top4, most, c4);
   }
-  __device__ __forceinline__ float dist(float x, float c) const { return far ? (x - off) * c : fmaf(x, c, off); }
+  __device__ __forceinline__ float dist4(float x, float c4) const { return FINE ? (x - off) * c4 : __fmul_rn(x, c4) - m4; }      // a quarter of it, of a far reference
+  __device__ __forceinline__ float dist(float x, float c, float c4) const { return far ? 4.f * dist4(x, c4) : fmaf(x, c, off); }
   __device__ __forceinline__ void add(float d) {             // d >= LP_NONE or NaN
     const float e = exp2_fast(d);
     s += e;
     q = fmaf(e, d, q);
   }
   template <int N>
-  __device__ __forceinline__ void add_far(const float (&x)[N], float c) {
+  __device__ __forceinline__ void add_far(const float (&x)[N], float c4) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) add(max_nan((x[e] - off) * c, LP_NONE));
+    for (int e = 0; e < N; ++e) add(max_nan(4.f * dist4(x[e], c4), LP_NONE));
   }
   template <int N>
   __device__ __forceinline__ float take(const float (&x)[N], float c, float c4) {
@@ -109,7 +115,7 @@ struct LogSum {
 #pragma unroll
     for (int e = 1; e < N; ++e) most = max_nan(most, x[e]);
     reach(most, c4);
-    if (far) add_far(x, c);
+    if (far) add_far(x, c4);
     else
 #pragma unroll
       for (int e = 0; e < N; ++e) add(max_nan(fmaf(x[e], c, off), LP_NONE));
@@ -117,7 +123,6 @@ struct LogSum {
   }
   // Eight logits as they are stored.  bf16: the largest and the way out of -inf two at a time - a logit under -1e30 stands for any such, and its
   // probability is zero without the product 0 (-inf) - unless they all are that small.
-  template <int T>
   __device__ __forceinline__ float take8(const Raw8<T>& r, float c, float c4) {
     if constexpr (T == T_BF16) {
       const uint32_t m = max_nan_bf16x2(max_nan_bf16x2(r.w[0], r.w[1]), max_nan_bf16x2(r.w[2], r.w[3]));
@@ -127,7 +132,7 @@ struct LogSum {
       if (far) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = r.value(e);
-        add_far(x, c);
+        add_far(x, c4);
         return most;
       }
       Raw8<T> f;
@@ -146,16 +151,15 @@ struct LogSum {
   // The sums of groups of G lanes, in each of them: first the largest reference, then one move, then two trees
   template <int G>
   __device__ __forceinline__ void join_lanes(float c4) {
-    const float mine = m4(c4);
-    float to = mine, x = off;
+    float to = m4, x = off;
 #pragma unroll
     for (int k = G / 2; k > 0; k >>= 1) to = fmaxf(to, __shfl_xor_sync(0xFFFFFFFFu, to, k));
-    if (__any_sync(0xFFFFFFFFu, is_far(to))) {               // several logits may have this product: the largest
-      x = mine == to ? off : neg_inf();
+    if (FINE && __any_sync(0xFFFFFFFFu, is_far(to))) {       // several logits may have this product: the largest
+      x = m4 == to ? off : neg_inf();
 #pragma unroll
       for (int k = G / 2; k > 0; k >>= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, k));
     }
-    if (mine != to || far) move(to, x, c4);
+    if (m4 != to || (FINE && far)) move(to, x, c4);
 #pragma unroll
     for (int k = G / 2; k > 0; k >>= 1) {
       s += __shfl_xor_sync(0xFFFFFFFFu, s, k);
@@ -165,16 +169,17 @@ struct LogSum {
 };
 
 // What a row's sums say
+template <int T>
 struct LogRow {
-  LogSum t;
-  float m4, l2;                             // l2: log2 s
+  LogSum<T> t;
+  float l2;                                 // log2 s
   bool none;                                // nothing but -inf
-  __device__ __forceinline__ LogRow(const LogSum& sum, float c4) : t(sum), m4(sum.m4(c4)), l2(log2f(sum.s)), none(sum.s == 0.f) {}
-  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far ? (l2 == l2 ? m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, m4, l2) * LP_LN2; }
+  __device__ __forceinline__ explicit LogRow(const LogSum<T>& sum) : t(sum), l2(log2f(sum.s)), none(sum.s == 0.f) {}
+  __device__ __forceinline__ float lse() const { return none ? neg_inf() : t.far ? (l2 == l2 ? t.m4 * (4.f * LP_LN2) : l2) : fmaf(4.f, t.m4, l2) * LP_LN2; }
   __device__ __forceinline__ float logp(float x, float c, float c4) const {
     if (none) return neg_inf();
-    if (!t.far && !(fabsf(x) < 1e30f)) return (__fmul_rn(x, c4) - m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
-    const float lp = t.far ? ((x - t.off) * c4 - 0.25f * l2) * (4.f * LP_LN2) : (t.dist(x, c) - l2) * LP_LN2;
+    const float lp = t.far ? (t.dist4(x, c4) - 0.25f * l2) * (4.f * LP_LN2) :
+                     fabsf(x) < 1e30f ? (fmaf(x, c, t.off) - l2) * LP_LN2 : (__fmul_rn(x, c4) - t.m4 - 0.25f * l2) * (4.f * LP_LN2);      // c x may overflow
     return lp > 0.f ? 0.f : lp;                              // by rounding only
   }
   __device__ __forceinline__ float entropy() const {
@@ -186,36 +191,37 @@ struct LogRow {
 // The gradient by a logit, p (a lp + b) with lp = log2 p = d - log2 s, as 2^d (a' d + b'), a' = a / s, b' = (b - a log2 s) / s; at the token plus g / T.  d is what the sums
 // took: log2 s joined to the addend of c x loses its digits beside a far reference (logits around 1e6: p off by 1.6 %, and a row's gradients then
 // do not sum to zero).
+template <int T>
 struct LogGrad {
-  float c, off, a, b, g;                    // a and b: the ones above with a dash
+  LogSum<T> t;
+  float c, c4, a, b, g;                     // a and b: the ones above with a dash
   uint32_t low;                             // twice, in bf16: a logit whose d is LP_NONE or below, by the rounding's step at most
-  bool far, none;
-  __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow& r, float g_, float h) {
-    c = k.c; off = r.t.off; far = r.t.far; none = r.none;
+  bool none;
+  __device__ __forceinline__ LogGrad(const LogpArgs& k, const LogRow<T>& r, float g_, float h) {
+    t = r.t; c = k.c; c4 = k.c4; none = r.none;
     const float by_lp = -h * LP_LN2 * k.inv_t, inv_s = 1.f / r.t.s;
     a = by_lp * inv_s;
     b = (-(g_ + h * r.entropy()) * k.inv_t - by_lp * r.l2) * inv_s;
     g = none ? 0.f : g_ * k.inv_t;
-    const uint32_t w = __float_as_uint((LP_NONE - off) / c);
+    const uint32_t w = __float_as_uint((LP_NONE - t.off) / c);
     low = ((int32_t)w < 0 ? (w + 0xFFFFu) >> 16 : w >> 16) * 0x10001u;          // rounded down
   }
   __device__ __forceinline__ float at(float x) const {
     if (none) return 0.f;
-    const float d = max_nan(far ? (x - off) * c : fmaf(x, c, off), LP_NONE);
+    const float d = max_nan(t.dist(x, c, c4), LP_NONE);
     return exp2_fast(d) * fmaf(a, d, b);
   }
   // bf16: logits are kept at `low` or above two at a time, so that no d is far below LP_NONE: with -inf, or a mask's lowest number, a d + b could be
   // infinite beside the probability zero (-1e30 as the least: NaN from d_entropy = 342 on at T = 0.001)
-  template <int T>
   __device__ __forceinline__ void at8(const Raw8<T>& r, float (&x)[8]) const {
     if constexpr (T == T_BF16) {
-      if (!far && !none) {
+      if (!t.far && !none) {
         Raw8<T> f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) f.w[k] = max_nan_bf16x2(r.w[k], low);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float d = fmaf(f.value(e), c, off);
+          const float d = fmaf(f.value(e), c, t.off);
           x[e] = exp2_fast(d) * fmaf(a, d, b);
         }
         return;
@@ -235,7 +241,7 @@ __device__ __forceinline__ float token_weight(const LogpArgs& a, long long row, 
   return token < a.vocab ? a.d_logp[row] : quiet_nan();
 }
 template <int T>
-__device__ __forceinline__ void write_row(const LogpArgs& a, const LogRow& r, long long row, long long token) {
+__device__ __forceinline__ void write_row(const LogpArgs& a, const LogRow<T>& r, long long row, long long token) {
   if (a.lse) a.lse[row] = r.lse();
   if (a.entropy) a.entropy[row] = r.entropy();
   if (a.logp) a.logp[row] = token < 0 ? 0.f : token >= a.vocab ? quiet_nan() : r.logp(Elem<T>::get(a.x, row * a.ld + token), a.c, a.c4);
@@ -249,12 +255,12 @@ __global__ void __launch_bounds__(128) logp_short_kernel(const __grid_constant__
   const bool live = row < a.rows;
   const long long base = live ? row * a.ld : 0;
   float x[E];
-  LogSum t;
+  LogSum<T> t;
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = live && i * G + lane < vocab ? Elem<T>::get(a.x, base + i * G + lane) : neg_inf();
   t.take(x, a.c, a.c4);
-  if (G > 1) t.join_lanes<G>(a.c4);
-  const LogRow r(t, a.c4);
+  if (G > 1) t.template join_lanes<G>(a.c4);
+  const LogRow<T> r(t);
   const long long token = live ? token_of(a, row) : -1;
   if (live && lane == 0) write_row<T>(a, r, row, token);
   if (a.top) {
@@ -285,7 +291,7 @@ __global__ void __launch_bounds__(128) logp_short_kernel(const __grid_constant__
   }
   __syncwarp();              // the token's logit has been read: the gradient may go over the logits
   if (a.out && live) {
-    const LogGrad d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
+    const LogGrad<T> d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       const int v = i * G + lane;
@@ -456,9 +462,9 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
   const long long first = (long long)part * slice_len;
   const Slice<T> sl(a.x, row * a.ld + first, (int)max(0ll, min((long long)slice_len, a.vocab - first)));
 
-  LogSum t;
+  LogSum<T> t;
   float most = neg_inf();                                              // of the thread's share
-  auto some = [&](const Raw8<T>& r) { most = max_nan(most, t.template take8<T>(r, a.c, a.c4)); };
+  auto some = [&](const Raw8<T>& r) { most = max_nan(most, t.take8(r, a.c, a.c4)); };
   auto single = [&](float v) {
     const float x[1] = {v};
     most = max_nan(most, t.take(x, a.c, a.c4));
@@ -483,27 +489,27 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     for (int k = 0; k < AHEAD - 1; ++k)
       if (g + k * NT < sl.groups) some(r[k]);
   }
-  t.join_lanes<32>(a.c4);
-  if (lane == 0) { sh.m4[warp] = t.m4(a.c4); sh.s[warp] = t.s; sh.q[warp] = t.q; sh.off[warp] = t.off; }
+  t.template join_lanes<32>(a.c4);
+  if (lane == 0) { sh.m4[warp] = t.m4; sh.s[warp] = t.s; sh.q[warp] = t.q; sh.off[warp] = t.off; }
   __syncthreads();
   constexpr int WARPS = NT / 32;
-  t = LogSum();                                                          // every warp joins the warps' sums: the same in all
+  t = LogSum<T>();                                                          // every warp joins the warps' sums: the same in all
   if (lane < WARPS) { t.set(sh.m4[lane], sh.off[lane]); t.s = sh.s[lane]; t.q = sh.q[lane]; }
-  t.join_lanes<32>(a.c4);
+  t.template join_lanes<32>(a.c4);
   if (a.top) {
     const bool any = tid < sl.groups || tid < sl.head || tid < sl.tail;
     top_of_slice<T, NT>(sh, sl, (uint32_t)first, a.top, any ? logit_key(most) : 0u);
   }
   if (slices > 1) {
-    if (tid == 0) { sh.row[0] = t.m4(a.c4); sh.row[1] = t.s; sh.row[2] = t.q; sh.row[3] = t.off; }
+    if (tid == 0) { sh.row[0] = t.m4; sh.row[1] = t.s; sh.row[2] = t.q; sh.row[3] = t.off; }
     __syncthreads();
     cluster_sync_all();
-    t = LogSum();
+    t = LogSum<T>();
     if (lane < slices) {
       const uint32_t from = cluster_addr(smem_addr(sh.row), (uint32_t)lane);
       t.set(ld_cluster1(from), ld_cluster1(from + 12)); t.s = ld_cluster1(from + 4); t.q = ld_cluster1(from + 8);
     }
-    t.join_lanes<32>(a.c4);
+    t.template join_lanes<32>(a.c4);
     if (a.top && part == 0) {
       for (int i = tid; i < slices * a.top; i += NT)
         sh.list[i] = ld_cluster64(cluster_addr(smem_addr(sh.best + i % a.top), (uint32_t)(i / a.top)));
@@ -512,7 +518,7 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     cluster_sync_all();                                                  // the others' sums and lists have been read
     if (a.top && part == 0) rank_words<NT>(sh.list, slices * a.top, a.top, sh.best);
   }
-  const LogRow r(t, a.c4);
+  const LogRow<T> r(t);
   const long long token = token_of(a, row);
   if (part == 0) {
     if (tid == 0) write_row<T>(a, r, row, token);
@@ -527,7 +533,7 @@ __global__ void __launch_bounds__(NT, LP_THREADS / NT) logp_row_kernel(const __g
     // logits, nobody writes before that.
     if (slices > 1) cluster_sync_all();
     else __syncthreads();
-    const LogGrad d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
+    const LogGrad<T> d(a, r, token_weight(a, row, token), a.d_entropy ? a.d_entropy[row] : 0.f);
     const int tok = token >= first && token < first + sl.n ? (int)(token - first) : -1;
     char* out = static_cast<char*>(a.out) + (row * a.ldo + first) * Elem<T>::bytes;
     const bool wide = ((reinterpret_cast<uintptr_t>(out) + sl.head * Elem<T>::bytes) & 15) == 0;
