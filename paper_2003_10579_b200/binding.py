@@ -977,6 +977,18 @@ def _apart(written, others, what):
                 raise ValueError("%s overlaps a tensor that is still to be read, or another result" % what)
 
 
+def _results_apart(need, dy, x, w, residual, grad, dx, dw, db):
+    """Refuses results of linear_backward that lie over what is still to be read: db, dx, dw are written in this order.  A Checkpoint's buffers count as the tensor that it
+    stands for; dx takes them too where the activation's slope is in it (grad)."""
+    kept = isinstance(x, Checkpoint)
+    values = [x.codes, x.scales] if kept else [x]
+    for_dw = values if "w" in need else []
+    left = ([dy] if "x" in need or "w" in need else []) + ([w, residual] if "x" in need else []) + (for_dw or (values if grad and "x" in need else []))
+    _apart(db if "b" in need else None, left, "db")
+    _apart(dx if "x" in need else None, for_dw + ([db] if "b" in need else []), "dx")
+    _apart(dw if "w" in need else None, [t for n, t in (("x", dx), ("b", db)) if n in need], "dw")
+
+
 def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=torch.float32, out=None, stream=None):
     """(dx, dw, db) of linear(x, w, bias) from dy [tokens, out], w [out, in] and x: the tensor [tokens, in] itself, or a Checkpoint.  With a
     Checkpoint v the layer's input was x_act(v) and is taken as x_act of the kept values, rounded to dy's type; dx is then the gradient by v,
@@ -1003,12 +1015,8 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     if stream is not None:
         _given(stream, device, *(t for t in (dy, x, w, residual) if t is not None))
     dx, dw, db = out or (None, None, None)
-    if out:                                  # what is written first must leave what is read, or stays, alone: db, dx, dw in this order
-        left = ([dy] if "x" in need or "w" in need else []) + ([w, residual] if "x" in need else []) + ([] if kept or "w" not in need else [x])
-        _apart(db if "b" in need else None, left, "db")
-        _apart(dx if "x" in need else None, [] if kept or "w" not in need else [x], "dx")
-        _apart(dw if "w" in need else None, [t for n, t in (("x", dx), ("b", db)) if n in need], "dw")
-        _apart(dx if "x" in need else None, [db] if "b" in need else [], "dx")
+    if out:
+        _results_apart(need, dy, x, w, residual, kept and code != 0, dx, dw, db)
     if "b" in need:
         if a_t:
             raise ValueError("db needs dy with neighbouring elements along its last dimension")
