@@ -190,6 +190,14 @@ class Simulation:
         _check(lib.sim_create(C.byref(prob), P, K, VARIANTS[variant], SimDelay(DELAYS[delay_kind], mu, shift),
                               eta, m, seed, n_replicas, replica_base, _stream_ptr(stream), C.byref(self._h)))
 
+    def _new(self, shape, dtype):
+        """Room for a result.  The handle's stream waits for the current one, which may still be reading that memory as a tensor that was let go."""
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        current, own = torch.cuda.current_stream(self.device), self.stream if self.stream is not None else torch.cuda.default_stream(self.device)
+        if own != current:
+            own.wait_stream(current)
+        return t
+
     def set_params(self, w0):
         assert w0.is_cuda and w0.dtype == torch.float32 and w0.numel() == self.n_params
         _check(lib.sim_set_params(self._h, _ptr(w0)), self._h)
@@ -225,26 +233,26 @@ class Simulation:
 
     def trace(self, to_numpy=True):
         J, Km = self.trace_size()
-        R, dev = self.R, self.device
-        out = {"t": torch.empty((R, J), dtype=torch.float64, device=dev),
-               "loss": torch.empty((R, J), dtype=torch.float32, device=dev),
-               "dist2": torch.empty((R, J), dtype=torch.float32, device=dev),
-               "K": torch.empty((R, J), dtype=_U16, device=dev),
-               "worker": torch.empty((R, J, Km), dtype=_U16, device=dev),
-               "stale": torch.empty((R, J, Km), dtype=_U32, device=dev),
-               "seq": torch.empty((R, J, Km), dtype=_U32, device=dev)}
+        R = self.R
+        out = {"t": self._new((R, J), torch.float64),
+               "loss": self._new((R, J), torch.float32),
+               "dist2": self._new((R, J), torch.float32),
+               "K": self._new((R, J), _U16),
+               "worker": self._new((R, J, Km), _U16),
+               "stale": self._new((R, J, Km), _U32),
+               "seq": self._new((R, J, Km), _U32)}
         _check(lib.sim_get_trace(self._h, *[_ptr(out[k]) for k in ("t", "loss", "dist2", "K", "worker", "stale", "seq")]),
                self._h)
         return {k: v.cpu().numpy() for k, v in out.items()} if to_numpy else out
 
     def params(self, to_numpy=True):
-        w = torch.empty((self.R, self.n_params), dtype=torch.float32, device=self.device)
+        w = self._new((self.R, self.n_params), torch.float32)
         _check(lib.sim_get_params(self._h, _ptr(w)), self._h)
         return w.cpu().numpy() if to_numpy else w
 
     def eval_loss(self, to_numpy=True, mxfp4=False):
         """Full-data risk F(w_j) of every replica's current parameters; mxfp4: with data and parameters in 4 bits."""
-        out = torch.empty((self.R,), dtype=torch.float32, device=self.device)
+        out = self._new((self.R,), torch.float32)
         _check((lib.sim_eval_loss_mxfp4 if mxfp4 else lib.sim_eval_loss)(self._h, _ptr(out)), self._h)
         if self.stream is not None:
             self.stream.synchronize()
@@ -257,10 +265,10 @@ class Simulation:
         logp (of the labels) and entropy [rows], and for top > 0 top_ids and top_logp [rows, top]."""
         rows = (self._keep[0].shape[0] if self._keep else 0) - first if rows is None else rows
         n = max(rows, 0)
-        out = {"logp": torch.empty((n,), dtype=torch.float32, device=self.device), "entropy": torch.empty((n,), dtype=torch.float32, device=self.device)}
+        out = {"logp": self._new((n,), torch.float32), "entropy": self._new((n,), torch.float32)}
         if top > 0:
-            out["top_ids"] = torch.empty((n, top), dtype=torch.int32, device=self.device)
-            out["top_logp"] = torch.empty((n, top), dtype=torch.float32, device=self.device)
+            out["top_ids"] = self._new((n, top), torch.int32)
+            out["top_logp"] = self._new((n, top), torch.float32)
         _check(lib.sim_eval_log_probs(self._h, replica, first, rows, top, *[_ptr(out.get(k)) for k in ("logp", "entropy", "top_ids", "top_logp")]), self._h)
         if self.stream is not None:
             self.stream.synchronize()
@@ -271,8 +279,8 @@ class Simulation:
     def error_curve(self, grid):
         """Mean minibatch loss over replicas against simulated wall clock at the times in `grid`."""
         g = torch.as_tensor(np.asarray(grid, np.float64)).to(self.device)
-        mean = torch.empty((g.numel(),), dtype=torch.float32, device=self.device)
-        cnt = torch.empty((g.numel(),), dtype=torch.int32, device=self.device)
+        mean = self._new((g.numel(),), torch.float32)
+        cnt = self._new((g.numel(),), torch.int32)
         _check(lib.sim_error_curve(self._h, _ptr(g), g.numel(), _ptr(mean), _ptr(cnt)), self._h)
         return mean.cpu().numpy(), cnt.cpu().numpy()
 
@@ -284,16 +292,16 @@ class Simulation:
         """(risk [R, E], t [R, E]): entry 0 is F(w_0) at time 0, entry i the risk after i * every updates."""
         E = C.c_int64()
         _check(lib.sim_risk_trace_size(self._h, C.byref(E)), self._h)
-        risk = torch.empty((self.R, E.value), dtype=torch.float32, device=self.device)
-        t = torch.empty((self.R, E.value), dtype=torch.float64, device=self.device)
+        risk = self._new((self.R, E.value), torch.float32)
+        t = self._new((self.R, E.value), torch.float64)
         _check(lib.sim_get_risk_trace(self._h, _ptr(risk), _ptr(t)), self._h)
         return (risk.cpu().numpy(), t.cpu().numpy()) if to_numpy else (risk, t)
 
     def risk_curve(self, grid, f_star=0.0):
         """Mean over replicas of F(w) - f_star against simulated wall clock at the times in `grid`."""
         g = torch.as_tensor(np.asarray(grid, np.float64)).to(self.device)
-        mean = torch.empty((g.numel(),), dtype=torch.float32, device=self.device)
-        cnt = torch.empty((g.numel(),), dtype=torch.int32, device=self.device)
+        mean = self._new((g.numel(),), torch.float32)
+        cnt = self._new((g.numel(),), torch.int32)
         _check(lib.sim_risk_curve(self._h, _ptr(g), g.numel(), f_star, _ptr(mean), _ptr(cnt)), self._h)
         return mean.cpu().numpy(), cnt.cpu().numpy()
 
@@ -317,8 +325,7 @@ def risk_envelope(sims, grid, f_star=0.0):
     """Lower envelope over several simulations' risk curves on a common grid: (env [G], best [G])."""
     dev = sims[0].device
     g = torch.as_tensor(np.asarray(grid, np.float64)).to(dev)
-    env = torch.empty((g.numel(),), dtype=torch.float32, device=dev)
-    best = torch.empty((g.numel(),), dtype=torch.int32, device=dev)
+    env, best = sims[0]._new((g.numel(),), torch.float32), sims[0]._new((g.numel(),), torch.int32)
     hs = (C.c_void_p * len(sims))(*[s._h for s in sims])
     st = lib.sim_risk_envelope(hs, len(sims), _ptr(g), g.numel(), f_star, _ptr(env), _ptr(best))
     _check(st)

@@ -158,3 +158,26 @@ def test_a_workers_step_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_results_on_the_handles_stream_wait_for_the_current_one():
+    """A handle with a stream of its own writes its results into new memory, which the current stream may still be reading as another tensor that was let go."""
+    from paper_2003_10579_b200 import binding as B
+    n, d, C = 4096, 64, 10
+    data = inputs.make_mixture(n, d, C, 0.3, 33)
+    st = torch.cuda.Stream()
+    sim = B.Simulation(to_device(data), P=4, K=2, variant="ksync", delay_kind="exp", mu=1.0, eta=0.02, m=8, seed=1, n_replicas=3, stream=st)
+    sim.run(2)
+    want = sim.log_probs()
+    for call in (sim.log_probs, sim.eval_loss, sim.params, sim.trace):
+        old = [torch.full((n,), 7.0, device="cuda") for _ in range(4)] + [torch.full((3, sim.n_params), 7.0, device="cuda"), torch.full((3,), 7.0, device="cuda")]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)                    # some 10 ms
+        kept = [t.clone() for t in old]
+        del old
+        call()
+        torch.cuda.synchronize()
+        assert all((t == 7.0).all() for t in kept), call
+    got = sim.log_probs()
+    assert all((got[k] == want[k]).all() for k in want)
+    sim.close()
