@@ -152,3 +152,18 @@ def test_graph(B):
     torch.cuda.synchronize()
     for _, out in graphs:
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+@pytest.mark.parametrize("cols", [96, 70])
+def test_a_nan_block_is_not_read_without_an_activation(B, cols):
+    """x_act "none": dx is dy w, whatever was kept; dw is NaN in the lost columns alone."""
+    x = matrix(40, cols, torch.bfloat16, 8)
+    x[3, 40] = float("inf")
+    q, w = B.checkpoint(x), matrix(24, cols, torch.bfloat16, 10)
+    for rows in (40, 4):
+        part, dy = B.Checkpoint(q.codes, q.scales, rows, cols), matrix(40, 24, torch.bfloat16, 11)[:rows]
+        dx, dw, _ = B.linear_backward(dy, part, w)
+        assert not torch.isnan(dx).any() and torch.equal(dx, B.linear(dy, w.t()))
+        lost = torch.zeros(24, cols, dtype=torch.bool, device=DEV)
+        lost[:, 32:64] = True
+        assert torch.equal(torch.isnan(dw), lost)
