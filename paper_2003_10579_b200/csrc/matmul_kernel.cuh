@@ -37,7 +37,7 @@ struct MmArgs {
   const void* res;
   void* c;
   long long ldr, ldc;
-  int vec_c, vec_r, vec_b;    // rows on 16-byte boundaries (vec_c 2: on 32-byte ones)
+  int vec_c, vec_r;           // rows on 16-byte boundaries (vec_c 2: on 32-byte ones)
 };
 
 // ---- the tail -----------------------------------------------------------------------------------------------------------------------

@@ -416,7 +416,6 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
   g.z_codes = p->z_codes; g.z_scales = p->z_scales; g.res = p->residual; g.ldr = p->ldr; g.c = p->c; g.ldc = p->ldc;
   g.vec_c = rows_aligned(p->c, M, p->ldc, p->c_type, 32) ? 2 : rows_aligned(p->c, M, p->ldc, p->c_type, 16) ? 1 : 0;
   g.vec_r = p->residual && rows_aligned(p->residual, M, p->ldr, p->c_type, 16);
-  g.vec_b = p->bias && aligned(p->bias, 16);
   CUtensorMap ma{}, mb{};
   if (K > 0 && (!make_map(&ma, a.p, p->type, a.rows, a.cols, a.ld, a.t ? 64 : 128) ||
                 !make_map(&mb, b.p, p->type, b.rows, b.cols, b.ld, b.t ? 64 : q.pair ? 128 : (uint32_t)q.bn)))
