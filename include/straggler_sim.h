@@ -523,9 +523,9 @@ sim_status sim_matmul(const sim_product* p, void* workspace, int64_t workspace_b
  *   d_logits[r][v] = (d_logp[r] ([v = token] - p[v]) - d_entropy[r] p[v] (log p[v] + entropy[r])) / temperature: the gradient of a loss whose
  *                    derivatives by logp and entropy are d_logp and d_entropy (either may be NULL: zero)
  * Any result may be NULL; a call for d_logits alone is the backward pass.  tokens: 4- or 8-byte integers; a negative one is no token (logp 0,
- * no gradient by it), one of at least vocab makes logp and the row's gradient NaN.  A logit of -inf has probability 0; a row
- * of nothing else has lse and every log probability -inf, entropy 0 and gradient 0.  A row with a NaN or +inf is NaN.  A logit over 2^126 temperature
- * counts as infinite.  d_logits may be logits itself with the same rows.  vocab in [1, 2^30], rows up to 2^27, top up to 32, temperature in [0.001, 1000].
+ * no gradient by it), one of at least vocab makes logp and, beside d_logp, the row's gradient NaN.  A logit of -inf has probability 0; a row
+ * of nothing else has lse and every log probability -inf, entropy 0 and gradient 0.  A row with a NaN or +inf is NaN.  A logit beyond 2^129 temperature
+ * counts as infinite.  What all logits of a row have in common takes no digits from anything but lse.  d_logits may be logits itself with the same rows.  vocab in [1, 2^30], rows up to 2^27, top up to 32, temperature in [0.001, 1000].
  * Sums are fp32, in a fixed order: the same bits every time.
  */
 sim_status sim_log_probs(const void* logits, sim_dtype type, int64_t rows, int64_t vocab, int64_t ld, const void* tokens, int32_t token_bytes, float temperature, int32_t top,

@@ -715,6 +715,8 @@ def mx_matmul(a, b, dtype=torch.bfloat16, *, out=None, stream=None):
 
 
 # ---- operators of a worker for models of language-model size --------------------------------------------------------------
+# Results stand outside torch's graph, whether or not an operand requires a gradient: the backward passes are calls of their own (linear_backward, act_backward,
+# log_probs_backward).
 class Checkpoint:
     """A matrix [rows, cols] kept in 8 bits: E4M3 codes in rows of 32 ceil(cols / 32) bytes and a power-of-two scale byte per block of 32
     elements of a row, [rows, ceil(cols / 32)].  codes (16-byte aligned) and scales are flat uint8 tensors."""
@@ -1000,8 +1002,8 @@ def linear_backward(dy, x, w, *, x_act="none", residual=None, need="xwb", dtype=
     """(dx, dw, db) of linear(x, w, bias) from dy [tokens, out], w [out, in] and x: the tensor [tokens, in] itself, or a Checkpoint.  With a
     Checkpoint v the layer's input was x_act(v) and is taken as x_act of the kept values, rounded to dy's type; dx is then the gradient by v,
     (dy w) x_act'(v).  residual [tokens, in]: added to dx (the gradient that reached the input another way).  dx has dy's type, dw [out, in]
-    and db [out] have dtype (float32 or dy's).  need: which of them ("x", "w", "b"); the others are None.  out: (dx, dw, db) to write
-    into, each may be None; none may lie over a tensor that another of the three still needs."""
+    and db [out] have dtype (float32 or dy's).  dx and dw take dy and w with either dimension in memory's order, db dy with its last.  need: which of them ("x", "w", "b"); the others are None.  out: (dx, dw, db) to write
+    into, each may be None; none may lie over a tensor, or a Checkpoint's buffers, that another of the three still needs."""
     code = _act_code(x_act)
     M, N, lda, a_t = _side(dy, "dy")
     Nw, K, ldb, b_t = _side(w, "w", (dy.dtype,))

@@ -17,7 +17,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 __device__ __forceinline__ float exp2_fast(float d) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
 __device__ __forceinline__ float rcp_fast(float d) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d)); return r; }
 
-// 1 / (1 + 2^-d).  The approximate power and reciprocal are off by about 2^-21 of the value at most, far below a 16-bit type's half step.
+// 1 / (1 + 2^-d).  The approximate power and reciprocal are off by about 2^-21 of the value at most, far below a 16-bit type's half step and eight of fp32's.  Values under
+// 2^-126 are taken as zero: silu below -87.3 is, where it is 1e-36 and less.
 __device__ __forceinline__ float logistic2(float d) { return rcp_fast(1.f + exp2_fast(-d)); }
 
 template <int ACT>

@@ -8,9 +8,11 @@
 // Two kernels.  mm_pair_kernel: pairs of multiprocessors on 256 x 256 tiles (cta_group::2), persistent, two sets of accumulators, for
 // large products.  mm_tile_kernel: a 128 x BN tile a block, the blocks of a cluster sharing one along k where there are few; with
 // SWAP the operand with few rows is the instruction's N side (16, 32 or 64), so that nothing is multiplied for rows that do not exist.
-// Bounds: large products the tensor cores and, over longer runs, the power limit (4096 x 8192 x 8192 348 us = 1.58 PFLOP/s in short runs, 420 to 440
-// in long ones, where a library's product of the same sizes takes 356 and 420); middling ones a block's chain of stages (300 cycles each: 256 of MMA) beside
+// Bounds: large products the tensor cores and, over longer runs, the power limit (4096 x 8192 x 8192 436 to 450 us in a user's calls one after
+// the other, where a library's product alone takes 420; in runs too short for the limit 348 us = 1.58 PFLOP/s and 356); middling ones a block's chain of stages (300 cycles each: 256 of MMA) beside
 // about 4 us of launch, set-up and tail (2048 x 1024 x 512 7.7 us, 600^3 6.7); few rows the weights' way from memory (1 x 4096 x 12288 20.3 us, floor 15.4).
+// The tensor cores add fp32 and round towards zero, in their own order: at k = 8192 a sum is 9e-6 of itself off on average (k = 512: 5e-7), a library's 16-bit
+// product exactly as much, sums in fp32 instructions 1e-6.  One bf16 result in 217 then comes out a place beside the rounded 64-bit value (fp32 sums: one in 1800).
 // Waits are bounded; where one runs out the tile is written as NaN.
 #pragma once
 #include <type_traits>

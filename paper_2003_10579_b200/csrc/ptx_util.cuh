@@ -200,7 +200,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {   // 
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok != 0;
 }
-// The warp's wait for a whole tile: one lane sleeps instead of polling, which leaves the issue slots to the others (4096 x 8192 x 8192: 128 us
+// The warp's wait for a whole tile: one lane sleeps instead of polling, which leaves the issue slots to the others (the 4-bit product of 4096 x 8192 x 8192: 128 us
 // polling, 113 us).  The limit is four seconds; the longest tile whose operands fit the memory takes 0.2 s.
 __device__ __forceinline__ bool mbar_wait_warp_long(uint32_t bar, uint32_t parity) {
   bool ok = false;

@@ -105,8 +105,9 @@ cudaError_t act_backward(const CkptArgs& a, sim_act act, dim3 grid, cudaStream_t
   if (a.codes) return a.vec ? act_backward_kept<T, true>(a, act, grid, st) : act_backward_kept<T, false>(a, act, grid, st);
   return a.vec ? launch_act_backward<T, ACT_NONE, false, true>(a, grid, st) : launch_act_backward<T, ACT_NONE, false, false>(a, grid, st);
 }
-// Blocks along the rows: at least 32 rows each (four a warp), up to four (a cluster, whose size is a power of two: clusters of three or seven blocks ran
-// slower than half as many), and from there no more than fill the device a few times over
+// Blocks along the rows: one for every 32 rows begun, rounded up to a power of two (so that each has 17 rows or more) up to the eight of a cluster, where three or
+// seven blocks ran slower than half as many; and from there no more than fill a B200's 148 multiprocessors a few times over (a constant: the workspace is asked
+// for without a device)
 int64_t sum_splits(int64_t rows, int64_t cols) {
   const int64_t strips = (cols + 255) / 256, most = (rows + 31) / 32, want = (8 * 148 + strips - 1) / strips;
   const int64_t s = most < want ? most : want;
@@ -254,7 +255,9 @@ Plan plan_of(int64_t M, int64_t N, int64_t K, int sms) {
   const int64_t ra = q.swap ? N : M, rb = q.swap ? M : N;
   const int kb = (int)((K + 63) / 64);
   // Pairs of multiprocessors where tiles of 128 x 128 would take turns (1008 x 1531 x 2736, 176 such tiles: 13.9 us against 18.1; 2048 x 2048 x 1200, 160:
-  // 16.1 against 16.0; 1536 x 8192 x 1664, 156: 42.7 against 44.1; 1800 x 64 x 1400, 165: 7.4 against 6.9; 1531 x 1008 x 2736, 264: 11.8 against 13.8).  Where each has a multiprocessor, not
+  // 16.1 against 16.0; 1536 x 8192 x 1664, 156: 42.7 against 44.1; 1531 x 1008 x 2736, 264: 11.8 against 13.8; 4000 x 64 x 4000, 1024: 15.0 against 15.9; 3000 x
+  // 128 x 3000, 576: 11.5 against 12.2).  The count of tiles alone is too coarse where k is short: 1800 x 64 x 1400, 165 tiles, 7.5 us against 7.0; 1800 x 512 x
+  // 1400 9.7 against 9.4; 1800 x 128 x 2500, 300 tiles, 80 of the pairs' 256 x 256 in two turns, 14.6 against 10.9.  Where each tile has a multiprocessor, not
   // (640 x 8192 x 3000, 120 tiles: 43 against 33; 300 x 4096 x 4096, 96: 24.6 against 18.5; 700 x 1024 x 3000, 144: 12.1 against 8.9)
   q.pair = kb > 0 && ra > 128 && rb > 128 && (ra + 127) / 128 * ((rb + 127) / 128) > sms;
   q.split = 1;
